@@ -13,7 +13,7 @@ BUILD_DIR = os.path.join(PKG, "_build")
 LIB_PATH = os.path.join(PKG, "libavsg.so")
 
 SOURCES = ["avsg_host.hip", "match_hash.hip", "match_dualptr.hip", "gather.hip", "step_pipelined.hip",
-           "step_early.hip"]
+           "step_early.hip", "latent_host.hip", "latent_cache.hip", "latent_attend.hip", "mx4.hip", "mx4_matmul.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
