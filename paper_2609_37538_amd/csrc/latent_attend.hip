@@ -1,96 +1,404 @@
-// Attention of a step's query tokens over latent cache rows.
+// Attention of a step's query tokens over latent cache rows:
+//   out = sum_i w_i v_i / sum_i w_i,  w_i = exp(scale q . k_i),
+// in one pass over the rows.  Every head of a token reads the same rows, and a
+// row's latent part is key and value at once, so a row is brought in once per
+// workgroup and serves up to 64 heads twice: 2 * (576 + 512) operations per row
+// and head, on the matrix cores.
 #include "latent_internal.h"
 
 namespace avsg {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kTile = 64;
+constexpr int kRowTile = 64;                  // rows of one pass through the loop
+constexpr int kRowWaves = kRowTile / 16;      // waves that share them, 16 each
+// LDS row of values: 1024 bytes and 32 more, so that the four rows whose
+// columns one group of 16 lanes reads at once lie in different banks
+constexpr int kValueStride = kLatent * 2 + 32;
+constexpr int kValueBytes = kRowTile * kValueStride;
+// Weights are kept relative to a reference that need not be the maximum: it is
+// raised only when a score passes it by this much (in powers of two), which in
+// float32 and bfloat16 costs no accuracy and saves the exchange of maxima
+// between waves for nearly every tile.
+constexpr float kSlack = 40.f;
 
-// One workgroup per (query token, head): 64 entries at a time, each wave takes
-// the scores of 16 of them (a lane has latent columns 8l..8l+7 and rotated
-// column l), then every thread adds the 64 rows, weighted, to two columns of the
-// output.  The sum is kept relative to the running maximum.
-template <bool kMx4>
-__global__ __launch_bounds__(kThreads) void attend_kernel(AttendParams p) {
-  __shared__ float score[kTile];
-  __shared__ uint64_t row_at[kTile];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t token = blockIdx.x;
-  const int head = blockIdx.y, r = static_cast<int>(token / p.n_q);
-  const __bf16* q = p.q + token * p.q_token_stride + head * p.q_head_stride;
-  float ql[8], qr = static_cast<float>(q[kLatent + lane]);
-  for (int i = 0; i < 8; ++i) ql[i] = static_cast<float>(q[8 * lane + i]);
+__device__ __align__(16) const unsigned char zero_row[kRowBytesBf16] = {};
+
+// What is known of a row before its address: loaded two tiles ahead.
+struct RowMeta {
+  int row, pos, page;
+};
+
+// kHeadTiles * 16 heads per workgroup; kHeadGroups groups of four waves.  In
+// the first half of a tile wave (rt, hg) multiplies the keys of its 16 rows with the
+// queries of its heads (held in registers), turns scores into weights, and
+// leaves the weights and its rows' values in LDS.  In the second half each wave
+// multiplies all 64 rows' weights of all heads with its own range of the 512
+// columns of the values.  Operands of the products:
+//   scores   A = keys     lane l: row l % 16, eight columns     B = queries  lane l: head l % 16, the same columns
+//            result lane l: head l % 16, rows (l / 16) * 4 .. + 3
+//   output   A = values^T lane l: column l % 16, eight rows     B = weights  lane l: head l % 16, the same rows
+//            result lane l: head l % 16, columns (l / 16) * 4 .. + 3
+// The eight rows of the second product are rows (l / 16) * 4 .. + 3 of two
+// 16-row tiles: what a lane holds of the first one's result, so weights need no
+// exchange within a wave.
+template <int kHeadTiles, int kHeadGroups, bool kMx4, bool kTwoBuffers>
+__global__ __launch_bounds__(256 * kHeadGroups, 2) void attend_kernel(AttendParams p, int head_blocks, int tiles_per_split) {
+  constexpr int kTiles = kHeadTiles / kHeadGroups;         // head tiles of a wave's scores
+  constexpr int kCols = kLatent / (kRowWaves * kHeadGroups);   // columns of a wave's output
+  constexpr int kColTiles = kCols / 16;
+  constexpr int kBuffers = kTwoBuffers ? 2 : 1;
+  constexpr int kWeightBytes = kHeadTiles * 2048;
+  constexpr int kKeySteps = kMx4 ? 4 : 16;
+  extern __shared__ __align__(16) unsigned char lds[];
+  unsigned char* const values = lds;
+  unsigned char* const weights = lds + kBuffers * kValueBytes;
+  float* const wave_top = reinterpret_cast<float*>(weights + kBuffers * kWeightBytes);   // [4][heads]
+  float* const reference = wave_top + kRowWaves * kHeadTiles * 16;                       // [heads]
+  int* const raised = reinterpret_cast<int*>(reference + kHeadTiles * 16);               // [2]
+
+  const int lane = threadIdx.x & 63, l16 = lane & 15, quad = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int rt = wave % kRowWaves, hg = wave / kRowWaves;
+
+  // workgroups of one request lie next to each other on one XCD, whose L2 then
+  // serves the rows that they share
+  const unsigned total = gridDim.x, per = total / kXcds, more = total % kXcds, xcd = blockIdx.x % kXcds;
+  const unsigned id = xcd * per + min(xcd, more) + blockIdx.x / kXcds;
+  const unsigned share = head_blocks * p.splits;
+  const int64_t token = id / share;
+  const int hb = (id % share) % head_blocks, split = (id % share) / head_blocks;
+  const int r = static_cast<int>(token / p.n_q);
+  const int head0 = hb * kHeadTiles * 16;
+
   const int64_t len = p.lens ? p.lens[token] : INT64_MAX;
-  float top = -INFINITY, total = 0.f, o[2] = {0.f, 0.f};
-  for (int first = 0; first < p.topk; first += kTile) {
-    __syncthreads();
-    if (threadIdx.x < kTile) {
-      const int i = first + threadIdx.x;
-      uint64_t at = 0;
-      if (i < p.topk) {
-        const int64_t pos = p.index ? p.index[token * p.topk + i] : i;
-        if (pos >= 0 && pos < len) at = cache_row(p.cache, r, p.rows ? p.rows[token * p.topk + i] : i);
-      }
-      row_at[threadIdx.x] = at;
+  // entries that can count: with their positions given, any
+  const int limit = p.index ? p.topk : static_cast<int>(len < 0 ? 0 : len < p.topk ? len : p.topk);
+  const int tile0 = split * tiles_per_split;
+  const int tiles = min(tiles_per_split, (limit + kRowTile - 1) / kRowTile - tile0);
+  const int32_t* const rows = p.rows ? p.rows + token * p.topk : nullptr;
+  const int32_t* const index = p.index ? p.index + token * p.topk : nullptr;
+
+  for (int i = threadIdx.x; i < kHeadTiles * 16; i += blockDim.x) reference[i] = -INFINITY;
+  if (threadIdx.x < 2) raised[threadIdx.x] = 0;
+
+  auto load_meta = [&](int t) {
+    RowMeta m{-1, -1, -1};
+    const int i = (tile0 + t) * kRowTile + rt * 16 + l16;
+    if (t < tiles && i < limit) {
+      m.row = rows ? rows[i] : i;
+      m.pos = index ? index[i] : i;
+      if (!rows && p.cache.table && i < p.cache.capacity)
+        m.page = p.cache.table[static_cast<int64_t>(r) * p.cache.pages_per_request + (i >> p.cache.page_shift)];
     }
-    __syncthreads();
-    for (int i = wave * 16; i < wave * 16 + 16; ++i) {
-      const uint64_t at = row_at[i];
-      float s = 0.f;
-      if (at != 0) {
-        bf16x8 x;
-        if constexpr (kMx4)
-          x = mx4_decode8(load_global<uint32_t>(at + 4 * lane),
-                          mx4_unit(load_global<uint8_t>(at + kMx4CodeBytes + lane / 4)));
-        else
-          x = load_global<bf16x8>(at + 16 * lane);
-        for (int k = 0; k < 8; ++k) s += ql[k] * static_cast<float>(x[k]);
-        s += qr * static_cast<float>(load_global<__bf16>(at + (kMx4 ? kMx4RopeAt : kLatent * 2) + 2 * lane));
-      }
-      for (int d = 32; d > 0; d /= 2) s += __shfl_xor(s, d);
-      if (lane == 0) score[i] = at != 0 ? s * p.scale : -INFINITY;
+    return m;
+  };
+  auto address = [&](const RowMeta& m) -> uint64_t {
+    if (m.row < 0 || m.row >= p.cache.capacity || m.pos < 0 || m.pos >= len) return 0;
+    int64_t page = m.page;
+    if (rows || !p.cache.table) {
+      page = static_cast<int64_t>(r) * p.cache.pages_per_request + (m.row >> p.cache.page_shift);
+      if (p.cache.table) page = p.cache.table[page];
     }
-    __syncthreads();
-    float high = top;
-    for (int i = 0; i < kTile; ++i)
-      if (row_at[i] != 0) high = fmaxf(high, score[i]);
-    const float base = high == -INFINITY ? 0.f : high, keep = expf(top - base);
-    if (top != -INFINITY) total *= keep, o[0] *= keep, o[1] *= keep;
-    for (int i = 0; i < kTile; ++i) {
-      const uint64_t at = row_at[i];
-      if (at == 0) continue;
-      const float w = expf(score[i] - base);
-      total += w;
-      bf16x2 v;
-      if constexpr (kMx4)
-        v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(
-            load_global<uint8_t>(at + threadIdx.x),
-            mx4_unit(load_global<uint8_t>(at + kMx4CodeBytes + threadIdx.x / 16)), 0);
-      else
-        v = load_global<bf16x2>(at + 4 * threadIdx.x);
-      o[0] += w * static_cast<float>(v[0]);
-      o[1] += w * static_cast<float>(v[1]);
+    if (page < 0 || page >= p.cache.pages) return 0;
+    return p.cache.base + page * p.cache.page_stride + (m.row & p.cache.page_mask) * p.cache.row_stride;
+  };
+
+  // 4-bit rows: step j has block 4j + quad, whose 16 bytes are four operands'
+  // columns; bfloat16 rows: step j has columns 32j + 8 quad.  Queries lie alike.
+  u32x4 key[kKeySteps], scales{}, turned[2];
+  unsigned counts = 0;   // bits of this lane's four rows (quad * 4 + i) that count
+  auto load_keys = [&](const RowMeta& m) {
+    uint64_t at = address(m);
+    counts = static_cast<unsigned>(__ballot(at != 0) >> (quad * 4)) & 15u;
+    if (at == 0) at = reinterpret_cast<uint64_t>(zero_row);
+    const uint64_t a = at + 16 * quad;
+#pragma unroll
+    for (int j = 0; j < kKeySteps; ++j) key[j] = load_global<u32x4>(a + 64 * j);
+    if constexpr (kMx4) scales = load_global<u32x4>(at + kMx4CodeBytes);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) turned[j] = load_global<u32x4>(a + (kMx4 ? kMx4RopeAt : kLatent * 2) + 64 * j);
+  };
+
+  RowMeta next = load_meta(0);
+  bf16x8 query[kTiles][18];
+#pragma unroll
+  for (int h = 0; h < kTiles; ++h) {
+    const int head = head0 + (hg * kTiles + h) * 16 + l16;
+    const bool there = head < p.heads;
+    const __bf16* q = p.q + token * p.q_token_stride + (there ? head : 0) * p.q_head_stride;
+#pragma unroll
+    for (int j = 0; j < 18; ++j) {
+      const int col = j >= 16 ? 32 * j + 8 * quad : kMx4 ? ((j / 4) * 4 + quad) * 32 + (j % 4) * 8 : 32 * j + 8 * quad;
+      query[h][j] = *reinterpret_cast<const bf16x8*>(q + col);
+      if (!there) query[h][j] = bf16x8{};
     }
-    top = high;
   }
-  const float by = total == 0.f ? 0.f : 1.f / total;
-  __bf16* out = p.out + token * p.out_token_stride + head * p.out_head_stride + 2 * threadIdx.x;
-  *reinterpret_cast<bf16x2*>(out) = bf16x2{static_cast<__bf16>(o[0] * by), static_cast<__bf16>(o[1] * by)};
-  if (p.lse && threadIdx.x == 0) p.lse[token * p.heads + head] = total == 0.f ? -INFINITY : top + logf(total);
+  load_keys(next);
+  next = load_meta(1);
+
+  const float scale = p.scale * 1.4426950408889634f;   // scores in powers of two
+  float ref[kTiles], sum[kTiles];
+#pragma unroll
+  for (int h = 0; h < kTiles; ++h) ref[h] = -INFINITY, sum[h] = 0.f;
+  f32x4 out[kColTiles][kHeadTiles];
+#pragma unroll
+  for (int c = 0; c < kColTiles; ++c)
+#pragma unroll
+    for (int h = 0; h < kHeadTiles; ++h) out[c][h] = f32x4{};
+
+  const unsigned value_to = (rt * 16 + l16) * kValueStride + 16 * quad;
+  const unsigned value_from = (quad * 4 + l16 / 4) * kValueStride + (wave * kCols + (l16 & 3) * 4) * 2;
+  const unsigned weight_to = hg * kTiles * 2048 + (rt >> 1) * 1024 + lane * 16 + (rt & 1) * 8;
+  __syncthreads();
+
+  for (int t = 0; t < tiles; ++t) {
+    const int buf = kTwoBuffers ? t & 1 : 0;
+    unsigned char* const v_lds = values + buf * kValueBytes;
+    unsigned char* const w_lds = weights + buf * kWeightBytes;
+    // one buffer: every wave is done with the last tile's
+    if constexpr (!kTwoBuffers) __syncthreads();
+
+    f32x4 score[kTiles][2];
+#pragma unroll
+    for (int h = 0; h < kTiles; ++h) score[h][0] = score[h][1] = f32x4{};
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      bf16x8 k;
+      if constexpr (kMx4) k = mx4_decode8(key[j / 4][j % 4], mx4_unit((scales[j / 4] >> (8 * quad)) & 255u));
+      else k = __builtin_bit_cast(bf16x8, key[j]);
+      // with two groups of waves on the same rows, each leaves half of the values
+      if (kHeadGroups == 1 || j / 8 == hg) {
+        const int at = kMx4 ? (j / 4) * 256 + 48 * quad + (j % 4) * 16 : 64 * j;
+        *reinterpret_cast<bf16x8*>(v_lds + value_to + at) = k;
+      }
+#pragma unroll
+      for (int h = 0; h < kTiles; ++h)
+        score[h][j & 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, query[h][j], score[h][j & 1], 0, 0, 0);
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int h = 0; h < kTiles; ++h)
+        score[h][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, turned[j]), query[h][16 + j],
+                                                              score[h][j], 0, 0, 0);
+    const unsigned now = counts;
+    load_keys(next);
+    next = load_meta(t + 2);
+
+    // weights relative to the reference as it is; a score far above it is noted
+    bool above = false;
+    f32x4 s[kTiles];
+    auto weigh = [&](int h) {
+      const float base = ref[h] == -INFINITY ? 0.f : ref[h];
+      bf16x4 w;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float e = (now >> i) & 1 ? __builtin_amdgcn_exp2f(s[h][i] - base) : 0.f;
+        sum[h] += e;
+        // rounded once; the sum keeps float32 weights, so the rounding errors
+        // of many rows cancel in the output and do not touch the sum
+        w[i] = static_cast<__bf16>(e);
+      }
+      *reinterpret_cast<bf16x4*>(w_lds + weight_to + h * 2048) = w;
+    };
+    float before[kTiles];
+#pragma unroll
+    for (int h = 0; h < kTiles; ++h) {
+      before[h] = sum[h];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        s[h][i] = (score[h][0][i] + score[h][1][i]) * scale;
+        above |= ((now >> i) & 1) && s[h][i] > ref[h] + kSlack;
+      }
+      weigh(h);
+    }
+    if (__any(above) && lane == 0) raised[t & 1] = t + 1;
+    __syncthreads();
+
+    if (raised[t & 1] == t + 1) {
+      // some score lies far above the reference: all waves agree on new ones and
+      // bring what they hold to them
+#pragma unroll
+      for (int h = 0; h < kTiles; ++h) {
+        float top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if ((now >> i) & 1) top = fmaxf(top, s[h][i]);
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        if (quad == 0) wave_top[rt * kHeadTiles * 16 + (hg * kTiles + h) * 16 + l16] = top;
+      }
+      __syncthreads();
+      float fresh[kHeadTiles];
+#pragma unroll
+      for (int h = 0; h < kHeadTiles; ++h) {
+        const float old = reference[h * 16 + l16];
+        float top = old;
+#pragma unroll
+        for (int w = 0; w < kRowWaves; ++w) top = fmaxf(top, wave_top[w * kHeadTiles * 16 + h * 16 + l16]);
+        const float by = old == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(old - top);
+        fresh[h] = top;
+#pragma unroll
+        for (int c = 0; c < kColTiles; ++c) out[c][h] = old == -INFINITY ? out[c][h] : out[c][h] * by;
+      }
+#pragma unroll
+      for (int h = 0; h < kTiles; ++h) {
+        float top = fresh[0];
+#pragma unroll
+        for (int g = 1; g < kHeadGroups; ++g) top = hg == g ? fresh[g * kTiles + h] : hg == 0 ? fresh[h] : top;
+        if constexpr (kHeadGroups == 1) top = fresh[h];
+        sum[h] = ref[h] == -INFINITY ? before[h] : before[h] * __builtin_amdgcn_exp2f(ref[h] - top);
+        ref[h] = top;
+        weigh(h);
+      }
+      __syncthreads();
+      // read again after the next tile's barrier at the earliest
+      if (wave == 0 && quad == 0) {
+#pragma unroll
+        for (int h = 0; h < kHeadTiles; ++h) reference[h * 16 + l16] = fresh[h];
+      }
+    }
+
+#pragma unroll
+    for (int pair = 0; pair < 2; ++pair) {
+      bf16x8 w[kHeadTiles];
+#pragma unroll
+      for (int h = 0; h < kHeadTiles; ++h)
+        w[h] = *reinterpret_cast<const bf16x8*>(w_lds + h * 2048 + pair * 1024 + lane * 16);
+#pragma unroll
+      for (int c = 0; c < kColTiles; ++c) {
+        typedef __attribute__((address_space(3))) bf16x4* lds_ptr;
+        const unsigned at = value_from + pair * 32 * kValueStride + c * 32;
+        const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_ptr)(v_lds + at));
+        const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_ptr)(v_lds + at + 16 * kValueStride));
+        const bf16x8 v{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+#pragma unroll
+        for (int h = 0; h < kHeadTiles; ++h)
+          out[c][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, w[h], out[c][h], 0, 0, 0);
+      }
+    }
+  }
+
+  // the waves' sums of weights
+  __syncthreads();
+#pragma unroll
+  for (int h = 0; h < kTiles; ++h) {
+    float x = sum[h];
+    x += __shfl_xor(x, 16);
+    x += __shfl_xor(x, 32);
+    if (quad == 0) wave_top[rt * kHeadTiles * 16 + (hg * kTiles + h) * 16 + l16] = x;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int h = 0; h < kHeadTiles; ++h) {
+    const int head = head0 + h * 16 + l16;
+    if (head >= p.heads) continue;
+    float all = 0.f;
+#pragma unroll
+    for (int w = 0; w < kRowWaves; ++w) all += wave_top[w * kHeadTiles * 16 + h * 16 + l16];
+    const float base = reference[h * 16 + l16];
+    const int col = wave * kCols + quad * 4;
+    if (p.splits > 1) {
+      const int64_t part = (token * p.splits + split) * p.heads + head;
+      if (wave == 0 && quad == 0) p.part_ml[part] = f32x2{base, all};
+      if (all != 0.f) {
+#pragma unroll
+        for (int c = 0; c < kColTiles; ++c)
+          *reinterpret_cast<f32x4*>(p.part_out + part * kLatent + col + c * 16) = out[c][h];
+      }
+      continue;
+    }
+    const float by = all == 0.f ? 0.f : 1.f / all;
+    __bf16* to = p.out + token * p.out_token_stride + head * p.out_head_stride + col;
+#pragma unroll
+    for (int c = 0; c < kColTiles; ++c) {
+      const f32x4 o = out[c][h] * by;
+      *reinterpret_cast<bf16x4*>(to + c * 16) =
+          bf16x4{static_cast<__bf16>(o[0]), static_cast<__bf16>(o[1]), static_cast<__bf16>(o[2]), static_cast<__bf16>(o[3])};
+    }
+    if (p.lse && wave == 0 && quad == 0)
+      p.lse[token * p.heads + head] =
+          all == 0.f ? -INFINITY : ((base == -INFINITY ? 0.f : base) + __builtin_amdgcn_logf(all)) * 0.6931471805599453f;
+  }
+}
+
+// Joins the parts of one (query token, head): four columns per thread.  Parts
+// without a row that counts hold no sums.
+__global__ __launch_bounds__(kLatent / 4) void combine_kernel(AttendParams p) {
+  const int64_t token = blockIdx.x / p.heads;
+  const int head = static_cast<int>(blockIdx.x - token * p.heads), col = threadIdx.x * 4;
+  const int64_t first = token * p.splits * p.heads + head;
+  float top = -INFINITY;
+  for (int i = 0; i < p.splits; ++i) {
+    const f32x2 ml = p.part_ml[first + static_cast<int64_t>(i) * p.heads];
+    if (ml[1] != 0.f) top = fmaxf(top, ml[0]);
+  }
+  const float base = top == -INFINITY ? 0.f : top;
+  float all = 0.f;
+  f32x4 o{};
+  for (int i = 0; i < p.splits; ++i) {
+    const int64_t part = first + static_cast<int64_t>(i) * p.heads;
+    const f32x2 ml = p.part_ml[part];
+    if (ml[1] == 0.f) continue;
+    const float w = __builtin_amdgcn_exp2f(ml[0] - base);
+    all += w * ml[1];
+    o += *reinterpret_cast<const f32x4*>(p.part_out + part * kLatent + col) * w;
+  }
+  o *= all == 0.f ? 0.f : 1.f / all;
+  *reinterpret_cast<bf16x4*>(p.out + token * p.out_token_stride + head * p.out_head_stride + col) =
+      bf16x4{static_cast<__bf16>(o[0]), static_cast<__bf16>(o[1]), static_cast<__bf16>(o[2]), static_cast<__bf16>(o[3])};
+  if (p.lse && threadIdx.x == 0)
+    p.lse[token * p.heads + head] = all == 0.f ? -INFINITY : (base + __builtin_amdgcn_logf(all)) * 0.6931471805599453f;
+}
+
+// Head tiles of a workgroup: the fewest that hold the heads, at most four.
+int head_tiles(int heads) { return heads <= 16 ? 1 : heads <= 32 ? 2 : 4; }
+
+template <int kHeadTiles, int kHeadGroups, bool kMx4, bool kTwoBuffers>
+hipError_t launch_one(const AttendParams& p, hipStream_t s) {
+  constexpr int kBuffers = kTwoBuffers ? 2 : 1;
+  constexpr size_t lds = kBuffers * (kValueBytes + kHeadTiles * 2048) + (kRowWaves + 1) * kHeadTiles * 16 * 4 + 16;
+  static_assert(lds <= 160 * 1024, "LDS of a workgroup");
+  const auto kernel = &attend_kernel<kHeadTiles, kHeadGroups, kMx4, kTwoBuffers>;
+  static const hipError_t ready =
+      hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lds));
+  if (ready != hipSuccess) return ready;
+  const int head_blocks = (p.heads + kHeadTiles * 16 - 1) / (kHeadTiles * 16);
+  const int tiles = (p.topk + kRowTile - 1) / kRowTile;
+  const int64_t groups = static_cast<int64_t>(p.cache.batch) * p.n_q * head_blocks * p.splits;
+  if (groups > INT32_MAX) return hipErrorInvalidValue;
+  kernel<<<dim3(static_cast<unsigned>(groups)), 256 * kHeadGroups, lds, s>>>(p, head_blocks, (tiles + p.splits - 1) / p.splits);
+  return hipGetLastError();
+}
+
+template <bool kMx4>
+hipError_t launch_format(const AttendParams& p, hipStream_t s) {
+  switch (head_tiles(p.heads)) {
+    case 1: return launch_one<1, 1, kMx4, false>(p, s);
+    case 2: return launch_one<2, 1, kMx4, false>(p, s);
+    default: return launch_one<4, 2, kMx4, true>(p, s);
+  }
 }
 
 }  // namespace
 
+// Splits so that every CU has work (two workgroups of up to 32 heads, one of
+// 64), but no part smaller than a tile.
 int attend_splits(int batch, int n_q, int heads, int topk) {
-  (void)batch, (void)n_q, (void)heads, (void)topk;
-  return 1;
+  constexpr int64_t kCus = 256;
+  const int per = head_tiles(heads);
+  const int64_t groups = static_cast<int64_t>(batch) * n_q * ((heads + per * 16 - 1) / (per * 16));
+  const int64_t want = (per == 4 ? kCus : 2 * kCus) / groups;
+  const int tiles = (topk + kRowTile - 1) / kRowTile;
+  if (want <= 1 || tiles <= 1) return 1;
+  const int64_t each = (tiles + want - 1) / want;
+  return static_cast<int>((tiles + each - 1) / each);
 }
 
 hipError_t launch_attend(const AttendParams& p, int format, hipStream_t s) {
-  const dim3 grid(static_cast<unsigned>(p.cache.batch * p.n_q), static_cast<unsigned>(p.heads));
-  if (format == 1) attend_kernel<true><<<grid, kThreads, 0, s>>>(p);
-  else attend_kernel<false><<<grid, kThreads, 0, s>>>(p);
+  hipError_t e = format == 1 ? launch_format<true>(p, s) : launch_format<false>(p, s);
+  if (e != hipSuccess || p.splits <= 1) return e;
+  combine_kernel<<<dim3(static_cast<unsigned>(p.cache.batch * p.n_q * p.heads)), kLatent / 4, 0, s>>>(p);
   return hipGetLastError();
 }
 
