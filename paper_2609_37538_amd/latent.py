@@ -134,50 +134,71 @@ def avsg_latent_last_error() -> str:
 
 # ---------------------------------------------------------------------------
 # wrappers (torch supplies device memory and streams)
+#
+# A small call's time on the GPU is a few microseconds, so the checks below are
+# written for the case that passes: one comparison each, and the text of an
+# error is put together only where there is one.
 # ---------------------------------------------------------------------------
+_t = None            # torch, once a wrapper is used
+_stream_of = None    # current stream of a GPU's index
+
+
+def _torch():
+    """torch, with the signatures of the library set."""
+    global _t, _stream_of
+    if _t is None:
+        import torch
+        load()
+        _stream_of = torch._C._cuda_getCurrentRawStream
+        _t = torch
+    return _t
+
+
 def _need(ok: bool, what: str) -> None:
     if not ok:
         raise ValueError(what)
 
 
-class _On:
-    """The current stream of a tensor's GPU, with that GPU current for the call."""
-
-    __slots__ = ("guard", "stream")
-
-    def __init__(self, device):
-        import torch
-        self.guard = None
-        if device.index is not None and device.index != torch.cuda.current_device():
-            self.guard = torch.cuda.device(device)
-        self.stream = torch.cuda.current_stream(device).cuda_stream
-
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-        return self.stream
-
-    def __exit__(self, *a):
-        if self.guard is not None:
-            self.guard.__exit__(*a)
+def _run(f, where: str, index: int, *args) -> None:
+    """Calls f on the current stream of GPU `index`, with that GPU current."""
+    if _t.cuda.current_device() == index:
+        rc = f(*args, _stream_of(index))
+    else:
+        with _t.cuda.device(index):
+            rc = f(*args, _stream_of(index))
+    if rc != 0:
+        _check(rc, where)
 
 
-def _ints(x, dtype, shape, device, what):
-    _need(x.dtype == dtype and x.device == device and x.is_contiguous() and tuple(x.shape) == tuple(shape),
-          f"{what} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {device}")
+def _ints(x, dtype, shape, device, what) -> int:
+    if x.dtype is not dtype or x.shape != shape or x.device != device or not x.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {device}")
     return x.data_ptr()
 
 
 def _vectors(x, shape, device, what):
-    """Checks a bfloat16 tensor whose vectors (last dimension) are read 16 bytes at a time."""
-    import torch
-    _need(x.dtype == torch.bfloat16 and x.device == device and tuple(x.shape) == tuple(shape),
-          f"{what} must be a bfloat16 tensor of shape {tuple(shape)} on {device}")
-    if x.numel():
-        _need(x.stride(-1) == 1 and x.data_ptr() % 16 == 0
-              and all(s % 8 == 0 or n == 1 for s, n in zip(x.stride()[:-1], x.shape[:-1])),
-              f"{what}: vectors must be contiguous and 16-byte aligned")
-    return [0 if n == 1 else s for s, n in zip(x.stride()[:-1], x.shape[:-1])]
+    """(address, strides) of a bfloat16 tensor whose vectors (last dimension) are read 16 bytes at a time."""
+    if x.dtype is not _t.bfloat16 or x.shape != shape or x.device != device:
+        raise ValueError(f"{what} must be a bfloat16 tensor of shape {tuple(shape)} on {device}")
+    at, strides = x.data_ptr(), x.stride()
+    if at & 15 or strides[-1] != 1 or any(map((7).__and__, strides[:-1])):
+        # strides of dimensions of one entry do not matter
+        strides = tuple(0 if n == 1 else st for st, n in zip(strides[:-1], shape)) + strides[-1:]
+        if x.numel() and (at & 15 or strides[-1] != 1 or any(st & 7 for st in strides[:-1])):
+            raise ValueError(f"{what}: vectors must be contiguous and 16-byte aligned")
+        if not x.numel():
+            strides = (0,) * len(shape)
+    return at, strides
+
+
+def _tokens(x, shape, device, what):
+    """(address, token stride, head stride) of a [B][n_q][H][...] tensor whose tokens lie at equal distances."""
+    at, (sb, st, sh, _) = _vectors(x, shape, device, what)
+    if shape[1] == 1:
+        return at, sb, sh
+    if shape[0] != 1 and sb != shape[1] * st:
+        raise ValueError(f"{what}: tokens must lie at equal distances")
+    return at, st, sh
 
 
 class LatentCache:
@@ -194,7 +215,7 @@ class LatentCache:
 
     def __init__(self, pool, batch: int, row_format: int, page_table=None, *, base: int = 0, pages: int = 0,
                  page_rows: int = 0, device=None):
-        import torch
+        torch = _torch()
         row = avsg_row_bytes(row_format)
         _need(row > 0, f"unknown row format {row_format}")
         _need(batch >= 1, "batch must be positive")
@@ -223,6 +244,7 @@ class LatentCache:
             per = pages // batch
         self.rows_per_request = per * page_rows
         self.c = AvsgCache(base, pages, page_stride, row_stride, row_format, batch, page_rows, per, table)
+        self._workspace = {}     # bytes by (n_q, heads, entries)
 
     @classmethod
     def of_slots(cls, operator, row_format: Optional[int] = None) -> "LatentCache":
@@ -236,34 +258,32 @@ class LatentCache:
         """Rotate `rope` [T][64] by the tokens' positions, bring `latent` [T][512] into the cache's
         format and write the rows (request [T] int32, position [T] int64).  angles: float32
         [positions][32][2], cosine and sine.  q_rope [T][H][64], rotated likewise, goes to q_out."""
-        import torch
-        t, dev = latent.shape[0], self.device
-        (ls,) = _vectors(latent, (t, AVSG_LATENT_DIM), dev, "latent")
-        (rs,) = _vectors(rope, (t, AVSG_ROPE_DIM), dev, "rope")
-        req = _ints(request, torch.int32, (t,), dev, "request")
-        pos = _ints(position, torch.int64, (t,), dev, "position")
-        ang = _ints(angles, torch.float32, (angles.shape[0], AVSG_ROPE_DIM // 2, 2), dev, "angles")
-        _need((q_rope is None) == (q_out is None), "q_rope and q_out go together")
-        heads = 0 if q_rope is None else q_rope.shape[1]
-        a = AvsgAppend(t, latent.data_ptr(), ls, rope.data_ptr(), rs, req, pos, ang, angles.shape[0], style, heads)
-        if heads:
-            a.q_token_stride, a.q_head_stride = _vectors(q_rope, (t, heads, AVSG_ROPE_DIM), dev, "q_rope")
-            a.q_out_token_stride, a.q_out_head_stride = _vectors(q_out, (t, heads, AVSG_ROPE_DIM), dev, "q_out")
-            a.d_q, a.d_q_out = q_rope.data_ptr(), q_out.data_ptr()
-        with _On(dev) as stream:
-            avsg_kv_append(self.c, a, stream)
+        t, dev, turns = latent.shape[0], self.device, angles.shape[0]
+        la, ls = _vectors(latent, (t, AVSG_LATENT_DIM), dev, "latent")
+        ra, rs = _vectors(rope, (t, AVSG_ROPE_DIM), dev, "rope")
+        req = _ints(request, _t.int32, (t,), dev, "request")
+        pos = _ints(position, _t.int64, (t,), dev, "position")
+        ang = _ints(angles, _t.float32, (turns, AVSG_ROPE_DIM // 2, 2), dev, "angles")
+        if q_rope is None:
+            _need(q_out is None, "q_rope and q_out go together")
+            a = AvsgAppend(t, la, ls[0], ra, rs[0], req, pos, ang, turns, style)
+        else:
+            _need(q_out is not None and q_rope.dim() == 3, "q_rope [T][H][64] and q_out go together")
+            shape = (t, q_rope.shape[1], AVSG_ROPE_DIM)
+            qa, qs = _vectors(q_rope, shape, dev, "q_rope")
+            oa, os_ = _vectors(q_out, shape, dev, "q_out")
+            a = AvsgAppend(t, la, ls[0], ra, rs[0], req, pos, ang, turns, style, shape[1], qa, qs[0], qs[1], oa, os_[0], os_[1])
+        _run(_lib.avsg_kv_append, "avsg_kv_append", dev.index, self.c, a)
 
     def read(self, request, position, out=None):
         """Rows as bfloat16 [n][576]; rows that do not exist read as zeros."""
-        import torch
         n, dev = request.shape[0], self.device
-        req = _ints(request, torch.int32, (n,), dev, "request")
-        pos = _ints(position, torch.int64, (n,), dev, "position")
+        req = _ints(request, _t.int32, (n,), dev, "request")
+        pos = _ints(position, _t.int64, (n,), dev, "position")
         if out is None:
-            out = torch.empty((n, KEY_DIM), dtype=torch.bfloat16, device=dev)
-        (stride,) = _vectors(out, (n, KEY_DIM), dev, "out")
-        with _On(dev) as stream:
-            avsg_kv_read(self.c, n, req, pos, out.data_ptr(), stride, stream)
+            out = _t.empty((n, KEY_DIM), dtype=_t.bfloat16, device=dev)
+        at, st = _vectors(out, (n, KEY_DIM), dev, "out")
+        _run(_lib.avsg_kv_read, "avsg_kv_read", dev.index, self.c, n, req, pos, at, st[0])
         return out
 
     def attend(self, q, rows=None, index=None, lens=None, *, scale: float, longest: Optional[int] = None, out=None,
@@ -275,63 +295,52 @@ class LatentCache:
         index: int32 [B][n_q][K] their positions (the step's selections), or None: entry i has
             position i.
         lens: int64 [B][n_q] positions a query token may see, or None: all."""
-        import torch
         dev = self.device
         _need(q.dim() == 4, "q must be [batch][n_q][heads][576]")
-        b, n_q, heads = q.shape[0], q.shape[1], q.shape[2]
-        _need(b == self.batch and n_q >= 1 and heads >= 1, f"q must hold {self.batch} requests, and a token and a head")
+        b, n_q, heads, _ = q.shape
+        if b != self.batch or n_q < 1 or heads < 1:
+            raise ValueError(f"q must hold {self.batch} requests, and a token and a head")
         if rows is not None:
+            _need(longest is None, "longest goes with rows=None")
             k = rows.shape[-1]
         elif index is not None:
             k = index.shape[-1]
         else:
             k = self.rows_per_request if longest is None else longest
-        _need(rows is None or longest is None, "longest goes with rows=None")
         _need(0 <= k <= 0x7fffffff, "too many entries")
-        a = AvsgAttention(n_q, heads, k, scale)
-        a.q_token_stride, a.q_head_stride = self._tokens(q, (b, n_q, heads, KEY_DIM), "q")
-        a.d_q = q.data_ptr()
-        if rows is not None:
-            a.d_rows = _ints(rows, torch.int32, (b, n_q, k), dev, "rows") if k else None
-        if index is not None:
-            a.d_index = _ints(index, torch.int32, (b, n_q, k), dev, "index") if k else None
-        if lens is not None:
-            a.d_lens = _ints(lens, torch.int64, (b, n_q), dev, "lens")
+        qa, qt, qh = _tokens(q, (b, n_q, heads, KEY_DIM), dev, "q")
+        rows_at = None if rows is None else _ints(rows, _t.int32, (b, n_q, k), dev, "rows")
+        index_at = None if index is None else _ints(index, _t.int32, (b, n_q, k), dev, "index")
+        lens_at = None if lens is None else _ints(lens, _t.int64, (b, n_q), dev, "lens")
         if out is None:
-            out = torch.empty((b, n_q, heads, AVSG_LATENT_DIM), dtype=torch.bfloat16, device=dev)
-        a.out_token_stride, a.out_head_stride = self._tokens(out, (b, n_q, heads, AVSG_LATENT_DIM), "out")
-        a.d_out = out.data_ptr()
+            out = _t.empty((b, n_q, heads, AVSG_LATENT_DIM), dtype=_t.bfloat16, device=dev)
+        oa, ot, oh = _tokens(out, (b, n_q, heads, AVSG_LATENT_DIM), dev, "out")
         if lse is None:
-            lse = torch.empty((b, n_q, heads), dtype=torch.float32, device=dev)
-        a.d_lse = _ints(lse, torch.float32, (b, n_q, heads), dev, "lse")
-        need = avsg_attend_workspace_bytes(b, n_q, heads, k)
-        ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
-        with _On(dev) as stream:
-            avsg_attend(self.c, a, ws.data_ptr() if need else None, need, stream)
+            lse = _t.empty((b, n_q, heads), dtype=_t.float32, device=dev)
+        lse_at = _ints(lse, _t.float32, (b, n_q, heads), dev, "lse")
+        need = self._workspace.get((n_q, heads, k))
+        if need is None:
+            need = self._workspace[n_q, heads, k] = avsg_attend_workspace_bytes(b, n_q, heads, k)
+        ws = _t.empty(need, dtype=_t.uint8, device=dev) if need else None
+        a = AvsgAttention(n_q, heads, k, scale, qa, qt, qh, rows_at, index_at, lens_at, oa, ot, oh, lse_at)
+        _run(_lib.avsg_attend, "avsg_attend", dev.index, self.c, a, ws.data_ptr() if need else None, need)
         return out, lse
-
-    def _tokens(self, x, shape, what):
-        """(token stride, head stride) of a [B][n_q][H][...] tensor whose tokens lie at equal distances."""
-        sb, st, sh = _vectors(x, shape, self.device, what)
-        b, n_q = shape[0], shape[1]
-        _need(b == 1 or n_q == 1 or sb == n_q * st, f"{what}: tokens must lie at equal distances")
-        return (st if n_q > 1 else sb), sh
 
 
 class Mx4:
     """A matrix or a batch of them in 4-bit microscaled form: codes uint8 [..., K/2] (column 2i in
     the low half of byte i) and scales uint8 [..., K/32]."""
 
-    __slots__ = ("codes", "scales")
+    __slots__ = ("codes", "scales", "_view")
 
     def __init__(self, codes, scales):
-        import torch
+        torch = _torch()
         _need(codes.dtype == torch.uint8 and scales.dtype == torch.uint8 and codes.is_cuda
               and codes.device == scales.device, "codes and scales must be uint8 tensors on one GPU")
         _need(codes.dim() in (2, 3) and codes.shape[:-1] == scales.shape[:-1]
               and codes.shape[-1] == scales.shape[-1] * (AVSG_MX4_BLOCK // 2),
               "codes [..., K/2] and scales [..., K/32] must belong together and have two or three dimensions")
-        self.codes, self.scales = codes, scales
+        self.codes, self.scales, self._view = codes, scales, None
 
     @property
     def shape(self):
@@ -342,78 +351,89 @@ class Mx4:
         """With two leading dimensions exchanged (the columns stay in place)."""
         n = self.codes.dim()
         _need(i % n != n - 1 and j % n != n - 1, "columns cannot be exchanged: blocks lie along them")
-        return Mx4(self.codes.transpose(i, j), self.scales.transpose(i, j))
+        return _mx4(self.codes.transpose(i, j), self.scales.transpose(i, j))
 
-    def _c(self, what: str) -> AvsgMx4:
-        c, s = self.codes, self.scales
-        if c.numel():
-            _need(c.stride(-1) == 1 and (s.stride(-1) == 1 or s.shape[-1] == 1) and c.data_ptr() % 16 == 0
-                  and all(st % 16 == 0 or n == 1 for st, n in zip(c.stride()[:-1], c.shape[:-1])),
-                  f"{what}: rows of codes must be contiguous and 16-byte aligned")
-        else:
-            return AvsgMx4(c.data_ptr(), s.data_ptr(), 0, 0, 0, 0)
-        three = c.dim() == 3
-        return AvsgMx4(c.data_ptr(), s.data_ptr(), c.stride(-2) if c.shape[-2] > 1 else 0,
-                       c.stride(0) if three and c.shape[0] > 1 else 0, s.stride(-2) if s.shape[-2] > 1 else 0,
-                       s.stride(0) if three and s.shape[0] > 1 else 0)
+    def _c(self) -> AvsgMx4:
+        """The matrix as the library takes it; made once, for codes and scales do not move."""
+        if self._view is None:
+            c, s = self.codes, self.scales
+            if not c.numel():
+                self._view = AvsgMx4(c.data_ptr(), s.data_ptr(), 0, 0, 0, 0)
+                return self._view
+            cs = [0 if n == 1 else st for st, n in zip(c.stride(), c.shape)]
+            ss = [0 if n == 1 else st for st, n in zip(s.stride(), s.shape)]
+            _need(c.stride(-1) == 1 and ss[-1] <= 1 and c.data_ptr() & 15 == 0 and all(st % 16 == 0 for st in cs[:-1]),
+                  "rows of codes must be contiguous and 16-byte aligned")
+            three = len(cs) == 3
+            self._view = AvsgMx4(c.data_ptr(), s.data_ptr(), cs[-2], cs[0] if three else 0, ss[-2], ss[0] if three else 0)
+        return self._view
+
+
+def _mx4(codes, scales) -> Mx4:
+    """An Mx4 of tensors that are known to belong together."""
+    m = Mx4.__new__(Mx4)
+    m.codes, m.scales, m._view = codes, scales, None
+    return m
 
 
 def _plain_type(x, what):
-    import torch
-    _need(x.is_cuda and x.dtype in (torch.bfloat16, torch.float32), f"{what} must be a bfloat16 or float32 cuda tensor")
-    return AVSG_BF16 if x.dtype == torch.bfloat16 else AVSG_F32
+    if x.dtype is _t.bfloat16 and x.is_cuda:
+        return AVSG_BF16
+    _need(x.is_cuda and x.dtype is _t.float32, f"{what} must be a bfloat16 or float32 cuda tensor")
+    return AVSG_F32
 
 
 def mx4_quantize(x) -> Mx4:
     """4-bit form of x, [R][K] or [A][R][K] with K a multiple of 32, in bfloat16 or float32."""
-    import torch
+    torch = _t or _torch()
     dtype = _plain_type(x, "x")
-    _need(x.dim() in (2, 3) and x.shape[-1] % AVSG_MX4_BLOCK == 0, "x must be [..., K] with K a multiple of 32")
-    k = x.shape[-1]
-    rows = x.numel() // k if k else 0
-    _need(x.dim() == 2 or x.shape[0] == 1 or x.shape[1] == 1 or x.stride(0) == x.shape[1] * x.stride(1),
-          "x: rows must lie at equal distances")
-    many = x.dim() - 2 if x.shape[-2] > 1 else 0
-    stride = x.stride(many) if rows > 1 else 0
-    _need(not x.numel() or (x.stride(-1) == 1 and x.data_ptr() % 16 == 0 and stride * x.element_size() % 16 == 0),
-          "x: rows must be contiguous and 16-byte aligned")
-    codes = torch.empty((*x.shape[:-1], k // 2), dtype=torch.uint8, device=x.device)
-    scales = torch.empty((*x.shape[:-1], k // AVSG_MX4_BLOCK), dtype=torch.uint8, device=x.device)
-    with _On(x.device) as stream:
-        avsg_mx4_quantize(x.data_ptr(), dtype, rows, k, stride, codes.data_ptr(), scales.data_ptr(), stream)
-    return Mx4(codes, scales)
+    shape, dev = x.shape, x.device
+    dims, k = len(shape), shape[-1]
+    _need(dims in (2, 3) and k % AVSG_MX4_BLOCK == 0, "x must be [..., K] with K a multiple of 32")
+    rows = shape[0] * shape[1] if dims == 3 else shape[0]
+    if x.is_contiguous():
+        stride = k
+    else:
+        _need(dims == 2 or shape[0] == 1 or shape[1] == 1 or x.stride(0) == shape[1] * x.stride(1),
+              "x: rows must lie at equal distances")
+        stride = x.stride(dims - 2 if shape[-2] > 1 else 0) if rows > 1 else 0
+        _need(not rows * k or x.stride(-1) == 1 and stride * (2 if dtype == AVSG_BF16 else 4) % 16 == 0,
+              "x: rows must be contiguous and 16-byte aligned")
+    at = x.data_ptr()
+    _need(at & 15 == 0, "x: rows must be 16-byte aligned")
+    codes = torch.empty((*shape[:-1], k // 2), dtype=torch.uint8, device=dev)
+    scales = torch.empty((*shape[:-1], k // AVSG_MX4_BLOCK), dtype=torch.uint8, device=dev)
+    _run(_lib.avsg_mx4_quantize, "avsg_mx4_quantize", dev.index, at, dtype, rows, k, stride, codes.data_ptr(),
+         scales.data_ptr())
+    return _mx4(codes, scales)
 
 
 def mx4_dequantize(m: Mx4, dtype=None):
     """The values that a contiguous Mx4 stands for, in bfloat16 (the default) or float32."""
-    import torch
-    out = torch.empty(m.shape, dtype=dtype or torch.bfloat16, device=m.codes.device)
-    kind = _plain_type(out, "dtype")
-    _need(m.codes.is_contiguous() and m.scales.is_contiguous(), "codes and scales must be contiguous")
-    k = m.shape[-1]
-    c = AvsgMx4(m.codes.data_ptr(), m.scales.data_ptr(), k // 2, 0, k // AVSG_MX4_BLOCK, 0)
-    with _On(out.device) as stream:
-        avsg_mx4_dequantize(c, out.numel() // k if k else 0, k, out.data_ptr(), kind, k, stream)
+    codes, scales = m.codes, m.scales
+    _need(codes.is_contiguous() and scales.is_contiguous(), "codes and scales must be contiguous")
+    out = _t.empty(m.shape, dtype=dtype or _t.bfloat16, device=codes.device)
+    kind, k = _plain_type(out, "dtype"), out.shape[-1]
+    _run(_lib.avsg_mx4_dequantize, "avsg_mx4_dequantize", codes.device.index,
+         AvsgMx4(codes.data_ptr(), scales.data_ptr(), k // 2, 0, k // AVSG_MX4_BLOCK, 0),
+         out.numel() // k if k else 0, k, out.data_ptr(), kind, k)
     return out
 
 
 def mx4_matmul(a: Mx4, b: Mx4, out=None, dtype=None):
     """a b^T for a [M][K] and b [N][K], or for batches of both; `out` ([M][N] or [batch][M][N],
     bfloat16 or float32, rows contiguous) or a new tensor of `dtype` (bfloat16)."""
-    import torch
-    _need(a.codes.dim() == b.codes.dim() and a.shape[-1] == b.shape[-1] and a.codes.device == b.codes.device,
-          "a and b must have the same dimensions, columns and GPU")
-    three = a.codes.dim() == 3
-    batch = a.shape[0] if three else 1
-    _need(not three or b.shape[0] == batch, "a and b must have the same batch")
-    m, n, k = a.shape[-2], b.shape[-2], a.shape[-1]
-    shape = (batch, m, n) if three else (m, n)
+    sa, sb, dev = a.shape, b.shape, a.codes.device
+    three = len(sa) == 3
+    if len(sa) != len(sb) or sa[-1] != sb[-1] or dev != b.codes.device or (three and sa[0] != sb[0]):
+        raise ValueError("a and b must have the same dimensions, batch, columns and GPU")
+    shape = (*sa[:-1], sb[-2])
     if out is None:
-        out = torch.empty(shape, dtype=dtype or torch.bfloat16, device=a.codes.device)
-    _need(tuple(out.shape) == shape and out.device == a.codes.device and (n <= 1 or out.stride(-1) == 1),
-          f"out must be {shape} on {a.codes.device} with contiguous rows")
+        out = _t.empty(shape, dtype=dtype or _t.bfloat16, device=dev)
+    st = out.stride()
+    if out.shape != shape or out.device != dev or (shape[-1] > 1 and st[-1] != 1):
+        raise ValueError(f"out must be {shape} on {dev} with contiguous rows")
     kind = _plain_type(out, "out")
-    with _On(out.device) as stream:
-        avsg_mx4_matmul(a._c("a"), b._c("b"), batch, m, n, k, out.data_ptr(), kind, out.stride(-2),
-                        out.stride(0) if three else 0, stream)
+    _run(_lib.avsg_mx4_matmul, "avsg_mx4_matmul", dev.index, a._c(), b._c(), sa[0] if three else 1, shape[-2], shape[-1],
+         sa[-1], out.data_ptr(), kind, st[-2], st[0] if three else 0)
     return out
