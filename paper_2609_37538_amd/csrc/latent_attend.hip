@@ -4,367 +4,564 @@
 // row's latent part is key and value at once, so a row is brought in once per
 // workgroup and serves up to 64 heads twice: 2 * (576 + 512) operations per row
 // and head, on the matrix cores.
+#include <type_traits>
+
 #include "latent_internal.h"
 
 namespace avsg {
 namespace {
 
-constexpr int kRowTile = 64;                  // rows of one pass through the loop
-constexpr int kRowWaves = kRowTile / 16;      // waves that share them, 16 each
-// LDS row of values: 1024 bytes and 32 more, so that the four rows whose
-// columns one group of 16 lanes reads at once lie in different banks
-constexpr int kValueStride = kLatent * 2 + 32;
+constexpr int kRowTile = 64;                  // rows of one pass through the narrow kernel's loop
+// Values in LDS: rows of 1024 bytes.  Of every 256 bytes (all banks) row x has
+// its 32-byte pieces exchanged by x mod 8 and the halves of a piece by bit 3 of
+// x.  Sixteen lanes that write 16 bytes each of the same columns of 16 rows, and
+// groups of 16 lanes that read 32 bytes each of four rows, then meet every
+// bank equally often.
+constexpr int kValueStride = kLatent * 2;
 constexpr int kValueBytes = kRowTile * kValueStride;
+// Byte of a row's 256 at which 16-byte part `part` lies.
+__device__ __forceinline__ unsigned value_part(unsigned row, unsigned part) {
+  return ((part ^ ((row & 7) * 2 + ((row >> 3) & 1))) & 15) * 16;
+}
 // Weights are kept relative to a reference that need not be the maximum: it is
 // raised only when a score passes it by this much (in powers of two), which in
 // float32 and bfloat16 costs no accuracy and saves the exchange of maxima
 // between waves for nearly every tile.
 constexpr float kSlack = 40.f;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
+// The order in which the compiler is to issue what stands before in a block:
+// the next `n` instructions of a kind.
+constexpr int kVector = 0x2, kMatrix = 0x8, kLdsRead = 0x100, kLdsWrite = 0x200;
+#define kSchedule(kind, n) __builtin_amdgcn_sched_group_barrier(kind, n, 0)
+
+// What the loads of entries that do not count read in place of a row.
 __device__ __align__(16) const unsigned char zero_row[kRowBytesBf16] = {};
 
-// What is known of a row before its address: loaded two tiles ahead.
-struct RowMeta {
-  int row, pos, page;
+__device__ __forceinline__ float zero_if_none(float reference) { return reference == -INFINITY ? 0.f : reference; }
+
+__device__ __forceinline__ bf16x4 rounded(f32x4 x) {
+  return bf16x4{static_cast<__bf16>(x[0]), static_cast<__bf16>(x[1]), static_cast<__bf16>(x[2]), static_cast<__bf16>(x[3])};
+}
+
+// A lane's number that the compiler takes for a new value: what is derived from
+// it is computed where it is used and not kept in registers across the loop.
+__device__ __forceinline__ int lane_here() {
+  int x = threadIdx.x & 63;
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
+// A workgroup's share of the work: a block of heads of one query token over a
+// run of tiles of its entries.
+struct Share {
+  int64_t token, len;
+  int request, head_block, split, tile0, tiles, limit;
 };
 
-// kHeadTiles * 16 heads per workgroup; kKeyGroups groups of four waves.  In the
-// first half of a tile wave (rt, kg) multiplies its share of the columns of the
-// keys of its 16 rows with the queries (held in registers) and leaves the
-// values that it expanded on the way in LDS.  With two groups the halves of a
-// score meet in LDS, each group taking half of the heads.  Scores become weights,
-// which go to LDS.  In the second half each wave multiplies all 64 rows' weights
-// of all heads with its own range of the 512 columns of the values.  Operands of
-// the products:
+__device__ __forceinline__ Share share_of(const AttendParams& p, int head_blocks, int tiles_per_split, int tile_rows) {
+  Share w;
+  // workgroups of one request lie next to each other on one XCD, whose L2 then
+  // serves the rows that they share
+  const unsigned total = gridDim.x, per = total / kXcds, more = total % kXcds, xcd = blockIdx.x % kXcds;
+  const unsigned id = xcd * per + min(xcd, more) + blockIdx.x / kXcds;
+  const unsigned share = head_blocks * p.splits;
+  w.token = id / share;
+  w.head_block = (id % share) % head_blocks;
+  w.split = (id % share) / head_blocks;
+  w.request = static_cast<int>(w.token / p.n_q);
+  w.len = p.lens ? p.lens[w.token] : INT64_MAX;
+  // entries that can count: with their positions given, any
+  w.limit = p.index ? p.topk : static_cast<int>(w.len < 0 ? 0 : w.len < p.topk ? w.len : p.topk);
+  w.tile0 = w.split * tiles_per_split;
+  w.tiles = min(tiles_per_split, (w.limit + tile_rows - 1) / tile_rows - w.tile0);
+  return w;
+}
+
+// One wave finds rows, 64 at a time, one per lane: what is read of them comes
+// first, some tiles later their addresses go to LDS, and all waves fetch their
+// keys a tile ahead.
+struct RowFinder {
+  int row, pos, page;   // of this lane's row of those looked at last
+
+  __device__ __forceinline__ void look(const AttendParams& p, const Share& w, int t, int tile_rows) {
+    row = pos = page = -1;
+    const int i = (w.tile0 + t) * tile_rows + lane_here();
+    if (i >= w.limit || i >= (w.tile0 + w.tiles) * tile_rows) return;
+    row = p.rows ? p.rows[w.token * p.topk + i] : i;
+    pos = p.index ? p.index[w.token * p.topk + i] : i;
+    if (!p.rows && p.cache.table && i < p.cache.capacity)
+      page = p.cache.table[static_cast<int64_t>(w.request) * p.cache.pages_per_request + (i >> p.cache.page_shift)];
+  }
+  // the address of that row, 0 where it does not count
+  __device__ __forceinline__ uint64_t address(const AttendParams& p, const Share& w) const {
+    const CacheView& c = p.cache;
+    if (row < 0 || row >= c.capacity || pos < 0 || pos >= w.len) return 0;
+    int64_t at = page;
+    if (p.rows || !c.table) {
+      at = static_cast<int64_t>(w.request) * c.pages_per_request + (row >> c.page_shift);
+      if (c.table) at = c.table[at];
+    }
+    if (at < 0 || at >= c.pages) return 0;
+    return c.base + at * c.page_stride + (row & c.page_mask) * c.row_stride;
+  }
+};
+
+typedef __attribute__((address_space(3))) bf16x4* lds_bf16x4;
+
+// Operand of the output product: columns l % 16 of a 16-column tile, of rows
+// quad * 4 .. + 3 of two 16-row tiles that follow each other.  `at`: this lane's
+// place in the first.
+__device__ __forceinline__ bf16x8 load_values(const unsigned char* lds, unsigned at) {
+  const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4)(lds + at));
+  const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4)(lds + at + 16 * kValueStride));
+  return bf16x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+}
+// That place for a wave whose columns start at `col`, a multiple of 64.
+__device__ __forceinline__ unsigned values_from(int lane, int col) {
+  const unsigned row = (lane >> 4) * 4 + (lane & 15) / 4;
+  return row * kValueStride + (col * 2 & ~255) + value_part(row, col / 8 % 16 + (lane & 3) / 2) + (lane & 1) * 8;
+}
+
+// Queries take the scale's sign (or its zero), so that with a positive scale
+// products compare like scores.
+__device__ __forceinline__ bf16x8 load_query(const AttendParams& p, const Share& w, int head, int col) {
+  const bool there = head < p.heads;
+  bf16x8 x = *reinterpret_cast<const bf16x8*>(p.q + w.token * p.q_token_stride + (there ? head : 0) * p.q_head_stride + col);
+  if (!there || p.scale == 0.f) x = bf16x8{};
+  return p.scale < 0.f ? -x : x;
+}
+
+// Result of one head: four columns of every column tile of a wave, whose sum
+// of weights is `all` relative to `reference`.
+template <int kColTiles, typename Out>
+__device__ __forceinline__ void store_head(const AttendParams& p, const Share& w, int head, int col, Out out, float reference,
+                                           float all, bool first) {
+  if (p.splits > 1) {
+    const int64_t part = (w.token * p.splits + w.split) * p.heads + head;
+    if (first) p.part_ml[part] = f32x2{reference, all};
+    if (all != 0.f) {
+#pragma unroll
+      for (int c = 0; c < kColTiles; ++c) *reinterpret_cast<f32x4*>(p.part_out + part * kLatent + col + c * 16) = out(c);
+    }
+    return;
+  }
+  const float by = all == 0.f ? 0.f : 1.f / all;
+  __bf16* to = p.out + w.token * p.out_token_stride + head * p.out_head_stride + col;
+#pragma unroll
+  for (int c = 0; c < kColTiles; ++c) *reinterpret_cast<bf16x4*>(to + c * 16) = rounded(out(c) * by);
+  if (p.lse && first)
+    p.lse[w.token * p.heads + head] = all == 0.f ? -INFINITY : (zero_if_none(reference) + __builtin_amdgcn_logf(all)) * kLn2;
+}
+
+// Operands of the products, in both kernels below:
 //   scores   A = keys     lane l: row l % 16, eight columns     B = queries  lane l: head l % 16, the same columns
 //            result lane l: head l % 16, rows (l / 16) * 4 .. + 3
 //   output   A = values^T lane l: column l % 16, eight rows     B = weights  lane l: head l % 16, the same rows
 //            result lane l: head l % 16, columns (l / 16) * 4 .. + 3
 // The eight rows of the second product are rows (l / 16) * 4 .. + 3 of two
 // 16-row tiles: what a lane holds of the first one's result, so weights need no
-// exchange within a wave.
-// 64 heads: queries and output of a wave fill 208 of the 256 registers that two
-// waves per SIMD leave; splitting the keys' columns (not the heads) between the
-// groups leaves each wave half of the keys to load and to expand.
-template <int kHeadTiles, int kKeyGroups, bool kMx4>
-__global__ __launch_bounds__(256 * kKeyGroups, 2) void attend_kernel(AttendParams p, int head_blocks, int tiles_per_split) {
-  constexpr int kTiles = kHeadTiles / kKeyGroups;              // head tiles whose weights a wave makes
-  constexpr int kCols = kLatent / (kRowWaves * kKeyGroups);    // columns of a wave's output
-  constexpr int kColTiles = kCols / 16;
-  constexpr int kValueBuffers = kKeyGroups;
-  constexpr int kWeightBytes = kHeadTiles * 2048;
-  constexpr int kHalves = 2 / kKeyGroups;                      // of the key columns, a wave's share
-  constexpr int kLoads = (kMx4 ? 2 : 8) * kHalves;             // 16 bytes each
-  constexpr int kSteps = 8 * kHalves;                          // products over 32 latent columns
-  constexpr int kChains = kHeadTiles == 1 ? 2 : 1;             // sums that a head tile's products alternate between
+// exchange within a wave.  Of the 4-bit latent columns a lane has blocks of 32
+// (16 bytes, four products' eight columns each), of bfloat16 ones eight columns
+// of every 32.
+
+// Up to 16 heads.  Four waves score 16 rows each against all 576 columns, leave
+// weights and expanded values in LDS, and take 128 of the 512 columns each of the
+// output.  So few heads make the rows' bytes count, and two workgroups per CU
+// keep 50 KB of them in flight.
+template <bool kMx4>
+__global__ __launch_bounds__(256, 2) void attend_kernel(AttendParams p, int tiles_per_split) {
+  constexpr int kWaves = 4, kCols = kLatent / kWaves, kColTiles = kCols / 16;
+  constexpr int kLoads = kMx4 ? 4 : 16;
   extern __shared__ __align__(16) unsigned char lds[];
   unsigned char* const values = lds;
-  unsigned char* const weights = lds + kValueBuffers * kValueBytes;
-  float* const wave_top = reinterpret_cast<float*>(weights + kWeightBytes);   // [4][heads]
-  float* const reference = wave_top + kRowWaves * kHeadTiles * 16;            // [heads]
-  int* const raised = reinterpret_cast<int*>(reference + kHeadTiles * 16);    // [4]
-  unsigned char* const halves = reinterpret_cast<unsigned char*>(raised + 4); // two groups: [4][2][kTiles][64] f32x4
+  unsigned char* const weights = lds + kValueBytes;                              // [2][64 lanes] 16 bytes
+  uint64_t* const row_at = reinterpret_cast<uint64_t*>(weights + 2048);          // [2][64]: rows of a tile, 0 = none
+  float* const wave_top = reinterpret_cast<float*>(row_at + 2 * kRowTile);       // [4][16]
+  float* const reference = wave_top + kWaves * 16;                               // [16]
+  int* const raised = reinterpret_cast<int*>(reference + 16);                    // [4]
 
   const int lane = threadIdx.x & 63, l16 = lane & 15, quad = lane >> 4;
-  // A lane's number that the compiler takes for a new value: what is derived from
-  // it is computed where it is used and not kept in registers across the loop.
-  auto here = [&]() {
-    int x = lane;
-    asm volatile("" : "+v"(x));
-    return x;
-  };
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int rt = wave % kRowWaves, kg = wave / kRowWaves;
+  const Share w = share_of(p, 1, tiles_per_split, kRowTile);
 
-  // workgroups of one request lie next to each other on one XCD, whose L2 then
-  // serves the rows that they share
-  const unsigned total = gridDim.x, per = total / kXcds, more = total % kXcds, xcd = blockIdx.x % kXcds;
-  const unsigned id = xcd * per + min(xcd, more) + blockIdx.x / kXcds;
-  const unsigned share = head_blocks * p.splits;
-  const int64_t token = id / share;
-  const int hb = (id % share) % head_blocks, split = (id % share) / head_blocks;
-  const int r = static_cast<int>(token / p.n_q);
-  const int head0 = hb * kHeadTiles * 16;
-
-  const int64_t len = p.lens ? p.lens[token] : INT64_MAX;
-  // entries that can count: with their positions given, any
-  const int limit = p.index ? p.topk : static_cast<int>(len < 0 ? 0 : len < p.topk ? len : p.topk);
-  const int tile0 = split * tiles_per_split;
-  const int tiles = min(tiles_per_split, (limit + kRowTile - 1) / kRowTile - tile0);
-  const int32_t* const rows = p.rows ? p.rows + token * p.topk : nullptr;
-  const int32_t* const index = p.index ? p.index + token * p.topk : nullptr;
-
-  for (int i = threadIdx.x; i < kHeadTiles * 16; i += blockDim.x) reference[i] = -INFINITY;
-  if (threadIdx.x < 4) raised[threadIdx.x] = 0;
-
-  auto load_meta = [&](int t) {
-    RowMeta m{-1, -1, -1};
-    const int i = (tile0 + t) * kRowTile + rt * 16 + (here() & 15);
-    if (t < tiles && i < limit) {
-      m.row = rows ? rows[i] : i;
-      m.pos = index ? index[i] : i;
-      if (!rows && p.cache.table && i < p.cache.capacity)
-        m.page = p.cache.table[static_cast<int64_t>(r) * p.cache.pages_per_request + (i >> p.cache.page_shift)];
-    }
-    return m;
-  };
-  auto address = [&](const RowMeta& m) -> uint64_t {
-    if (m.row < 0 || m.row >= p.cache.capacity || m.pos < 0 || m.pos >= len) return 0;
-    int64_t page = m.page;
-    if (rows || !p.cache.table) {
-      page = static_cast<int64_t>(r) * p.cache.pages_per_request + (m.row >> p.cache.page_shift);
-      if (p.cache.table) page = p.cache.table[page];
-    }
-    if (page < 0 || page >= p.cache.pages) return 0;
-    return p.cache.base + page * p.cache.page_stride + (m.row & p.cache.page_mask) * p.cache.row_stride;
-  };
-
-  // A half is 256 columns in a row, eight steps of 32.  4-bit rows: of every four
-  // steps a lane has one block of 32 columns, 16 bytes; bfloat16 rows: of every
-  // step eight columns.
-  u32x4 key[kLoads], turned[kHalves];
-  u32x2 scales[kHalves];
-  unsigned counts = 0;   // bits of this lane's four rows (quad * 4 + i) that count
-  auto load_keys = [&](const RowMeta& m) {
-    uint64_t at = address(m);
-    const unsigned x = here() >> 4;
-    counts = static_cast<unsigned>(__ballot(at != 0) >> (x * 4)) & 15u;
-    if (at == 0) at = reinterpret_cast<uint64_t>(zero_row);
-    const uint64_t a = at + (16 * x + kg * (kMx4 ? 128 : 512));
-#pragma unroll
-    for (int j = 0; j < kLoads; ++j) key[j] = load_global<u32x4>(a + 64 * j);
-#pragma unroll
-    for (int j = 0; j < kHalves; ++j) {
-      if constexpr (kMx4) scales[j] = load_global<u32x2>(at + kMx4CodeBytes + 8 * (kg + j));
-      turned[j] = load_global<u32x4>(at + (16 * x + (kMx4 ? kMx4RopeAt : kLatent * 2) + 64 * kg) + 64 * j);
-    }
-  };
-
-  RowMeta next = load_meta(0);
-  // a group's own head tiles come first
-  bf16x8 query[kHeadTiles][kSteps + kHalves];
-#pragma unroll
-  for (int h = 0; h < kHeadTiles; ++h) {
-    const int head = head0 + (h + kg * kTiles) % kHeadTiles * 16 + l16;
-    const bool there = head < p.heads;
-    const __bf16* q = p.q + token * p.q_token_stride + (there ? head : 0) * p.q_head_stride;
-#pragma unroll
-    for (int j = 0; j < kSteps + kHalves; ++j) {
-      const int col = j >= kSteps ? kLatent + 32 * (kg + j - kSteps) + 8 * quad
-                      : kMx4      ? kg * 256 + ((j / 4) * 4 + quad) * 32 + (j % 4) * 8
-                                  : kg * 256 + 32 * j + 8 * quad;
-      query[h][j] = *reinterpret_cast<const bf16x8*>(q + col);
-      if (!there) query[h][j] = bf16x8{};
-    }
+  RowFinder finder{};
+  auto leave = [&](const RowFinder& f, int t) { row_at[(t & 1) * kRowTile + lane_here()] = f.address(p, w); };
+  if (wave == 0) {
+    RowFinder second;
+    finder.look(p, w, 0, kRowTile);
+    second.look(p, w, 1, kRowTile);
+    leave(finder, 0);
+    finder.look(p, w, 2, kRowTile);
+    leave(second, 1);
   }
-  load_keys(next);
-  next = load_meta(1);
+  if (threadIdx.x < 16) reference[threadIdx.x] = -INFINITY;
+  if (threadIdx.x < 4) raised[threadIdx.x] = 0;
+  bf16x8 query[18];
+#pragma unroll
+  for (int j = 0; j < 18; ++j)
+    query[j] = load_query(p, w, l16, kMx4 && j < 16 ? (j / 4 * 4 + quad) * 32 + j % 4 * 8 : 32 * j + 8 * quad);
 
-  const float scale = p.scale * 1.4426950408889634f;   // scores in powers of two
-  float ref[kTiles], sum[kTiles];
+  u32x4 key[kLoads], scales{}, turned[2];
+  unsigned counts = 0;   // bits of this lane's four rows (quad * 4 + i) that count
+  auto load_keys = [&](int t) {
+    const unsigned x = lane_here();
+    uint64_t at = row_at[(t & 1) * kRowTile + wave * 16 + (x & 15)];
+    counts = static_cast<unsigned>(__ballot(at != 0) >> (x / 16 * 4)) & 15u;
+    if (at == 0) at = reinterpret_cast<uint64_t>(zero_row);
+    if constexpr (kMx4) scales = load_global<u32x4>(at + kMx4CodeBytes);
+    at += x / 16 * 16;
 #pragma unroll
-  for (int h = 0; h < kTiles; ++h) ref[h] = -INFINITY, sum[h] = 0.f;
-  f32x4 out[kColTiles][kHeadTiles];
+    for (int j = 0; j < kLoads; ++j) key[j] = load_global<u32x4>(at + 64 * j);
 #pragma unroll
-  for (int c = 0; c < kColTiles; ++c)
-#pragma unroll
-    for (int h = 0; h < kHeadTiles; ++h) out[c][h] = f32x4{};
-
+    for (int j = 0; j < 2; ++j) turned[j] = load_global<u32x4>(at + (kMx4 ? kMx4RopeAt : kLatent * 2) + 64 * j);
+  };
   __syncthreads();
+  load_keys(0);
 
-  for (int t = 0; t < tiles; ++t) {
-    unsigned char* const v_lds = values + (kValueBuffers == 2 ? t & 1 : 0) * kValueBytes;
-    // one buffer: every wave is done with the last tile's
-    if constexpr (kValueBuffers == 1) __syncthreads();
+  const float scale = p.scale == 0.f ? 1.f : fabsf(p.scale) * kLog2e;   // scores in powers of two
+  const float per_scale = 1.f / scale;
+  float ref = -INFINITY, sum = 0.f;
+  f32x4 out[kColTiles];
+#pragma unroll
+  for (int c = 0; c < kColTiles; ++c) out[c] = f32x4{};
 
-    unsigned char* value_to;
-    int shift;
+  for (int t = 0; t < w.tiles; ++t) {
+    __syncthreads();   // every wave is done with the last tile's values and weights
+    f32x4 part[2] = {};   // sums that alternate
     {
-      const int x = here();
-      value_to = v_lds + (rt * 16 + (x & 15)) * kValueStride + (kMx4 ? 64 : 16) * (x >> 4) + 512 * kg;
-      shift = (x >> 4) * 8;
-    }
-    f32x4 score[kHeadTiles][kChains];
+      const int x = lane_here();
+      const unsigned to = (wave * 16 + (x & 15)) * kValueStride + value_part(x & 15, (kMx4 ? 4 : 1) * (x >> 4));
 #pragma unroll
-    for (int h = 0; h < kHeadTiles; ++h)
-#pragma unroll
-      for (int j = 0; j < kChains; ++j) score[h][j] = f32x4{};
-#pragma unroll
-    for (int j = 0; j < kSteps; ++j) {
-      bf16x8 k;
-      if constexpr (kMx4) k = mx4_decode8(key[j / 4][j % 4], mx4_unit((scales[j / 8][(j / 4) % 2] >> shift) & 255u));
-      else k = __builtin_bit_cast(bf16x8, key[j]);
-      *reinterpret_cast<bf16x8*>(value_to + (kMx4 ? (j / 4) * 256 + (j % 4) * 16 : 64 * j)) = k;
-#pragma unroll
-      for (int h = 0; h < kHeadTiles; ++h)
-        score[h][j % kChains] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, query[h][j], score[h][j % kChains], 0, 0, 0);
+      for (int j = 0; j < 16; ++j) {
+        bf16x8 k;
+        if constexpr (kMx4) k = mx4_decode8(key[j / 4][j % 4], mx4_unit((scales[j / 4] >> (x / 16 * 8)) & 255u));
+        else k = __builtin_bit_cast(bf16x8, key[j]);
+        *reinterpret_cast<bf16x8*>(values + (to ^ (j % 4 * (kMx4 ? 16 : 64))) + j / 4 * 256) = k;
+        part[j & 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, query[j], part[j & 1], 0, 0, 0);
+      }
     }
 #pragma unroll
-    for (int j = 0; j < kHalves; ++j)
-#pragma unroll
-      for (int h = 0; h < kHeadTiles; ++h)
-        score[h][j % kChains] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, turned[j]), query[h][kSteps + j],
-                                                                        score[h][j % kChains], 0, 0, 0);
+    for (int j = 0; j < 2; ++j)
+      part[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, turned[j]), query[16 + j], part[j], 0, 0, 0);
     const unsigned now = counts;
-    load_keys(next);
-    next = load_meta(t + 2);
-
-    f32x4 s[kTiles];
-    if constexpr (kKeyGroups == 2) {
-      f32x4* const mine = reinterpret_cast<f32x4*>(halves) + (rt * 2 + kg) * kTiles * 64 + here();
-      const f32x4* const theirs = reinterpret_cast<const f32x4*>(halves) + (rt * 2 + (kg ^ 1)) * kTiles * 64 + here();
-#pragma unroll
-      for (int h = 0; h < kTiles; ++h) mine[h * 64] = score[kTiles + h][0];
-      __syncthreads();
-#pragma unroll
-      for (int h = 0; h < kTiles; ++h) s[h] = score[h][0] + theirs[h * 64];
-    } else {
-#pragma unroll
-      for (int h = 0; h < kTiles; ++h) s[h] = kChains == 2 ? score[h][0] + score[h][kChains - 1] : score[h][0];
+    if (t + 1 < w.tiles) load_keys(t + 1);
+    if (wave == 0) {
+      leave(finder, t + 2);
+      finder.look(p, w, t + 3, kRowTile);
     }
 
-    unsigned char* const weight_to = weights + kg * kTiles * 2048 + (rt >> 1) * 1024 + here() * 16 + (rt & 1) * 8;
+    f32x4 s = part[0] + part[1];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (!((now >> i) & 1)) s[i] = -INFINITY;
     // weights relative to the reference as it is; a score far above it is noted
-    auto weigh = [&](int h) {
-      const float base = ref[h] == -INFINITY ? 0.f : ref[h];
-      bf16x4 w;
+    float add;
+    auto weigh = [&]() {
+      const float base = zero_if_none(ref);
+      f32x4 e;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float e = __builtin_amdgcn_exp2f(s[h][i] - base);
-        sum[h] += e;
-        // rounded once; the sum keeps float32 weights, so the rounding errors
-        // of many rows cancel in the output and do not touch the sum
-        w[i] = static_cast<__bf16>(e);
-      }
-      *reinterpret_cast<bf16x4*>(weight_to + h * 2048) = w;
+      for (int i = 0; i < 4; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], scale, -base));
+      add = (e[0] + e[1]) + (e[2] + e[3]);
+      // rounded once; the sum keeps float32 weights, so the rounding errors
+      // of many rows cancel in the output and do not touch the sum
+      *reinterpret_cast<bf16x4*>(weights + (wave >> 1) * 1024 + lane * 16 + (wave & 1) * 8) = rounded(e);
     };
-    bool above = false;
-    float before[kTiles];
-#pragma unroll
-    for (int h = 0; h < kTiles; ++h) {
-      before[h] = sum[h];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        s[h][i] = (now >> i) & 1 ? s[h][i] * scale : -INFINITY;
-        above |= s[h][i] > ref[h] + kSlack;
-      }
-      weigh(h);
-    }
-    if (__any(above) && lane == 0) raised[t & 1] = t + 1;
+    const float top = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
+    weigh();
+    if (__any(top > (ref + kSlack) * per_scale) && lane == 0) raised[t & 1] = t + 1;
     __syncthreads();
-
     if (raised[t & 1] == t + 1) {
-      const int x = here(), x16 = x & 15;
       // some score lies far above the reference: all waves agree on new ones and
       // bring what they hold to them
-#pragma unroll
-      for (int h = 0; h < kTiles; ++h) {
-        float top = fmaxf(fmaxf(s[h][0], s[h][1]), fmaxf(s[h][2], s[h][3]));
-        top = fmaxf(top, __shfl_xor(top, 16));
-        top = fmaxf(top, __shfl_xor(top, 32));
-        if (x < 16) wave_top[rt * kHeadTiles * 16 + (kg * kTiles + h) * 16 + x16] = top;
-      }
+      float high = top * scale;
+      high = fmaxf(high, __shfl_xor(high, 16));
+      high = fmaxf(high, __shfl_xor(high, 32));
+      if (quad == 0) wave_top[wave * 16 + l16] = high;
       __syncthreads();
-      auto fresh = [&](int head) {
-        float top = reference[head];
+      high = reference[l16];
 #pragma unroll
-        for (int w = 0; w < kRowWaves; ++w) top = fmaxf(top, wave_top[w * kHeadTiles * 16 + head]);
-        return top;
-      };
+      for (int i = 0; i < kWaves; ++i) high = fmaxf(high, wave_top[i * 16 + l16]);
+      // nothing is held yet where there is no reference
+      const float by = ref == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ref - high);
 #pragma unroll
-      for (int h = 0; h < kHeadTiles; ++h) {
-        const float old = reference[h * 16 + x16];
-        // nothing is held yet where there is no reference
-        const float by = old == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(old - fresh(h * 16 + x16));
-#pragma unroll
-        for (int c = 0; c < kColTiles; ++c) out[c][h] *= by;
-      }
-#pragma unroll
-      for (int h = 0; h < kTiles; ++h) {
-        const float top = fresh((kg * kTiles + h) * 16 + x16);
-        sum[h] = ref[h] == -INFINITY ? before[h] : before[h] * __builtin_amdgcn_exp2f(ref[h] - top);
-        ref[h] = top;
-        weigh(h);
-      }
+      for (int c = 0; c < kColTiles; ++c) out[c] *= by;
+      sum *= by;
+      ref = high;
+      weigh();
       __syncthreads();
       // read again after the next tile's barrier at the earliest
-      if (rt == 0 && x < 16) {
-#pragma unroll
-        for (int h = 0; h < kTiles; ++h) reference[(kg * kTiles + h) * 16 + x16] = ref[h];
-      }
+      if (wave == 0 && quad == 0) reference[l16] = ref;
     }
+    sum += add;
 
-    const int x = here();
-    const unsigned char* const weight_from = weights + x * 16;
-    const unsigned value_from = ((x >> 4) * 4 + (x & 15) / 4) * kValueStride + (wave * kCols + (x & 3) * 4) * 2;
-    typedef __attribute__((address_space(3))) bf16x4* lds_ptr;
-    auto load_values = [&](int i) {   // column tile i % kColTiles of row pair i / kColTiles
-      const unsigned at = value_from + i / kColTiles * 32 * kValueStride + i % kColTiles * 32;
-      const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_ptr)(v_lds + at));
-      const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_ptr)(v_lds + at + 16 * kValueStride));
-      return bf16x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-    };
-    bf16x8 v = load_values(0), w[kHeadTiles];
+    const unsigned from = values_from(lane_here(), wave * kCols);
 #pragma unroll
-    for (int i = 0; i < 2 * kColTiles; ++i) {
-      const int c = i % kColTiles;
-      if (c == 0) {
+    for (int pair = 0; pair < 2; ++pair) {
+      const bf16x8 x = *reinterpret_cast<const bf16x8*>(weights + pair * 1024 + lane_here() * 16);
 #pragma unroll
-        for (int h = 0; h < kHeadTiles; ++h)
-          w[h] = *reinterpret_cast<const bf16x8*>(weight_from + h * 2048 + i / kColTiles * 1024);
-      }
-      bf16x8 following{};
-      if (i + 1 < 2 * kColTiles) following = load_values(i + 1);
-      // 64 heads: the compiler is kept from reading further ahead than registers last
-      if constexpr (kHeadTiles == 4) __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int h = 0; h < kHeadTiles; ++h)
-        out[c][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, w[h], out[c][h], 0, 0, 0);
-      if constexpr (kHeadTiles == 4) __builtin_amdgcn_sched_barrier(0);
-      v = following;
+      for (int c = 0; c < kColTiles; ++c)
+        out[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(load_values(values, (from ^ (c * 32)) + pair * 32 * kValueStride), x,
+                                                         out[c], 0, 0, 0);
     }
   }
 
   // the waves' sums of weights
   __syncthreads();
+  sum += __shfl_xor(sum, 16);
+  sum += __shfl_xor(sum, 32);
+  if (quad == 0) wave_top[wave * 16 + l16] = sum;
+  __syncthreads();
+  if (l16 >= p.heads) return;
+  float all = 0.f;
 #pragma unroll
-  for (int h = 0; h < kTiles; ++h) {
-    float x = sum[h];
-    x += __shfl_xor(x, 16);
-    x += __shfl_xor(x, 32);
-    if (quad == 0) wave_top[rt * kHeadTiles * 16 + (kg * kTiles + h) * 16 + l16] = x;
+  for (int i = 0; i < kWaves; ++i) all += wave_top[i * 16 + l16];
+  store_head<kColTiles>(p, w, l16, wave * kCols + quad * 4, [&](int c) { return out[c]; }, reference[l16], all,
+                        wave == 0 && quad == 0);
+}
+
+// More than 16 heads, 64 at a time.  Eight waves work on 32 rows in three stages,
+// each a tile behind the one before, with one barrier per tile:
+//   scores   wave (rg, kg) multiplies a quarter of the key columns of 16 rows with
+//            the queries of all 64 heads (held in registers), and leaves the values that
+//            it expanded on the way and its part of the other waves' scores in LDS;
+//   weights  it adds up the four parts of its 16 rows' scores of 16 heads and leaves
+//            their weights in LDS;
+//   output   it multiplies all 32 rows' weights of all heads with 64 of the 512
+//            columns of the values.
+// Alone, each stage keeps one unit of a CU busy (matrix cores, LDS, conversion,
+// exponentials) and then waits for the others' waves: one after the other, with
+// a barrier each, they took 7100 cycles per 64 rows, of which the matrix cores worked
+// 2200, also with two such workgroups of 32 heads on a CU.  In one stream they overlap.
+constexpr int kWideRows = 32;
+constexpr int kWideHeads = 64;
+
+template <bool kMx4>
+__global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams p, int head_blocks, int tiles_per_split) {
+  constexpr int kTiles = kWideHeads / 16, kColTiles = kLatent / 8 / 16;
+  constexpr int kLoads = kMx4 ? 1 : 4;                     // 16 bytes each
+  constexpr int kBufferBytes = kWideRows * kValueStride;
+  extern __shared__ __align__(16) unsigned char lds[];
+  unsigned char* const values = lds;                                                        // [3] tiles
+  unsigned char* const weights = lds + 3 * kBufferBytes;                                    // [2][head tiles][64 lanes] 16 bytes
+  f32x4* const parts = reinterpret_cast<f32x4*>(weights + 2 * kTiles * 1024);               // [2][2][4][3][64]
+  uint64_t* const row_at = reinterpret_cast<uint64_t*>(parts + 2 * 2 * 4 * 3 * 64);         // [4] tiles: rows, 0 = none
+  float* const group_top = reinterpret_cast<float*>(row_at + 4 * kWideRows);                // [2][heads]
+  float* const reference = group_top + 2 * kWideHeads;                                      // [heads]
+  int* const raised = reinterpret_cast<int*>(reference + kWideHeads);                       // [2]
+
+  const int lane = threadIdx.x & 63, l16 = lane & 15, quad = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int rg = wave / 4, kg = wave % 4;
+  const Share w = share_of(p, head_blocks, tiles_per_split, kWideRows);
+  const int head0 = w.head_block * kWideHeads;
+
+  // the first wave finds the rows of two tiles at a time
+  RowFinder finder{};
+  auto leave = [&](const RowFinder& f, int t) { row_at[(t & 3) * kWideRows + lane_here()] = f.address(p, w); };
+  if (wave == 0) {
+    RowFinder second;
+    finder.look(p, w, 0, kWideRows);
+    second.look(p, w, 2, kWideRows);
+    leave(finder, 0);
+    finder.look(p, w, 4, kWideRows);
+    leave(second, 2);
   }
+  if (threadIdx.x < kWideHeads) reference[threadIdx.x] = -INFINITY;
+  if (threadIdx.x < 2) raised[threadIdx.x] = 0;
+
+  // The head tile whose weights the wave makes comes first.  Of the two steps of
+  // rotated columns it takes step kg % 2 for that one and the next.
+  bf16x8 query[kTiles][4], query_turned[2];
+#pragma unroll
+  for (int h = 0; h < kTiles; ++h)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      query[h][j] = load_query(p, w, head0 + (h + kg) % kTiles * 16 + l16, kg * 128 + (kMx4 ? 32 * quad + 8 * j : 32 * j + 8 * quad));
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+    query_turned[h] = load_query(p, w, head0 + (h + kg) % kTiles * 16 + l16, kLatent + kg % 2 * 32 + 8 * quad);
+
+  u32x4 key[kLoads], turned;
+  uint32_t scales = 0;
+  unsigned counts = 0;   // bits of this lane's rows (quad * 4 + i) that count, of the tile whose keys are held
+  auto load_keys = [&](int t) {
+    const unsigned x = lane_here();
+    uint64_t at = row_at[(t & 3) * kWideRows + rg * 16 + (x & 15)];
+    counts = static_cast<unsigned>(__ballot(at != 0) >> (x / 16 * 4)) & 15u;
+    if (at == 0) at = reinterpret_cast<uint64_t>(zero_row);
+    if constexpr (kMx4) scales = load_global<uint32_t>(at + kMx4CodeBytes + 4 * kg);
+    at += x / 16 * 16;
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) key[j] = load_global<u32x4>(at + kg * (kMx4 ? 64 : 256) + 64 * j);
+    turned = load_global<u32x4>(at + (kMx4 ? kMx4RopeAt : kLatent * 2) + kg % 2 * 64);
+  };
+  __syncthreads();
+  load_keys(0);
+
+  const float scale = p.scale == 0.f ? 1.f : fabsf(p.scale) * kLog2e;   // scores in powers of two
+  const float per_scale = 1.f / scale;
+  float ref = -INFINITY, sum = 0.f, add = 0.f;
+  f32x4 mine{}, s{};            // the wave's own part of its scores, and those scores of the tile that is weighed
+  unsigned now = 0;             // rows that count of the tile whose parts are in LDS
+  f32x4 out[kColTiles][kTiles];
+#pragma unroll
+  for (int c = 0; c < kColTiles; ++c)
+#pragma unroll
+    for (int h = 0; h < kTiles; ++h) out[c][h] = f32x4{};
+
+  // weights of s relative to the reference, for tile t
+  auto weigh = [&](int t) {
+    const float base = zero_if_none(ref);
+    f32x4 e;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) e[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[j], scale, -base));
+    add = (e[0] + e[1]) + (e[2] + e[3]);
+    // rounded once; the sum keeps float32 weights, so the rounding errors
+    // of many rows cancel in the output and do not touch the sum
+    *reinterpret_cast<bf16x4*>(weights + (t & 1) * kTiles * 1024 + kg * 1024 + lane_here() * 16 + rg * 8) = rounded(e);
+  };
+  // some score of tile t lies far above the reference: all waves agree on new
+  // ones and bring what they hold to them
+  auto raise = [&](int t) {
+    const int x = lane_here(), x16 = x & 15;
+    float high = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])) * scale;
+    high = fmaxf(high, __shfl_xor(high, 16));
+    high = fmaxf(high, __shfl_xor(high, 32));
+    if (x < 16) group_top[rg * kWideHeads + kg * 16 + x16] = high;
+    __syncthreads();
+    auto fresh = [&](int head) { return fmaxf(reference[head], fmaxf(group_top[head], group_top[kWideHeads + head])); };
+#pragma unroll
+    for (int h = 0; h < kTiles; ++h) {
+      const float old = reference[h * 16 + x16];
+      // nothing is held yet where there is no reference
+      const float by = old == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(old - fresh(h * 16 + x16));
+#pragma unroll
+      for (int c = 0; c < kColTiles; ++c) out[c][h] *= by;
+    }
+    high = fresh(kg * 16 + x16);
+    if (ref != -INFINITY) sum *= __builtin_amdgcn_exp2f(ref - high);
+    ref = high;
+    weigh(t);
+    __syncthreads();
+    // read again after the next barrier at the earliest
+    if (rg == 0 && x < 16) reference[kg * 16 + x16] = ref;
+  };
+
+  // one barrier's work: the output of tile t, weights of tile t + 1, scores of tile t + 2
+  auto stages = [&](auto with_output, auto with_weights, auto with_scores, int t, int buffer) {
+    constexpr bool kOutput = decltype(with_output)::value, kWeights = decltype(with_weights)::value,
+                   kScores = decltype(with_scores)::value;
+    if constexpr (kOutput) {
+      if (raised[t & 1] == t + 1) raise(t);
+      sum += add;
+    }
+    const int x = lane_here();
+    const unsigned char* const v_lds = values + buffer * kBufferBytes;
+    const unsigned v_from = values_from(x, wave * 64);
+    bf16x8 v[kColTiles], e[kTiles];
+    if constexpr (kOutput) {
+#pragma unroll
+      for (int h = 0; h < kTiles; ++h)
+        e[h] = *reinterpret_cast<const bf16x8*>(weights + (t & 1) * kTiles * 1024 + h * 1024 + x * 16);
+      v[0] = load_values(v_lds, v_from);
+      v[1] = load_values(v_lds, v_from ^ 32);
+    }
+    f32x4 theirs[3];
+    if constexpr (kWeights) {
+      const f32x4* const from = parts + (((t + 1) & 1) * 8 + rg * 4 + kg) * 3 * 64 + x;
+#pragma unroll
+      for (int n = 0; n < 3; ++n) theirs[n] = from[n * 64];
+    }
+    f32x4 part[kTiles];
+    if constexpr (kScores) {
+#pragma unroll
+      for (int h = 0; h < kTiles; ++h) part[h] = f32x4{};
+      unsigned char* const to = values + (buffer == 0 ? 2 : buffer - 1) * kBufferBytes;
+      const unsigned at = (rg * 16 + (x & 15)) * kValueStride + kg * 256 + value_part(x & 15, (kMx4 ? 4 : 1) * (x >> 4));
+      const float unit = mx4_unit((scales >> (x / 16 * 8)) & 255u);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        bf16x8 k;
+        if constexpr (kMx4) k = mx4_decode8(key[0][j], unit);
+        else k = __builtin_bit_cast(bf16x8, key[j]);
+        *reinterpret_cast<bf16x8*>(to + (at ^ (j * (kMx4 ? 16 : 64)))) = k;
+#pragma unroll
+        for (int h = 0; h < kTiles; ++h) part[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, query[h][j], part[h], 0, 0, 0);
+        if constexpr (kOutput) {
+          // a column tile of the output with each step of the scores
+          if (j + 2 < kColTiles) v[j + 2] = load_values(v_lds, v_from ^ ((j + 2) * 32));
+#pragma unroll
+          for (int h = 0; h < kTiles; ++h) out[j][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[j], e[h], out[j][h], 0, 0, 0);
+        }
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        part[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, turned), query_turned[h], part[h], 0, 0, 0);
+    } else if constexpr (kOutput) {
+#pragma unroll
+      for (int c = 0; c < kColTiles; ++c) {
+        if (c + 2 < kColTiles) v[c + 2] = load_values(v_lds, v_from ^ ((c + 2) * 32));
+#pragma unroll
+        for (int h = 0; h < kTiles; ++h) out[c][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[c], e[h], out[c][h], 0, 0, 0);
+      }
+    }
+    if constexpr (kWeights) {
+      s = (mine + theirs[0]) + (theirs[1] + theirs[2]);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s[j] = (now >> j) & 1 ? s[j] : -INFINITY;
+    }
+    if constexpr (kScores) {
+      now = counts;
+      load_keys(t + 3);
+      mine = part[0];
+#pragma unroll
+      for (int n = 1; n < 4; ++n) parts[(((t + 2) & 1) * 8 + rg * 4 + (kg + n) % 4) * 3 * 64 + (n - 1) * 64 + x] = part[n];
+    }
+    if constexpr (kWeights) {
+      weigh(t + 1);
+      // a score far above the reference is noted
+      const float top = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
+      if (__any(top > (ref + kSlack) * per_scale)) raised[(t + 1) & 1] = t + 2;
+    }
+    if constexpr (kScores) {
+      if (wave == 0 && t >= 0 && (t & 1) == 0) {
+        leave(finder, t + 4);
+        finder.look(p, w, t + 6, kWideRows);
+      }
+    }
+    __syncthreads();
+  };
+  const std::true_type yes{};
+  const std::false_type no{};
+  if (w.tiles > 0) {
+    stages(no, no, yes, -2, 1);
+    if (w.tiles > 1) {
+      stages(no, yes, yes, -1, 2);
+      int buffer = 0;
+      for (int t = 0; t + 2 < w.tiles; ++t) {
+        stages(yes, yes, yes, t, buffer);
+        buffer = buffer == 2 ? 0 : buffer + 1;
+      }
+      stages(yes, yes, no, w.tiles - 2, buffer);
+      stages(yes, no, no, w.tiles - 1, buffer == 2 ? 0 : buffer + 1);
+    } else {
+      stages(no, yes, no, -1, 2);
+      stages(yes, no, no, 0, 0);
+    }
+  }
+
+  // the waves' sums of weights
+  sum += __shfl_xor(sum, 16);
+  sum += __shfl_xor(sum, 32);
+  if (quad == 0) group_top[rg * kWideHeads + kg * 16 + l16] = sum;
   __syncthreads();
 #pragma unroll
-  for (int h = 0; h < kHeadTiles; ++h) {
+  for (int h = 0; h < kTiles; ++h) {
     const int head = head0 + h * 16 + l16;
     if (head >= p.heads) continue;
-    float all = 0.f;
-#pragma unroll
-    for (int w = 0; w < kRowWaves; ++w) all += wave_top[w * kHeadTiles * 16 + h * 16 + l16];
-    const float base = reference[h * 16 + l16];
-    const int col = wave * kCols + quad * 4;
-    if (p.splits > 1) {
-      const int64_t part = (token * p.splits + split) * p.heads + head;
-      if (wave == 0 && quad == 0) p.part_ml[part] = f32x2{base, all};
-      if (all != 0.f) {
-#pragma unroll
-        for (int c = 0; c < kColTiles; ++c)
-          *reinterpret_cast<f32x4*>(p.part_out + part * kLatent + col + c * 16) = out[c][h];
-      }
-      continue;
-    }
-    const float by = all == 0.f ? 0.f : 1.f / all;
-    __bf16* to = p.out + token * p.out_token_stride + head * p.out_head_stride + col;
-#pragma unroll
-    for (int c = 0; c < kColTiles; ++c) {
-      const f32x4 o = out[c][h] * by;
-      *reinterpret_cast<bf16x4*>(to + c * 16) =
-          bf16x4{static_cast<__bf16>(o[0]), static_cast<__bf16>(o[1]), static_cast<__bf16>(o[2]), static_cast<__bf16>(o[3])};
-    }
-    if (p.lse && wave == 0 && quad == 0)
-      p.lse[token * p.heads + head] =
-          all == 0.f ? -INFINITY : ((base == -INFINITY ? 0.f : base) + __builtin_amdgcn_logf(all)) * 0.6931471805599453f;
+    store_head<kColTiles>(p, w, head, wave * 64 + quad * 4, [&](int c) { return out[c][h]; }, reference[h * 16 + l16],
+                          group_top[h * 16 + l16] + group_top[kWideHeads + h * 16 + l16], wave == 0 && quad == 0);
   }
 }
 
@@ -397,45 +594,54 @@ __global__ __launch_bounds__(kLatent / 4) void combine_kernel(AttendParams p) {
     p.lse[token * p.heads + head] = all == 0.f ? -INFINITY : (base + __builtin_amdgcn_logf(all)) * 0.6931471805599453f;
 }
 
-// Head tiles of a workgroup: the fewest that hold the heads, at most four.
-int head_tiles(int heads) { return heads <= 16 ? 1 : heads <= 32 ? 2 : 4; }
+// Workgroups that share the heads of a query token, and rows of their tiles.
+int head_blocks_of(int heads) { return heads <= 16 ? 1 : (heads + kWideHeads - 1) / kWideHeads; }
+int tile_rows_of(int heads) { return heads <= 16 ? kRowTile : kWideRows; }
 
-template <int kHeadTiles, int kKeyGroups, bool kMx4>
-hipError_t launch_one(const AttendParams& p, hipStream_t s) {
-  constexpr size_t lds = kKeyGroups * kValueBytes + kHeadTiles * 2048 + (kRowWaves + 1) * kHeadTiles * 16 * 4 + 16 +
-                         (kKeyGroups == 2 ? kRowWaves * kHeadTiles * 1024 : 0);
-  static_assert(lds <= 160 * 1024, "LDS of a workgroup");
-  const auto kernel = &attend_kernel<kHeadTiles, kKeyGroups, kMx4>;
-  static const hipError_t ready =
-      hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lds));
+template <typename Kernel>
+hipError_t allow_lds(Kernel kernel, size_t lds) {
+  return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lds));
+}
+
+template <bool kMx4>
+hipError_t launch_narrow(const AttendParams& p, int64_t groups, int tiles_per_split, hipStream_t s) {
+  constexpr size_t lds = kValueBytes + 2048 + 2 * kRowTile * 8 + 5 * 16 * 4 + 16;
+  static_assert(2 * lds <= 160 * 1024, "LDS of two workgroups");
+  static const hipError_t ready = allow_lds(&attend_kernel<kMx4>, lds);
   if (ready != hipSuccess) return ready;
-  const int head_blocks = (p.heads + kHeadTiles * 16 - 1) / (kHeadTiles * 16);
-  const int tiles = (p.topk + kRowTile - 1) / kRowTile;
-  const int64_t groups = static_cast<int64_t>(p.cache.batch) * p.n_q * head_blocks * p.splits;
-  if (groups > INT32_MAX) return hipErrorInvalidValue;
-  kernel<<<dim3(static_cast<unsigned>(groups)), 256 * kKeyGroups, lds, s>>>(p, head_blocks, (tiles + p.splits - 1) / p.splits);
+  attend_kernel<kMx4><<<dim3(static_cast<unsigned>(groups)), 256, lds, s>>>(p, tiles_per_split);
+  return hipGetLastError();
+}
+
+template <bool kMx4>
+hipError_t launch_wide(const AttendParams& p, int64_t groups, int head_blocks, int tiles_per_split, hipStream_t s) {
+  constexpr size_t lds = 3 * kWideRows * kValueStride + 2 * (kWideHeads / 16) * 1024 + 2 * 2 * 4 * 3 * 1024 + 4 * kWideRows * 8 +
+                         3 * kWideHeads * 4 + 8;
+  static_assert(lds <= 160 * 1024, "LDS of a workgroup");
+  static const hipError_t ready = allow_lds(&attend_wide_kernel<kMx4>, lds);
+  if (ready != hipSuccess) return ready;
+  attend_wide_kernel<kMx4><<<dim3(static_cast<unsigned>(groups)), 512, lds, s>>>(p, head_blocks, tiles_per_split);
   return hipGetLastError();
 }
 
 template <bool kMx4>
 hipError_t launch_format(const AttendParams& p, hipStream_t s) {
-  switch (head_tiles(p.heads)) {
-    case 1: return launch_one<1, 1, kMx4>(p, s);
-    case 2: return launch_one<2, 2, kMx4>(p, s);
-    default: return launch_one<4, 2, kMx4>(p, s);
-  }
+  const int head_blocks = head_blocks_of(p.heads), rows = tile_rows_of(p.heads);
+  const int tiles = (p.topk + rows - 1) / rows, each = (tiles + p.splits - 1) / p.splits;
+  const int64_t groups = static_cast<int64_t>(p.cache.batch) * p.n_q * head_blocks * p.splits;
+  if (groups > INT32_MAX) return hipErrorInvalidValue;
+  return p.heads <= 16 ? launch_narrow<kMx4>(p, groups, each, s) : launch_wide<kMx4>(p, groups, head_blocks, each, s);
 }
 
 }  // namespace
 
-// Splits so that every CU has work (two workgroups of up to 32 heads, one of
-// 64), but no part smaller than a tile.
+// Splits so that every CU has work (two workgroups of up to 16 heads, one of
+// 64), but no part smaller than a tile of 64 rows.
 int attend_splits(int batch, int n_q, int heads, int topk) {
   constexpr int64_t kCus = 256;
-  const int per = head_tiles(heads);
-  const int64_t groups = static_cast<int64_t>(batch) * n_q * ((heads + per * 16 - 1) / (per * 16));
-  const int64_t want = (per == 4 ? kCus : 2 * kCus) / groups;
-  const int tiles = (topk + kRowTile - 1) / kRowTile;
+  const int64_t groups = static_cast<int64_t>(batch) * n_q * head_blocks_of(heads);
+  const int64_t want = (heads <= 16 ? 2 * kCus : kCus) / groups;
+  const int tiles = (topk + 63) / 64;
   if (want <= 1 || tiles <= 1) return 1;
   const int64_t each = (tiles + want - 1) / want;
   return static_cast<int>((tiles + each - 1) / each);
