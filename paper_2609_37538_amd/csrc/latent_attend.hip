@@ -32,7 +32,7 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 // The order in which the compiler is to issue what stands before in a block:
 // the next `n` instructions of a kind.
-constexpr int kVector = 0x2, kMatrix = 0x8, kLdsRead = 0x100, kLdsWrite = 0x200;
+constexpr int kMatrix = 0x8, kLdsRead = 0x100;
 #define kSchedule(kind, n) __builtin_amdgcn_sched_group_barrier(kind, n, 0)
 
 // What the loads of entries that do not count read in place of a row.
@@ -78,16 +78,16 @@ __device__ __forceinline__ Share share_of(const AttendParams& p, int head_blocks
   return w;
 }
 
-// One wave finds rows, 64 at a time, one per lane: what is read of them comes
-// first, some tiles later their addresses go to LDS, and all waves fetch their
-// keys a tile ahead.
+// Finds the row of an entry: what is read of it comes first, its address (0: it
+// does not count) some tiles later.
 struct RowFinder {
   int row, pos, page;   // of this lane's row of those looked at last
 
-  __device__ __forceinline__ void look(const AttendParams& p, const Share& w, int t, int tile_rows) {
+  // entry `n` of the share
+  __device__ __forceinline__ void look(const AttendParams& p, const Share& w, int n, int tile_rows) {
     row = pos = page = -1;
-    const int i = (w.tile0 + t) * tile_rows + lane_here();
-    if (i >= w.limit || i >= (w.tile0 + w.tiles) * tile_rows) return;
+    const int i = w.tile0 * tile_rows + n;
+    if (i >= w.limit || n >= w.tiles * tile_rows) return;
     row = p.rows ? p.rows[w.token * p.topk + i] : i;
     pos = p.index ? p.index[w.token * p.topk + i] : i;
     if (!p.rows && p.cache.table && i < p.cache.capacity)
@@ -97,6 +97,9 @@ struct RowFinder {
   __device__ __forceinline__ uint64_t address(const AttendParams& p, const Share& w) const {
     const CacheView& c = p.cache;
     if (row < 0 || row >= c.capacity || pos < 0 || pos >= w.len) return 0;
+    // one page per request, as slots have it
+    if (!c.table && c.pages_per_request == 1)
+      return c.base + w.request * c.page_stride + static_cast<uint64_t>(static_cast<uint32_t>(row)) * static_cast<uint64_t>(c.row_stride);
     int64_t at = page;
     if (p.rows || !c.table) {
       at = static_cast<int64_t>(w.request) * c.pages_per_request + (row >> c.page_shift);
@@ -140,10 +143,8 @@ __device__ __forceinline__ void store_head(const AttendParams& p, const Share& w
   if (p.splits > 1) {
     const int64_t part = (w.token * p.splits + w.split) * p.heads + head;
     if (first) p.part_ml[part] = f32x2{reference, all};
-    if (all != 0.f) {
 #pragma unroll
-      for (int c = 0; c < kColTiles; ++c) *reinterpret_cast<f32x4*>(p.part_out + part * kLatent + col + c * 16) = out(c);
-    }
+    for (int c = 0; c < kColTiles; ++c) *reinterpret_cast<f32x4*>(p.part_out + part * kLatent + col + c * 16) = out(c);
     return;
   }
   const float by = all == 0.f ? 0.f : 1.f / all;
@@ -176,8 +177,7 @@ __global__ __launch_bounds__(256, 2) void attend_kernel(AttendParams p, int tile
   extern __shared__ __align__(16) unsigned char lds[];
   unsigned char* const values = lds;
   unsigned char* const weights = lds + kValueBytes;                              // [2][64 lanes] 16 bytes
-  uint64_t* const row_at = reinterpret_cast<uint64_t*>(weights + 2048);          // [2][64]: rows of a tile, 0 = none
-  float* const wave_top = reinterpret_cast<float*>(row_at + 2 * kRowTile);       // [4][16]
+  float* const wave_top = reinterpret_cast<float*>(weights + 2048);              // [4][16]
   float* const reference = wave_top + kWaves * 16;                               // [16]
   int* const raised = reinterpret_cast<int*>(reference + 16);                    // [4]
 
@@ -185,16 +185,9 @@ __global__ __launch_bounds__(256, 2) void attend_kernel(AttendParams p, int tile
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Share w = share_of(p, 1, tiles_per_split, kRowTile);
 
-  RowFinder finder{};
-  auto leave = [&](const RowFinder& f, int t) { row_at[(t & 1) * kRowTile + lane_here()] = f.address(p, w); };
-  if (wave == 0) {
-    RowFinder second;
-    finder.look(p, w, 0, kRowTile);
-    second.look(p, w, 1, kRowTile);
-    leave(finder, 0);
-    finder.look(p, w, 2, kRowTile);
-    leave(second, 1);
-  }
+  // every lane finds the row whose keys it loads, what is read of it two tiles ahead
+  RowFinder finder;
+  finder.look(p, w, wave * 16 + l16, kRowTile);
   if (threadIdx.x < 16) reference[threadIdx.x] = -INFINITY;
   if (threadIdx.x < 4) raised[threadIdx.x] = 0;
   bf16x8 query[18];
@@ -206,7 +199,8 @@ __global__ __launch_bounds__(256, 2) void attend_kernel(AttendParams p, int tile
   unsigned counts = 0;   // bits of this lane's four rows (quad * 4 + i) that count
   auto load_keys = [&](int t) {
     const unsigned x = lane_here();
-    uint64_t at = row_at[(t & 1) * kRowTile + wave * 16 + (x & 15)];
+    uint64_t at = finder.address(p, w);
+    finder.look(p, w, (t + 1) * kRowTile + wave * 16 + (x & 15), kRowTile);
     counts = static_cast<unsigned>(__ballot(at != 0) >> (x / 16 * 4)) & 15u;
     if (at == 0) at = reinterpret_cast<uint64_t>(zero_row);
     if constexpr (kMx4) scales = load_global<u32x4>(at + kMx4CodeBytes);
@@ -216,7 +210,6 @@ __global__ __launch_bounds__(256, 2) void attend_kernel(AttendParams p, int tile
 #pragma unroll
     for (int j = 0; j < 2; ++j) turned[j] = load_global<u32x4>(at + (kMx4 ? kMx4RopeAt : kLatent * 2) + 64 * j);
   };
-  __syncthreads();
   load_keys(0);
 
   const float scale = p.scale == 0.f ? 1.f : fabsf(p.scale) * kLog2e;   // scores in powers of two
@@ -246,10 +239,6 @@ __global__ __launch_bounds__(256, 2) void attend_kernel(AttendParams p, int tile
       part[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, turned[j]), query[16 + j], part[j], 0, 0, 0);
     const unsigned now = counts;
     if (t + 1 < w.tiles) load_keys(t + 1);
-    if (wave == 0) {
-      leave(finder, t + 2);
-      finder.look(p, w, t + 3, kRowTile);
-    }
 
     f32x4 s = part[0] + part[1];
 #pragma unroll
@@ -296,13 +285,27 @@ __global__ __launch_bounds__(256, 2) void attend_kernel(AttendParams p, int tile
     sum += add;
 
     const unsigned from = values_from(lane_here(), wave * kCols);
+    const unsigned char* const weight_from = weights + lane_here() * 16;
+    const bf16x8 e[2] = {*reinterpret_cast<const bf16x8*>(weight_from), *reinterpret_cast<const bf16x8*>(weight_from + 1024)};
+    // operands are read four products ahead: left to itself the compiler waits for each
+    auto load_step = [&](int n) {   // column tile n % kColTiles of rows n / kColTiles * 32 .. + 31
+      return load_values(values, (from ^ (n % kColTiles * 32)) + n / kColTiles * 32 * kValueStride);
+    };
+    constexpr int kAhead = 4;
+    bf16x8 v[kAhead];
 #pragma unroll
-    for (int pair = 0; pair < 2; ++pair) {
-      const bf16x8 x = *reinterpret_cast<const bf16x8*>(weights + pair * 1024 + lane_here() * 16);
+    for (int n = 0; n < kAhead; ++n) v[n] = load_step(n);
 #pragma unroll
-      for (int c = 0; c < kColTiles; ++c)
-        out[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(load_values(values, (from ^ (c * 32)) + pair * 32 * kValueStride), x,
-                                                         out[c], 0, 0, 0);
+    for (int n = 0; n < 2 * kColTiles; ++n) {
+      const bf16x8 x = v[n % kAhead];
+      if (n + kAhead < 2 * kColTiles) v[n % kAhead] = load_step(n + kAhead);
+      out[n % kColTiles] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, e[n / kColTiles], out[n % kColTiles], 0, 0, 0);
+    }
+    kSchedule(kLdsRead, 2 + 2 * kAhead);
+#pragma unroll
+    for (int n = 0; n < 2 * kColTiles; ++n) {
+      kSchedule(kMatrix, 1);
+      kSchedule(kLdsRead, 2);
     }
   }
 
@@ -356,15 +359,16 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams p, int
   const Share w = share_of(p, head_blocks, tiles_per_split, kWideRows);
   const int head0 = w.head_block * kWideHeads;
 
-  // the first wave finds the rows of two tiles at a time
+  // the first wave finds the rows of two tiles at a time, one per lane; their
+  // addresses go to LDS, and all waves fetch their keys a tile ahead
   RowFinder finder{};
   auto leave = [&](const RowFinder& f, int t) { row_at[(t & 3) * kWideRows + lane_here()] = f.address(p, w); };
   if (wave == 0) {
     RowFinder second;
-    finder.look(p, w, 0, kWideRows);
-    second.look(p, w, 2, kWideRows);
+    finder.look(p, w, lane, kWideRows);
+    second.look(p, w, 2 * kWideRows + lane, kWideRows);
     leave(finder, 0);
-    finder.look(p, w, 4, kWideRows);
+    finder.look(p, w, 4 * kWideRows + lane, kWideRows);
     leave(second, 2);
   }
   if (threadIdx.x < kWideHeads) reference[threadIdx.x] = -INFINITY;
@@ -385,19 +389,23 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams p, int
   u32x4 key[kLoads], turned;
   uint32_t scales = 0;
   unsigned counts = 0;   // bits of this lane's rows (quad * 4 + i) that count, of the tile whose keys are held
-  auto load_keys = [&](int t) {
-    const unsigned x = lane_here();
-    uint64_t at = row_at[(t & 3) * kWideRows + rg * 16 + (x & 15)];
-    counts = static_cast<unsigned>(__ballot(at != 0) >> (x / 16 * 4)) & 15u;
+  auto find_keys = [&](int t) { return row_at[(t & 3) * kWideRows + rg * 16 + l16]; };
+  auto take_keys = [&](uint64_t& at) {
+    counts = static_cast<unsigned>(__ballot(at != 0) >> (quad * 4)) & 15u;
     if (at == 0) at = reinterpret_cast<uint64_t>(zero_row);
-    if constexpr (kMx4) scales = load_global<uint32_t>(at + kMx4CodeBytes + 4 * kg);
-    at += x / 16 * 16;
-#pragma unroll
-    for (int j = 0; j < kLoads; ++j) key[j] = load_global<u32x4>(at + kg * (kMx4 ? 64 : 256) + 64 * j);
-    turned = load_global<u32x4>(at + (kMx4 ? kMx4RopeAt : kLatent * 2) + kg % 2 * 64);
+  };
+  auto load_part = [&](uint64_t at, int n) {   // of kLoads + 2 loads the n-th
+    if (n < kLoads) key[n] = load_global<u32x4>(at + (quad * 16 + kg * (kMx4 ? 64 : 256)) + 64 * n);
+    if (n == kLoads) turned = load_global<u32x4>(at + (quad * 16 + (kMx4 ? kMx4RopeAt : kLatent * 2) + kg % 2 * 64));
+    if (kMx4 && n == kLoads + 1) scales = load_global<uint32_t>(at + (kMx4CodeBytes + 4 * kg));
   };
   __syncthreads();
-  load_keys(0);
+  {
+    uint64_t at = find_keys(0);
+    take_keys(at);
+#pragma unroll
+    for (int n = 0; n < kLoads + 2; ++n) load_part(at, n);
+  }
 
   const float scale = p.scale == 0.f ? 1.f : fabsf(p.scale) * kLog2e;   // scores in powers of two
   const float per_scale = 1.f / scale;
@@ -448,62 +456,86 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams p, int
     if (rg == 0 && x < 16) reference[kg * 16 + x16] = ref;
   };
 
+  const unsigned lane16 = lane * 16;
+  const unsigned v_to = (rg * 16 + l16) * kValueStride + kg * 256 + value_part(l16, (kMx4 ? 4 : 1) * quad);
+  const unsigned v_from = values_from(lane, wave * 64);
+  const int scale_shift = quad * 8;
+
   // one barrier's work: the output of tile t, weights of tile t + 1, scores of tile t + 2
   auto stages = [&](auto with_output, auto with_weights, auto with_scores, int t, int buffer) {
     constexpr bool kOutput = decltype(with_output)::value, kWeights = decltype(with_weights)::value,
                    kScores = decltype(with_scores)::value;
-    if constexpr (kOutput) {
-      if (raised[t & 1] == t + 1) raise(t);
-      sum += add;
-    }
-    const int x = lane_here();
+    // what the other stages read of LDS comes while the scores' products run
+    int high = 0;
     const unsigned char* const v_lds = values + buffer * kBufferBytes;
-    const unsigned v_from = values_from(x, wave * 64);
+    const unsigned char* const e_lds = weights + (t & 1) * kTiles * 1024 + lane16;
+    constexpr int kAhead = 2;
     bf16x8 v[kColTiles], e[kTiles];
     if constexpr (kOutput) {
+      high = raised[t & 1];
 #pragma unroll
-      for (int h = 0; h < kTiles; ++h)
-        e[h] = *reinterpret_cast<const bf16x8*>(weights + (t & 1) * kTiles * 1024 + h * 1024 + x * 16);
-      v[0] = load_values(v_lds, v_from);
-      v[1] = load_values(v_lds, v_from ^ 32);
-    }
-    f32x4 theirs[3];
-    if constexpr (kWeights) {
-      const f32x4* const from = parts + (((t + 1) & 1) * 8 + rg * 4 + kg) * 3 * 64 + x;
+      for (int h = 0; h < kTiles; ++h) e[h] = *reinterpret_cast<const bf16x8*>(e_lds + h * 1024);
 #pragma unroll
-      for (int n = 0; n < 3; ++n) theirs[n] = from[n * 64];
+      for (int c = 0; c < kAhead; ++c) v[c] = load_values(v_lds, v_from ^ (c * 32));
     }
+    uint64_t next_at = 0;
+    if constexpr (kScores) next_at = find_keys(t + 3);
     f32x4 part[kTiles];
+    unsigned counted = 0;
     if constexpr (kScores) {
-#pragma unroll
-      for (int h = 0; h < kTiles; ++h) part[h] = f32x4{};
       unsigned char* const to = values + (buffer == 0 ? 2 : buffer - 1) * kBufferBytes;
-      const unsigned at = (rg * 16 + (x & 15)) * kValueStride + kg * 256 + value_part(x & 15, (kMx4 ? 4 : 1) * (x >> 4));
-      const float unit = mx4_unit((scales >> (x / 16 * 8)) & 255u);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
+      const float unit = mx4_unit((scales >> scale_shift) & 255u);
+      auto operand = [&](int j) {
         bf16x8 k;
         if constexpr (kMx4) k = mx4_decode8(key[0][j], unit);
         else k = __builtin_bit_cast(bf16x8, key[j]);
-        *reinterpret_cast<bf16x8*>(to + (at ^ (j * (kMx4 ? 16 : 64)))) = k;
+        return k;
+      };
+      // the operand of a step is expanded during the one before
+      bf16x8 k = operand(0);
+#pragma unroll
+      for (int h = 0; h < kTiles; ++h) part[h] = f32x4{};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        bf16x8 following{};
+        if (j < 3) following = operand(j + 1);
+        *reinterpret_cast<bf16x8*>(to + (v_to ^ (j * (kMx4 ? 16 : 64)))) = k;
 #pragma unroll
         for (int h = 0; h < kTiles; ++h) part[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, query[h][j], part[h], 0, 0, 0);
-        if constexpr (kOutput) {
-          // a column tile of the output with each step of the scores
-          if (j + 2 < kColTiles) v[j + 2] = load_values(v_lds, v_from ^ ((j + 2) * 32));
-#pragma unroll
-          for (int h = 0; h < kTiles; ++h) out[j][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[j], e[h], out[j][h], 0, 0, 0);
-        }
+        k = following;
       }
 #pragma unroll
       for (int h = 0; h < 2; ++h)
         part[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, turned), query_turned[h], part[h], 0, 0, 0);
-    } else if constexpr (kOutput) {
+      counted = counts;
+    }
+    if constexpr (kOutput) {
+      if (high == t + 1) {
+        raise(t);
 #pragma unroll
-      for (int c = 0; c < kColTiles; ++c) {
-        if (c + 2 < kColTiles) v[c + 2] = load_values(v_lds, v_from ^ ((c + 2) * 32));
+        for (int h = 0; h < kTiles; ++h) e[h] = *reinterpret_cast<const bf16x8*>(e_lds + h * 1024);
+      }
+      sum += add;
+    }
+    f32x4 theirs[3];
+    if constexpr (kWeights) {
+      const unsigned char* const from = reinterpret_cast<unsigned char*>(parts) + (((t + 1) & 1) * 8 + rg * 4 + kg) * 3 * 1024 + lane16;
+#pragma unroll
+      for (int n = 0; n < 3; ++n) theirs[n] = *reinterpret_cast<const f32x4*>(from + n * 1024);
+    }
+    if constexpr (kScores) take_keys(next_at);
+    unsigned char* const parts_to = reinterpret_cast<unsigned char*>(parts) + (((t + 2) & 1) * 8 + rg * 4) * 3 * 1024 + lane16;
+#pragma unroll
+    for (int c = 0; c < kColTiles; ++c) {
+      if constexpr (kOutput) {
+        if (c + kAhead < kColTiles) v[c + kAhead] = load_values(v_lds, v_from ^ ((c + kAhead) * 32));
 #pragma unroll
         for (int h = 0; h < kTiles; ++h) out[c][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[c], e[h], out[c][h], 0, 0, 0);
+      }
+      if constexpr (kScores) {
+        // the next keys' loads and the scores' way to the others, one by one between products
+        for (int n = c * (kLoads + 2) / 4; n < (c + 1) * (kLoads + 2) / 4; ++n) load_part(next_at, n);
+        if (c > 0) *reinterpret_cast<f32x4*>(parts_to + (kg + c) % 4 * 3 * 1024 + (c - 1) * 1024) = part[c];
       }
     }
     if constexpr (kWeights) {
@@ -512,11 +544,8 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams p, int
       for (int j = 0; j < 4; ++j) s[j] = (now >> j) & 1 ? s[j] : -INFINITY;
     }
     if constexpr (kScores) {
-      now = counts;
-      load_keys(t + 3);
+      now = counted;
       mine = part[0];
-#pragma unroll
-      for (int n = 1; n < 4; ++n) parts[(((t + 2) & 1) * 8 + rg * 4 + (kg + n) % 4) * 3 * 64 + (n - 1) * 64 + x] = part[n];
     }
     if constexpr (kWeights) {
       weigh(t + 1);
@@ -527,7 +556,7 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams p, int
     if constexpr (kScores) {
       if (wave == 0 && t >= 0 && (t & 1) == 0) {
         leave(finder, t + 4);
-        finder.look(p, w, t + 6, kWideRows);
+        finder.look(p, w, (t + 6) * kWideRows + lane_here(), kWideRows);
       }
     }
     __syncthreads();
@@ -565,33 +594,52 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams p, int
   }
 }
 
-// Joins the parts of one (query token, head): four columns per thread.  Parts
-// without a row that counts hold no sums.
-__global__ __launch_bounds__(kLatent / 4) void combine_kernel(AttendParams p) {
+// Joins the parts of one (query token, head).  The parts' factors are made once;
+// then four groups of threads add up every fourth part, four columns per thread,
+// with several parts in flight.
+constexpr int kMostSplits = 512;
+constexpr int kJoinGroups = 4;
+__global__ __launch_bounds__(kJoinGroups * kLatent / 4) void combine_kernel(AttendParams p) {
+  __shared__ float factor[kMostSplits], per_wave[2][8];
+  __shared__ f32x4 group_sum[kJoinGroups - 1][kLatent / 4];
   const int64_t token = blockIdx.x / p.heads;
-  const int head = static_cast<int>(blockIdx.x - token * p.heads), col = threadIdx.x * 4;
+  const int head = static_cast<int>(blockIdx.x - token * p.heads);
   const int64_t first = token * p.splits * p.heads + head;
-  float top = -INFINITY;
-  for (int i = 0; i < p.splits; ++i) {
-    const f32x2 ml = p.part_ml[first + static_cast<int64_t>(i) * p.heads];
-    if (ml[1] != 0.f) top = fmaxf(top, ml[0]);
-  }
-  const float base = top == -INFINITY ? 0.f : top;
-  float all = 0.f;
+  const int tid = threadIdx.x, wave = tid / 64;
+  const f32x2 ml = tid < p.splits ? p.part_ml[first + static_cast<int64_t>(tid) * p.heads] : f32x2{-INFINITY, 0.f};
+  float top = ml[1] != 0.f ? ml[0] : -INFINITY;   // a part without a row that counts has no reference
+#pragma unroll
+  for (int d = 32; d > 0; d /= 2) top = fmaxf(top, __shfl_xor(top, d));
+  if ((tid & 63) == 0) per_wave[0][wave] = top;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 8; ++i) top = fmaxf(top, per_wave[0][i]);
+  const float base = zero_if_none(top);
+  const float w = ml[1] != 0.f ? __builtin_amdgcn_exp2f(ml[0] - base) : 0.f;
+  factor[tid] = w;
+  float all = ml[1] != 0.f ? w * ml[1] : 0.f;
+#pragma unroll
+  for (int d = 32; d > 0; d /= 2) all += __shfl_xor(all, d);
+  if ((tid & 63) == 0) per_wave[1][wave] = all;
+  __syncthreads();
+  all = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) all += per_wave[1][i];
+
+  const int group = tid / (kLatent / 4), col = tid % (kLatent / 4) * 4;
+  const float* part = p.part_out + first * kLatent + col;
+  const int64_t stride = static_cast<int64_t>(p.heads) * kLatent;
   f32x4 o{};
-  for (int i = 0; i < p.splits; ++i) {
-    const int64_t part = first + static_cast<int64_t>(i) * p.heads;
-    const f32x2 ml = p.part_ml[part];
-    if (ml[1] == 0.f) continue;
-    const float w = __builtin_amdgcn_exp2f(ml[0] - base);
-    all += w * ml[1];
-    o += *reinterpret_cast<const f32x4*>(p.part_out + part * kLatent + col) * w;
-  }
+#pragma unroll 8
+  for (int i = group; i < p.splits; i += kJoinGroups) o += *reinterpret_cast<const f32x4*>(part + i * stride) * factor[i];
+  if (group > 0) group_sum[group - 1][col / 4] = o;
+  __syncthreads();
+  if (group > 0) return;
+#pragma unroll
+  for (int g = 0; g < kJoinGroups - 1; ++g) o += group_sum[g][col / 4];
   o *= all == 0.f ? 0.f : 1.f / all;
-  *reinterpret_cast<bf16x4*>(p.out + token * p.out_token_stride + head * p.out_head_stride + col) =
-      bf16x4{static_cast<__bf16>(o[0]), static_cast<__bf16>(o[1]), static_cast<__bf16>(o[2]), static_cast<__bf16>(o[3])};
-  if (p.lse && threadIdx.x == 0)
-    p.lse[token * p.heads + head] = all == 0.f ? -INFINITY : (base + __builtin_amdgcn_logf(all)) * 0.6931471805599453f;
+  *reinterpret_cast<bf16x4*>(p.out + token * p.out_token_stride + head * p.out_head_stride + col) = rounded(o);
+  if (p.lse && tid == 0) p.lse[token * p.heads + head] = all == 0.f ? -INFINITY : (base + __builtin_amdgcn_logf(all)) * kLn2;
 }
 
 // Workgroups that share the heads of a query token, and rows of their tiles.
@@ -605,7 +653,7 @@ hipError_t allow_lds(Kernel kernel, size_t lds) {
 
 template <bool kMx4>
 hipError_t launch_narrow(const AttendParams& p, int64_t groups, int tiles_per_split, hipStream_t s) {
-  constexpr size_t lds = kValueBytes + 2048 + 2 * kRowTile * 8 + 5 * 16 * 4 + 16;
+  constexpr size_t lds = kValueBytes + 2048 + 5 * 16 * 4 + 16;
   static_assert(2 * lds <= 160 * 1024, "LDS of two workgroups");
   static const hipError_t ready = allow_lds(&attend_kernel<kMx4>, lds);
   if (ready != hipSuccess) return ready;
@@ -650,7 +698,7 @@ int attend_splits(int batch, int n_q, int heads, int topk) {
 hipError_t launch_attend(const AttendParams& p, int format, hipStream_t s) {
   hipError_t e = format == 1 ? launch_format<true>(p, s) : launch_format<false>(p, s);
   if (e != hipSuccess || p.splits <= 1) return e;
-  combine_kernel<<<dim3(static_cast<unsigned>(p.cache.batch * p.n_q * p.heads)), kLatent / 4, 0, s>>>(p);
+  combine_kernel<<<dim3(static_cast<unsigned>(p.cache.batch * p.n_q * p.heads)), kJoinGroups * kLatent / 4, 0, s>>>(p);
   return hipGetLastError();
 }
 
