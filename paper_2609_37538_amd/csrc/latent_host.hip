@@ -247,6 +247,7 @@ avsg_status avsg_mx4_matmul(const avsg_mx4* a, const avsg_mx4* b, int32_t batch,
   p.f32 = out_type == AVSG_F32;
   p.out_stride = out_stride;
   p.out_batch_stride = out_batch_stride;
+  p.wide_stores = aligned(d_out, p.f32 ? 16 : 8) && (out_stride & 3) == 0 && (out_batch_stride & 3) == 0;
   return launched(launch_mx4_matmul(p, static_cast<hipStream_t>(stream)), "avsg_mx4_matmul");
 }
 

@@ -151,6 +151,7 @@ struct Mx4Product {
   int32_t m, n, k;
   void* out;
   bool f32;
+  bool wide_stores;   // four neighbouring outputs can be stored at once
   int64_t out_stride, out_batch_stride;
 };
 
