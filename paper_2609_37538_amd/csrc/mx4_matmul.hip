@@ -255,17 +255,13 @@ __global__ __launch_bounds__(kWavesM * kWavesN * 64, kWavesM * kWavesN / 4) void
           reinterpret_cast<const __attribute__((address_space(1))) void*>(reinterpret_cast<uint64_t>(from)),
           (__attribute__((address_space(3))) void*)(lds + buffer * kStage + (j * kWaves + wave) * 1024), 16, 0, 0);
     }
+    // eight scales, of the last step the row's last eight moved down: where they
+    // are zeros in place of scales, so are the codes
+    const int first = min(step * 8, blocks - 8), off = (step * 8 - first) * 8;
 #pragma unroll
     for (int j = 0; j < kScaleRows; ++j) {
-      const uint8_t* from = scale_row[j] + step * 8;
-      if (step * 8 + 8 <= blocks) {
-        __builtin_memcpy(&scales[j], from, 8);
-      } else {
-        scales[j] = 0x7f7f7f7f7f7f7f7full;
-#pragma unroll
-        for (int b = 0; b < 8; ++b)
-          if (step * 8 + b < blocks) scales[j] = (scales[j] & ~(0xffull << (8 * b))) | static_cast<uint64_t>(from[b]) << (8 * b);
-      }
+      __builtin_memcpy(&scales[j], scale_row[j] + first, 8);
+      scales[j] >>= off;
     }
   };
   auto leave_scales = [&](int buffer) {
@@ -277,16 +273,15 @@ __global__ __launch_bounds__(kWavesM * kWavesN * 64, kWavesM * kWavesN / 4) void
   f32x4 sum[kM][kN] = {};
   const int a0 = wave / kWavesN * (kM * 16), b0 = kTileM + wave % kWavesN * (kN * 16);
   const unsigned at = (l16 * 128) + ((quad ^ (l16 >> 1 & 7)) * 16);
-  if (steps > 0) {
-    fetch(0, 0);
-    leave_scales(0);
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-  }
+  fetch(0, 0);
+  leave_scales(0);
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
   for (int step = 0; step < steps; ++step) {
     const int buffer = step & 1;
     const unsigned char* const from = lds + buffer * kStage;
-    if (step + 1 < steps) fetch(step + 1, buffer ^ 1);
+    // (of the last step a second time: without a branch the products stay where they are)
+    fetch(min(step + 1, steps - 1), buffer ^ 1);
     u32x2 sa[kM], sb[kN];
 #pragma unroll
     for (int x = 0; x < kM; ++x) sa[x] = *reinterpret_cast<const u32x2*>(from + kRows * 128 + (a0 + x * 16 + l16) * 8) >> (quad * 8);
@@ -314,7 +309,7 @@ __global__ __launch_bounds__(kWavesM * kWavesN * 64, kWavesM * kWavesN / 4) void
       }
       __builtin_amdgcn_sched_barrier(0);
     }
-    if (step + 1 < steps) leave_scales(buffer ^ 1);
+    leave_scales(buffer ^ 1);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
   }

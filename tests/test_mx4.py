@@ -112,6 +112,29 @@ def test_product_of_heads(batch, m, n, k):
     assert (room[..., n:] == 3.0).all()
 
 
+@pytest.mark.parametrize("batch,m,n,k,f32", [(1, 2100, 1100, 1056, False), (1, 1100, 2100, 544, True), (20, 300, 300, 800, False),
+                                             (1, 4200, 4100, 544, False), (1, 4097, 4096, 1120, True), (70, 300, 500, 576, False)])
+def test_product_of_many_tiles(batch, m, n, k, f32):
+    """Tiles through LDS, small and large: columns that end inside a step, rows and columns that end
+    inside a tile, heads that interleave, an output whose rows are not aligned, and a NaN scale in the last block."""
+    from paper_2609_37538_amd import latent as L
+    g = gen(batch + m + k)
+    x = L.mx4_quantize(torch.randn(m, batch, k, generator=g, device="cuda") * torch.exp2(torch.randint(-8, 9, (m, 1, 1), generator=g, device="cuda").float()))
+    x, w = x.transpose(0, 1), L.mx4_quantize(torch.randn(batch, n, k, generator=g, device="cuda"))
+    room = torch.full((m, batch, n + 3), 3.0, dtype=torch.float32 if f32 else torch.bfloat16, device="cuda")
+    out = L.mx4_matmul(x, w, out=room[..., 1:n + 1].transpose(0, 1))
+    for i in sorted({0, batch // 2, batch - 1}):
+        product(L.Mx4(x.codes[i], x.scales[i]), L.Mx4(w.codes[i], w.scales[i]), out[i], f32)
+    assert (room[..., 0] == 3.0).all() and (room[..., n + 1:] == 3.0).all()
+    aligned = L.mx4_matmul(x, w, dtype=out.dtype)
+    assert torch.equal(aligned, out)
+    x.scales[batch - 1, m - 1, -1] = 255
+    out = L.mx4_matmul(x, w, dtype=out.dtype)
+    assert out[batch - 1, m - 1].isnan().all()
+    out[batch - 1, m - 1] = aligned[batch - 1, m - 1]
+    assert torch.equal(out, aligned)
+
+
 def test_product_of_extreme_scales():
     """Block scales across the whole range, and a block that is NaN in one row."""
     from paper_2609_37538_amd import latent as L
