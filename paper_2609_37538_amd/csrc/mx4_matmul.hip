@@ -9,6 +9,7 @@
 #include <type_traits>
 
 #include <algorithm>
+#include <utility>
 
 #include "latent_internal.h"
 
@@ -26,6 +27,16 @@ constexpr int kMatrix = 0x8, kLdsRead = 0x100;
 template <int kKind, int kCount>
 __device__ __forceinline__ void schedule() {
   __builtin_amdgcn_sched_group_barrier(kKind, kCount, 0);
+}
+
+// f(0), f(1), ..., each with its number as a constant.
+template <class F, int... kI>
+__device__ __forceinline__ void each(std::integer_sequence<int, kI...>, F f) {
+  (f(std::integral_constant<int, kI>{}), ...);
+}
+template <int kCount, class F>
+__device__ __forceinline__ void each(F f) {
+  each(std::make_integer_sequence<int, kCount>{}, f);
 }
 
 template <int kByteA, int kByteB>
@@ -59,6 +70,20 @@ __device__ __forceinline__ void store4(const Mx4Product& p, int64_t batch, int m
 #pragma unroll
     for (int j = 0; j < 4; ++j)
       if (n + j < p.n) to[j] = static_cast<__bf16>(x[j]);
+  }
+}
+
+// Eight neighbouring columns of a row in 16 bits.
+__device__ __forceinline__ void store8(const Mx4Product& p, int64_t batch, int m, int n, f32x4 x, f32x4 y) {
+  if (p.wide_stores && n + 7 < p.n) {
+    if (m >= p.m) return;
+    typedef __bf16 bf16x8_at_8 __attribute__((ext_vector_type(8), aligned(8)));
+    *reinterpret_cast<bf16x8_at_8*>(static_cast<__bf16*>(p.out) + batch * p.out_batch_stride + static_cast<int64_t>(m) * p.out_stride + n) =
+        bf16x8_at_8{static_cast<__bf16>(x[0]), static_cast<__bf16>(x[1]), static_cast<__bf16>(x[2]), static_cast<__bf16>(x[3]),
+                    static_cast<__bf16>(y[0]), static_cast<__bf16>(y[1]), static_cast<__bf16>(y[2]), static_cast<__bf16>(y[3])};
+  } else {
+    store4<false>(p, batch, m, n, x);
+    store4<false>(p, batch, m, n + 4, y);
   }
 }
 
@@ -188,6 +213,12 @@ __global__ __launch_bounds__(kWavesM * kWavesN * 64) void tile_kernel(Mx4Product
 // What columns past the end read in place of codes.
 __device__ __align__(16) const unsigned char zero_block[16] = {};
 
+// Bits of a row by which the staged blocks of 16 bytes are exchanged: the eight pairs
+// of the sixteen rows that are read together differ in them.
+__device__ __forceinline__ int exchange(int row, bool by_eights) {
+  return by_eights ? (row >> 1 & 1) | (row >> 2 & 6) : row >> 1 & 7;
+}
+
 // Larger products: tiles of kTileM x kTileN outputs, kWavesM x kWavesN waves.
 // Steps of 256 columns go from global memory to LDS without passing registers, the
 // next step's while this one's products run: 64 matrix instructions per wave and step
@@ -200,8 +231,7 @@ __global__ __launch_bounds__(kWavesM * kWavesN * 64, kWavesM * kWavesN / 4) void
   constexpr int kM = kTileM / kWavesM / 16, kN = kTileN / kWavesN / 16;
   constexpr int kRows = kTileM + kTileN;                 // rows of a, then rows of b
   constexpr int kLoads = kRows / 8 / kWaves;             // eight rows each
-  constexpr int kScaleRows = kRows / kThreads;           // rows whose scales a thread brings
-  static_assert(kRows % (8 * kWaves) == 0 && kRows % kThreads == 0, "shares of the loads");
+  static_assert(kRows % (8 * kWaves) == 0 && kRows == kThreads, "shares of the loads: a thread brings the scales of one row");
   constexpr int kStage = kRows * 136;                    // codes, then eight scales per row
   extern __shared__ __align__(16) unsigned char lds[];   // [2]
   const int lane = threadIdx.x & 63, l16 = lane & 15, quad = lane >> 4;
@@ -224,100 +254,114 @@ __global__ __launch_bounds__(kWavesM * kWavesN * 64, kWavesM * kWavesN / 4) void
   // eight rows are of one matrix
   auto from_a = [&](int j) { return (j * kWaves + wave) * 8 < kTileM; };
   uint32_t row_at[kLoads];
-  const int block_of = (lane & 7) ^ ((wave * 4 + lane / 16) & 7);
-  static_assert(kWaves % 2 == 0, "block_of is the same for all loads");
+  static_assert(kWaves % 4 == 0, "all loads exchange blocks alike");
+  const int block_a = (lane & 7) ^ exchange(wave * 8 + lane / 8, false), block_b = (lane & 7) ^ exchange(wave * 8 + lane / 8, !kF32);
 #pragma unroll
   for (int j = 0; j < kLoads; ++j) {
     const int r = (j * kWaves + wave) * 8 + lane / 8;
     row_at[j] = from_a(j) ? min(r, last_a) * static_cast<uint32_t>(p.a.code_stride)
                           : min(r - kTileM, last_b) * static_cast<uint32_t>(p.b.code_stride);
   }
-  const uint8_t* scale_row[kScaleRows];
-#pragma unroll
-  for (int j = 0; j < kScaleRows; ++j) {
-    const int r = j * kThreads + threadIdx.x;
-    const Mx4View& x = r < kTileM ? p.a : p.b;
-    const int64_t row = r < kTileM ? tm * kTileM + min(r, last_a) : tn * kTileN + min(r - kTileM, last_b);
-    scale_row[j] = x.scales + i * x.scale_batch_stride + row * x.scale_stride;
-  }
+  // The scales of a row: in LDS lane l of a wave's products finds its bytes, a
+  // tile of 16 rows after the other, first and second half of the step, in one place.
+  const int row = threadIdx.x, of_b = row - kTileM;
+  const bool is_a = of_b < 0;
+  const Mx4View& x = is_a ? p.a : p.b;
+  const uint8_t* const scale_row = x.scales + i * x.scale_batch_stride +
+                                   (is_a ? tm * kTileM + min(row, last_a) : tn * kTileN + min(of_b, last_b)) * x.scale_stride;
+  const int share = is_a ? kM : kN, in_wave = (is_a ? row : of_b) % (share * 16);
+  const int tile16 = is_a || kF32 ? in_wave / 16 : in_wave / 32 * 2 + (in_wave / 4 & 1);
+  const int lane16 = is_a || kF32 ? in_wave % 16 : (in_wave / 8 & 3) * 4 + (in_wave & 3);
+  const unsigned scales_at = kRows * 128 + (row - in_wave) * 8 + lane16 * (share * 2) + tile16 * 2;
 
-  uint64_t scales[kScaleRows];
-  auto fetch = [&](int step, int buffer) {
-#pragma unroll
-    for (int j = 0; j < kLoads; ++j) {
-      // (the compiler would keep eight advancing 64-bit addresses)
-      uint32_t row = row_at[j];
-      asm volatile("" : "+v"(row));
-      const int block = step * 8 + block_of;
-      const uint8_t* from = (from_a(j) ? codes_a : codes_b) + row + 16 * static_cast<uint32_t>(block);
-      if (block >= blocks) from = zero_block;
-      __builtin_amdgcn_global_load_lds(
-          reinterpret_cast<const __attribute__((address_space(1))) void*>(reinterpret_cast<uint64_t>(from)),
-          (__attribute__((address_space(3))) void*)(lds + buffer * kStage + (j * kWaves + wave) * 1024), 16, 0, 0);
-    }
-    // eight scales, of the last step the row's last eight moved down: where they
-    // are zeros in place of scales, so are the codes
+  uint32_t scales[2];
+  auto fetch = [&](int j, int step, int buffer) {
+    // (the compiler would keep eight advancing 64-bit addresses)
+    uint32_t row = row_at[j];
+    asm volatile("" : "+v"(row));
+    const int block = step * 8 + (from_a(j) ? block_a : block_b);
+    const uint8_t* from = (from_a(j) ? codes_a : codes_b) + row + 16 * static_cast<uint32_t>(block);
+    if (block >= blocks) from = zero_block;
+    __builtin_amdgcn_global_load_lds(
+        reinterpret_cast<const __attribute__((address_space(1))) void*>(reinterpret_cast<uint64_t>(from)),
+        (__attribute__((address_space(3))) void*)(lds + buffer * kStage + (j * kWaves + wave) * 1024), 16, 0, 0);
+  };
+  // eight scales, of the last step the row's last eight moved down: where they
+  // are zeros in place of scales, so are the codes
+  auto fetch_scales = [&](int step) {
     const int first = min(step * 8, blocks - 8), off = (step * 8 - first) * 8;
-#pragma unroll
-    for (int j = 0; j < kScaleRows; ++j) {
-      __builtin_memcpy(&scales[j], scale_row[j] + first, 8);
-      scales[j] >>= off;
-    }
+    uint64_t eight;
+    __builtin_memcpy(&eight, scale_row + first, 8);
+    eight >>= off;
+    scales[0] = static_cast<uint32_t>(eight), scales[1] = static_cast<uint32_t>(eight >> 32);
   };
   auto leave_scales = [&](int buffer) {
+    const uint32_t two[2] = {__builtin_amdgcn_perm(scales[1], scales[0], 0x05010400), __builtin_amdgcn_perm(scales[1], scales[0], 0x07030602)};
+    unsigned char* const to = lds + buffer * kStage + scales_at;
 #pragma unroll
-    for (int j = 0; j < kScaleRows; ++j)
-      reinterpret_cast<uint64_t*>(lds + buffer * kStage + kRows * 128)[j * kThreads + threadIdx.x] = scales[j];
+    for (int q = 0; q < 4; ++q) *reinterpret_cast<uint16_t*>(to + q * 16 * (share * 2)) = static_cast<uint16_t>(two[q / 2] >> (q % 2 * 16));
   };
 
   f32x4 sum[kM][kN] = {};
-  const int a0 = wave / kWavesN * (kM * 16), b0 = kTileM + wave % kWavesN * (kN * 16);
-  const unsigned at = (l16 * 128) + ((quad ^ (l16 >> 1 & 7)) * 16);
-  fetch(0, 0);
+  const int wave_a = wave / kWavesN * (kM * 16), wave_b = wave % kWavesN * (kN * 16);
+  const unsigned at_a = (wave_a + l16) * 128 + (quad ^ exchange(l16, false)) * 16;
+  // Row of b that is row l16 of the products' tile y.  For results of 16 bits
+  // it is such that a lane has eight neighbouring columns in two tiles.
+  auto row_b = [&](int y) { return kF32 ? y * 16 + l16 : y / 2 * 32 + l16 / 4 * 8 + y % 2 * 4 + l16 % 4; };
+  const unsigned at_b = (kTileM + wave_b + row_b(0)) * 128 + (quad ^ exchange(row_b(0), !kF32)) * 16;
+  auto from_row_b = [&](int y) { return (row_b(y) - row_b(0)) * 128; };
+#pragma unroll
+  for (int j = 0; j < kLoads; ++j) fetch(j, 0, 0);
+  fetch_scales(0);
   leave_scales(0);
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
   for (int step = 0; step < steps; ++step) {
     const int buffer = step & 1;
-    const unsigned char* const from = lds + buffer * kStage;
     // (of the last step a second time: without a branch the products stay where they are)
-    fetch(min(step + 1, steps - 1), buffer ^ 1);
-    u32x2 sa[kM], sb[kN];
+    const int next = min(step + 1, steps - 1);
+    const unsigned char* const from = lds + buffer * kStage;
+    uint32_t sa[kM / 2], sb[kN / 2];
+    __builtin_memcpy(sa, __builtin_assume_aligned(from + kRows * 128 + wave_a * 8 + lane * (kM * 2), kM * 2), kM * 2);
+    __builtin_memcpy(sb, __builtin_assume_aligned(from + kRows * 128 + (kTileM + wave_b) * 8 + lane * (kN * 2), kN * 2), kN * 2);
+    // Both halves' operands are in registers of their own: the second half's are
+    // read while the first half's products run, a tile of a at a time.
+    u32x4 a[2][kM], b[2][kN];
+    auto read_a = [&](int half, int x) { a[half][x] = *reinterpret_cast<const u32x4*>(from + x * 2048 + (at_a ^ (half * 64))); };
+    auto read_b = [&](int half, int y) { b[half][y] = *reinterpret_cast<const u32x4*>(from + from_row_b(y) + (at_b ^ (half * 64))); };
 #pragma unroll
-    for (int x = 0; x < kM; ++x) sa[x] = *reinterpret_cast<const u32x2*>(from + kRows * 128 + (a0 + x * 16 + l16) * 8) >> (quad * 8);
+    for (int y = 0; y < kN; ++y) read_b(0, y);
 #pragma unroll
-    for (int y = 0; y < kN; ++y) sb[y] = *reinterpret_cast<const u32x2*>(from + kRows * 128 + (b0 + y * 16 + l16) * 8) >> (quad * 8);
+    for (int x = 0; x < kM; ++x) read_a(0, x);
     __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      // a block of b for all of a's, which come two ahead: left to itself the
-      // compiler reads all of a step first and runs out of registers
-      u32x4 a[kM], b[kN];
-#pragma unroll
-      for (int y = 0; y < kN; ++y) b[y] = *reinterpret_cast<const u32x4*>(from + b0 * 128 + y * 2048 + (at ^ (half * 64)));
-#pragma unroll
-      for (int x = 0; x < kM; ++x) a[x] = *reinterpret_cast<const u32x4*>(from + a0 * 128 + x * 2048 + (at ^ (half * 64)));
-#pragma unroll
-      for (int x = 0; x < kM; ++x)
-#pragma unroll
-        for (int y = 0; y < kN; ++y) sum[x][y] = multiply<0, 0>(b[y], a[x], sum[x][y], sb[y][half], sa[x][half]);
-      schedule<kLdsRead, kN + 2>();
-#pragma unroll
-      for (int x = 0; x < kM; ++x) {
-        schedule<kMatrix, kN>();
-        schedule<kLdsRead, 1>();
-      }
-      __builtin_amdgcn_sched_barrier(0);
-    }
+    fetch_scales(next);
+    each<2>([&](auto half) {
+      each<kM>([&](auto x) {
+        each<kN>([&](auto y) {
+          sum[x][y] = multiply<y % 2 * 2 + half, x % 2 * 2 + half>(b[half][y], a[half][x], sum[x][y], sb[y / 2], sa[x / 2]);
+        });
+        if constexpr (half == 0) {
+          if constexpr (x < kN) read_b(1, x);
+          read_a(1, x);
+          constexpr int kEach = kLoads * 2 / kM;   // the loads in the first half of the first half
+          if constexpr (x * kEach < kLoads)
+            each<kEach>([&](auto j) { fetch(x * kEach + j, next, buffer ^ 1); });
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      });
+    });
     leave_scales(buffer ^ 1);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
   }
-  const int m0 = tm * kTileM + a0, n0 = tn * kTileN + b0 - kTileM;
-#pragma unroll
-  for (int x = 0; x < kM; ++x)
-#pragma unroll
-    for (int y = 0; y < kN; ++y) store4<kF32>(p, i, m0 + x * 16 + l16, n0 + y * 16 + quad * 4, sum[x][y]);
+  const int m0 = tm * kTileM + wave_a, n0 = tn * kTileN + wave_b;
+  each<kM>([&](auto x) {
+    if constexpr (kF32) {
+      each<kN>([&](auto y) { store4<kF32>(p, i, m0 + x * 16 + l16, n0 + y * 16 + quad * 4, sum[x][y]); });
+    } else {
+      each<kN / 2>([&](auto y) { store8(p, i, m0 + x * 16 + l16, n0 + y * 32 + quad * 8, sum[x][2 * y], sum[x][2 * y + 1]); });
+    }
+  });
 }
 
 template <int kTile, int kWavesM, int kWavesN, bool kF32>
