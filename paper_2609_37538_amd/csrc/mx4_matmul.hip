@@ -87,6 +87,25 @@ __device__ __forceinline__ void store8(const Mx4Product& p, int64_t batch, int m
   }
 }
 
+// Column of the result, and row of b, that is row l16 of tile y of the products'
+// second operand.  Results of 16 bits take them such that a lane has eight
+// neighbouring columns in two tiles, and four lanes 64 bytes.
+template <bool kF32>
+__device__ __forceinline__ constexpr int column_of(int y, int l16) {
+  return kF32 ? y * 16 + l16 : y / 2 * 32 + l16 / 4 * 8 + y % 2 * 4 + l16 % 4;
+}
+
+template <bool kF32, int kM, int kN>
+__device__ __forceinline__ void store_tiles(const Mx4Product& p, int64_t batch, int m, int n, int quad, f32x4 (&sum)[kM][kN]) {
+  each<kM>([&](auto x) {
+    if constexpr (kF32) {
+      each<kN>([&](auto y) { store4<kF32>(p, batch, m + x * 16, n + y * 16 + quad * 4, sum[x][y]); });
+    } else {
+      each<kN / 2>([&](auto y) { store8(p, batch, m + x * 16, n + y * 32 + quad * 8, sum[x][2 * y], sum[x][2 * y + 1]); });
+    }
+  });
+}
+
 // Few rows of a (up to 16 * kRowTiles): what counts is how fast b streams by.  A
 // workgroup takes 16 rows of b; its waves share the columns (wave w takes every
 // kWaves-th step of 128), several steps' loads in flight, and add up in LDS.
@@ -180,7 +199,7 @@ __global__ __launch_bounds__(kWavesM * kWavesN * 64) void tile_kernel(Mx4Product
   }
 #pragma unroll
   for (int r = 0; r < kN; ++r) {
-    const int64_t n = min(n0 + r * 16 + l16, p.n - 1);
+    const int64_t n = min(n0 + column_of<kF32>(r, l16), p.n - 1);
     cb[r] = n * p.b.code_stride, xb[r] = n * p.b.scale_stride;
   }
   f32x4 sum[kM][kN] = {};
@@ -204,10 +223,7 @@ __global__ __launch_bounds__(kWavesM * kWavesN * 64) void tile_kernel(Mx4Product
 #pragma unroll
       for (int y = 0; y < kN; ++y) sum[x][y] = multiply<0, 0>(b[y], a[x], sum[x][y], sb[y], sa[x]);
   }
-#pragma unroll
-  for (int x = 0; x < kM; ++x)
-#pragma unroll
-    for (int y = 0; y < kN; ++y) store4<kF32>(p, i, m0 + x * 16 + l16, n0 + y * 16 + quad * 4, sum[x][y]);
+  store_tiles<kF32>(p, i, m0 + l16, n0, quad, sum);
 }
 
 // What columns past the end read in place of codes.
@@ -305,11 +321,9 @@ __global__ __launch_bounds__(kWavesM * kWavesN * 64, kWavesM * kWavesN / 4) void
   f32x4 sum[kM][kN] = {};
   const int wave_a = wave / kWavesN * (kM * 16), wave_b = wave % kWavesN * (kN * 16);
   const unsigned at_a = (wave_a + l16) * 128 + (quad ^ exchange(l16, false)) * 16;
-  // Row of b that is row l16 of the products' tile y.  For results of 16 bits
-  // it is such that a lane has eight neighbouring columns in two tiles.
-  auto row_b = [&](int y) { return kF32 ? y * 16 + l16 : y / 2 * 32 + l16 / 4 * 8 + y % 2 * 4 + l16 % 4; };
-  const unsigned at_b = (kTileM + wave_b + row_b(0)) * 128 + (quad ^ exchange(row_b(0), !kF32)) * 16;
-  auto from_row_b = [&](int y) { return (row_b(y) - row_b(0)) * 128; };
+  const int row_b = column_of<kF32>(0, l16);
+  const unsigned at_b = (kTileM + wave_b + row_b) * 128 + (quad ^ exchange(row_b, !kF32)) * 16;
+  auto from_row_b = [&](int y) { return (column_of<kF32>(y, l16) - row_b) * 128; };
 #pragma unroll
   for (int j = 0; j < kLoads; ++j) fetch(j, 0, 0);
   fetch_scales(0);
@@ -343,9 +357,8 @@ __global__ __launch_bounds__(kWavesM * kWavesN * 64, kWavesM * kWavesN / 4) void
         if constexpr (half == 0) {
           if constexpr (x < kN) read_b(1, x);
           read_a(1, x);
-          constexpr int kEach = kLoads * 2 / kM;   // the loads in the first half of the first half
-          if constexpr (x * kEach < kLoads)
-            each<kEach>([&](auto j) { fetch(x * kEach + j, next, buffer ^ 1); });
+          // spread over the half: all of them ahead of the products took 6% longer
+          each<kLoads / kM>([&](auto j) { fetch(x * (kLoads / kM) + j, next, buffer ^ 1); });
         }
         __builtin_amdgcn_sched_barrier(0);
       });
@@ -355,13 +368,7 @@ __global__ __launch_bounds__(kWavesM * kWavesN * 64, kWavesM * kWavesN / 4) void
     __syncthreads();
   }
   const int m0 = tm * kTileM + wave_a, n0 = tn * kTileN + wave_b;
-  each<kM>([&](auto x) {
-    if constexpr (kF32) {
-      each<kN>([&](auto y) { store4<kF32>(p, i, m0 + x * 16 + l16, n0 + y * 16 + quad * 4, sum[x][y]); });
-    } else {
-      each<kN / 2>([&](auto y) { store8(p, i, m0 + x * 16 + l16, n0 + y * 32 + quad * 8, sum[x][2 * y], sum[x][2 * y + 1]); });
-    }
-  });
+  store_tiles<kF32>(p, i, m0 + l16, n0, quad, sum);
 }
 
 template <int kTile, int kWavesM, int kWavesN, bool kF32>
