@@ -239,26 +239,33 @@ __device__ __forceinline__ int exchange(int row, bool by_eights) {
 // Steps of 256 columns go from global memory to LDS without passing registers, the
 // next step's while this one's products run: 64 matrix instructions per wave and step
 // at 256 x 256.  In LDS a row has its 128 bytes of the step, its eight blocks exchanged by
-// bits 1..3 of the row, so that the sixteen lanes that read one block of sixteen
-// rows meet every bank; eight neighbouring lanes fetch a row's whole line.
-template <int kTileM, int kTileN, int kWavesM, int kWavesN, bool kF32>
-__global__ __launch_bounds__(kWavesM * kWavesN * 64, kWavesM * kWavesN / 4) void staged_kernel(Mx4Product p, int tiles_m, int tiles_n) {
+// three bits of the row, so that the sixteen lanes that read one block of sixteen
+// rows meet every bank; eight neighbouring lanes fetch a row's whole line.  kGroups groups
+// of such waves share the columns, a run of steps each, and add up in LDS.
+// 8192 x 4096 x 4096 takes 83 to 97 us, 2.8 to 3.3 PFLOP/s.  Its loop takes 4200 cycles
+// per step where the products take 2048: 2500 without the loads, of which L2
+// delivers 64 KiB to each of 256 CUs per step, 8 TB/s; half the traffic per product
+// would need tiles that the registers do not hold.
+template <int kTileM, int kTileN, int kWavesM, int kWavesN, int kGroups, bool kF32>
+__global__ __launch_bounds__(kGroups * kWavesM * kWavesN * 64, kGroups * kWavesM * kWavesN / 4) void staged_kernel(Mx4Product p, int tiles_m, int tiles_n) {
   constexpr int kWaves = kWavesM * kWavesN, kThreads = kWaves * 64;
   constexpr int kM = kTileM / kWavesM / 16, kN = kTileN / kWavesN / 16;
   constexpr int kRows = kTileM + kTileN;                 // rows of a, then rows of b
   constexpr int kLoads = kRows / 8 / kWaves;             // eight rows each
-  static_assert(kRows % (8 * kWaves) == 0 && kRows == kThreads, "shares of the loads: a thread brings the scales of one row");
+  static_assert(kRows % (8 * kWaves) == 0 && kRows <= kThreads, "shares of the loads: a thread brings the scales of one row");
   constexpr int kStage = kRows * 136;                    // codes, then eight scales per row
-  extern __shared__ __align__(16) unsigned char lds[];   // [2]
+  extern __shared__ __align__(16) unsigned char all_lds[];   // [kGroups][2][kStage], then the groups' sums
   const int lane = threadIdx.x & 63, l16 = lane & 15, quad = lane >> 4;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int group = kGroups > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / kThreads) : 0;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) - group * kWaves;
+  unsigned char* const lds = all_lds + group * 2 * kStage;
   // tiles of eight rows of tiles follow each other down the columns, on one XCD,
   // so that its L2 holds the operands they share
   const unsigned total = gridDim.x, per = total / kXcds, more = total % kXcds, xcd = blockIdx.x % kXcds;
   const unsigned id = xcd * per + min(xcd, more) + blockIdx.x / kXcds;
   constexpr int kGroup = 8;
-  const int in_group = kGroup * tiles_n, group = id / in_group, rows_here = min(kGroup, tiles_m - group * kGroup);
-  const int tm = group * kGroup + (id - group * in_group) % rows_here, tn = (id - group * in_group) / rows_here;
+  const int in_band = kGroup * tiles_n, band = id / in_band, rows_here = min(kGroup, tiles_m - band * kGroup);
+  const int tm = band * kGroup + (id - band * in_band) % rows_here, tn = (id - band * in_band) / rows_here;
   const int64_t i = blockIdx.y;
   const int blocks = p.k / kMx4Block, steps = (blocks + 7) / 8;
 
@@ -280,7 +287,7 @@ __global__ __launch_bounds__(kWavesM * kWavesN * 64, kWavesM * kWavesN / 4) void
   }
   // The scales of a row: in LDS lane l of a wave's products finds its bytes, a
   // tile of 16 rows after the other, first and second half of the step, in one place.
-  const int row = threadIdx.x, of_b = row - kTileM;
+  const int row = threadIdx.x % kRows, of_b = row - kTileM;
   const bool is_a = of_b < 0;
   const Mx4View& x = is_a ? p.a : p.b;
   const uint8_t* const scale_row = x.scales + i * x.scale_batch_stride +
@@ -305,7 +312,7 @@ __global__ __launch_bounds__(kWavesM * kWavesN * 64, kWavesM * kWavesN / 4) void
   // eight scales, of the last step the row's last eight moved down: where they
   // are zeros in place of scales, so are the codes
   auto fetch_scales = [&](int step) {
-    const int first = min(step * 8, blocks - 8), off = (step * 8 - first) * 8;
+    const int within = min(step, steps - 1) * 8, first = min(within, blocks - 8), off = (within - first) * 8;
     uint64_t eight;
     __builtin_memcpy(&eight, scale_row + first, 8);
     eight >>= off;
@@ -313,6 +320,7 @@ __global__ __launch_bounds__(kWavesM * kWavesN * 64, kWavesM * kWavesN / 4) void
   };
   auto leave_scales = [&](int buffer) {
     const uint32_t two[2] = {__builtin_amdgcn_perm(scales[1], scales[0], 0x05010400), __builtin_amdgcn_perm(scales[1], scales[0], 0x07030602)};
+    if (kRows < kThreads && wave * 64 >= kRows) return;
     unsigned char* const to = lds + buffer * kStage + scales_at;
 #pragma unroll
     for (int q = 0; q < 4; ++q) *reinterpret_cast<uint16_t*>(to + q * 16 * (share * 2)) = static_cast<uint16_t>(two[q / 2] >> (q % 2 * 16));
@@ -324,16 +332,18 @@ __global__ __launch_bounds__(kWavesM * kWavesN * 64, kWavesM * kWavesN / 4) void
   const int row_b = column_of<kF32>(0, l16);
   const unsigned at_b = (kTileM + wave_b + row_b) * 128 + (quad ^ exchange(row_b, !kF32)) * 16;
   auto from_row_b = [&](int y) { return (column_of<kF32>(y, l16) - row_b) * 128; };
+  // a group's steps follow each other; what it takes past the last step are zeros
+  const int first_step = group * ((steps + kGroups - 1) / kGroups), steps_here = (steps + kGroups - 1) / kGroups;
 #pragma unroll
-  for (int j = 0; j < kLoads; ++j) fetch(j, 0, 0);
-  fetch_scales(0);
+  for (int j = 0; j < kLoads; ++j) fetch(j, first_step, 0);
+  fetch_scales(first_step);
   leave_scales(0);
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
-  for (int step = 0; step < steps; ++step) {
+  for (int step = 0; step < steps_here; ++step) {
     const int buffer = step & 1;
-    // (of the last step a second time: without a branch the products stay where they are)
-    const int next = min(step + 1, steps - 1);
+    // (after the last step too: without a branch the products stay where they are)
+    const int next = first_step + step + 1;
     const unsigned char* const from = lds + buffer * kStage;
     uint32_t sa[kM / 2], sb[kN / 2];
     __builtin_memcpy(sa, __builtin_assume_aligned(from + kRows * 128 + wave_a * 8 + lane * (kM * 2), kM * 2), kM * 2);
@@ -367,43 +377,85 @@ __global__ __launch_bounds__(kWavesM * kWavesN * 64, kWavesM * kWavesN / 4) void
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
   }
+  if constexpr (kGroups > 1) {
+    f32x4* const sums = reinterpret_cast<f32x4*>(all_lds);
+    each<kM>([&](auto x) {
+      each<kN>([&](auto y) {
+        if (group > 0) sums[((group - 1) * kM * kN + x * kN + y) * kThreads + wave * 64 + lane] = sum[x][y];
+      });
+    });
+    __syncthreads();
+    if (group > 0) return;
+    each<kM>([&](auto x) {
+      each<kN>([&](auto y) {
+        each<kGroups - 1>([&](auto g) { sum[x][y] += sums[(g * kM * kN + x * kN + y) * kThreads + wave * 64 + lane]; });
+      });
+    });
+  }
   const int m0 = tm * kTileM + wave_a, n0 = tn * kTileN + wave_b;
   store_tiles<kF32>(p, i, m0 + l16, n0, quad, sum);
 }
 
-template <int kTile, int kWavesM, int kWavesN, bool kF32>
+template <int kTile, int kWavesM, int kWavesN, int kGroups, bool kF32>
 hipError_t launch_staged(const Mx4Product& p, int64_t tiles_m, int64_t tiles_n, hipStream_t s) {
-  constexpr int kLds = 2 * 2 * kTile * 136;
+  constexpr int kLds = kGroups * 2 * 2 * kTile * 136;
   static_assert(kLds <= 160 * 1024, "LDS of a workgroup");
-  const auto kernel = &staged_kernel<kTile, kTile, kWavesM, kWavesN, kF32>;
+  const auto kernel = &staged_kernel<kTile, kTile, kWavesM, kWavesN, kGroups, kF32>;
   static const hipError_t ready =
       hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
   if (ready != hipSuccess) return ready;
-  kernel<<<dim3(static_cast<unsigned>(tiles_m * tiles_n), p.batch), kWavesM * kWavesN * 64, kLds, s>>>(
+  kernel<<<dim3(static_cast<unsigned>(tiles_m * tiles_n), p.batch), kGroups * kWavesM * kWavesN * 64, kLds, s>>>(
       p, static_cast<int>(tiles_m), static_cast<int>(tiles_n));
   return hipGetLastError();
 }
 
+// Which kernel, by what each took (us, bfloat16 results, one call after the other in
+// a graph).  With 256 columns or more, which is a step of the staged kernels:
+//   rows x columns of out, k   thin   64, 2 groups   128, 2 groups    128    256
+//       1 x  4096, 4096         4.3       7.9            12.9        18.7
+//       1 x 32768, 4096        19.0      13.5            19.3        25.2
+//      32 x  4096, 4096         7.6       8.7            13.1        19.1
+//      64 x  4096, 4096        11.4       9.0            13.5        19.8
+//     512 x  4096, 4096                  13.5            15.0        20.9
+//    1024 x  4096, 4096                  24.9            17.3        22.6   34.0
+//    1536 x  4096, 4096                  37.3            32.7        29.6   38.3
+//    2304 x  4096, 4096                  55.6            50.8        51.6   39.0
+//    8192 x  4096, 4096                                             112.9   83.2
+//    2500 x  4096,  512                  19.8            16.3        12.8   12.1
+// Two groups halve the steps that wait for memory one after the other, while a
+// tile for each CU, or two, is all there is; large tiles read less per product.
+// With fewer columns (heads x rows x columns, k):
+//                              thin  straight from memory
+//     16 x  32 x 512, 128       3.0       3.7
+//      8 x 128 x 512, 224       4.2       5.2
+//     64 x   8 x 512, 128       3.9       3.7
+//    128 x 128 x 512, 128      25.5       7.2
 template <bool kF32>
 hipError_t launch(const Mx4Product& p, hipStream_t s) {
-  const int64_t tiles_m = (p.m + 127) / 128, tiles_n = (p.n + 127) / 128;
-  const int64_t wide_m = (p.m + 255) / 256, wide_n = (p.n + 255) / 256;
-  if (tiles_m * tiles_n > INT32_MAX) return hipErrorInvalidValue;
-  constexpr int64_t kCus = 256;
+  auto tiles = [](int64_t rows, int64_t by) { return (rows + by - 1) / by; };
+  const int64_t tiles_m = tiles(p.m, 128), tiles_n = tiles(p.n, 128), wide_m = tiles(p.m, 256), wide_n = tiles(p.n, 256);
+  const int64_t small_m = tiles(p.m, 64), small_n = tiles(p.n, 64);
+  if (small_m * small_n > INT32_MAX) return hipErrorInvalidValue;
   // offsets within a tile's rows are held in 32 bits
   const int64_t longest = std::max(p.a.code_stride, p.b.code_stride);
-  const bool staged = p.k > 512 && p.a.code_stride >= 0 && p.b.code_stride >= 0 && longest * 256 + p.k < (int64_t{1} << 31);
-  if (p.m <= 64 || tiles_m * tiles_n * p.batch < kCus / 2) {
-    const int rows = p.m <= 16 ? 16 : p.m <= 32 ? 32 : 64;
-    if ((p.m + rows - 1) / rows > 65535) return hipErrorInvalidValue;
-    const dim3 grid((p.n + 15) / 16, (p.m + rows - 1) / rows, p.batch);
+  const bool staged = p.k >= 256 && p.a.code_stride >= 0 && p.b.code_stride >= 0 && longest * 256 + p.k < (int64_t{1} << 31);
+  const int rows = p.m <= 16 ? 16 : p.m <= 32 ? 32 : 64;
+  const int64_t pieces = tiles(p.n, 16) * tiles(p.m, rows) * (rows / 16) * p.batch;
+  if (staged ? p.m <= 32 && pieces <= 512 : pieces <= 2048) {
+    const dim3 grid(tiles(p.n, 16), tiles(p.m, rows), p.batch);
     if (rows == 16) thin_kernel<1, 8, kF32><<<grid, 512, 0, s>>>(p);
     else if (rows == 32) thin_kernel<2, 4, kF32><<<grid, 256, 0, s>>>(p);
     else thin_kernel<4, 4, kF32><<<grid, 256, 0, s>>>(p);
     return hipGetLastError();
   }
-  if (staged && wide_m * wide_n * p.batch >= kCus) return launch_staged<256, 2, 4, kF32>(p, wide_m, wide_n, s);
-  if (staged) return launch_staged<128, 2, 2, kF32>(p, tiles_m, tiles_n, s);
+  if (staged) {
+    const int64_t all = tiles_m * tiles_n * p.batch;
+    if (small_m * small_n * p.batch <= 512) return launch_staged<64, 2, 2, 2, kF32>(p, small_m, small_n, s);
+    if (all <= 256) return launch_staged<128, 2, 2, 2, kF32>(p, tiles_m, tiles_n, s);
+    // (large tiles that few rows or columns leave half empty are no gain)
+    if (all > 512 && wide_m * wide_n * p.batch * 4 <= all + all / 4) return launch_staged<256, 2, 4, 1, kF32>(p, wide_m, wide_n, s);
+    return launch_staged<128, 2, 2, 1, kF32>(p, tiles_m, tiles_n, s);
+  }
   tile_kernel<128, 128, 2, 2, kF32><<<dim3(static_cast<unsigned>(tiles_m * tiles_n), p.batch), 256, 0, s>>>(
       p, static_cast<int>(tiles_m), static_cast<int>(tiles_n));
   return hipGetLastError();
