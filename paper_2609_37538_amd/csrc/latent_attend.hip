@@ -4,6 +4,8 @@
 // row's latent part is key and value at once, so a row is brought in once per
 // workgroup and serves up to 64 heads twice: 2 * (576 + 512) operations per row
 // and head, on the matrix cores.
+#include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "latent_internal.h"
@@ -65,7 +67,7 @@ __device__ __forceinline__ Share share_of(const AttendParams& p, int head_blocks
   // serves the rows that they share
   const unsigned total = gridDim.x, per = total / kXcds, more = total % kXcds, xcd = blockIdx.x % kXcds;
   const unsigned id = xcd * per + min(xcd, more) + blockIdx.x / kXcds;
-  const unsigned share = head_blocks * p.splits;
+  const unsigned share = head_blocks * p.plan.splits;
   w.token = id / share;
   w.head_block = (id % share) % head_blocks;
   w.split = (id % share) / head_blocks;
@@ -140,8 +142,8 @@ __device__ __forceinline__ bf16x8 load_query(const AttendParams& p, const Share&
 template <int kColTiles, typename Out>
 __device__ __forceinline__ void store_head(const AttendParams& p, const Share& w, int head, int col, Out out, float reference,
                                            float all, bool first) {
-  if (p.splits > 1) {
-    const int64_t part = (w.token * p.splits + w.split) * p.heads + head;
+  if (p.plan.splits > 1) {
+    const int64_t part = (w.token * p.plan.splits + w.split) * p.heads + head;
     if (first) p.part_ml[part] = f32x2{reference, all};
 #pragma unroll
     for (int c = 0; c < kColTiles; ++c) *reinterpret_cast<f32x4*>(p.part_out + part * kLatent + col + c * 16) = out(c);
@@ -166,12 +168,14 @@ __device__ __forceinline__ void store_head(const AttendParams& p, const Share& w
 // (16 bytes, four products' eight columns each), of bfloat16 ones eight columns
 // of every 32.
 
-// Up to 16 heads.  Four waves score 16 rows each against all 576 columns, leave
-// weights and expanded values in LDS, and take 128 of the 512 columns each of the
-// output.  So few heads make the rows' bytes count, and two workgroups per CU
-// keep 50 KB of them in flight.
+// 16 heads at a time: few heads, or few tokens.  Four waves score 16 rows each against
+// all 576 columns, leave weights and expanded values in LDS, and take 128 of the 512
+// columns each of the output.  So few heads make the rows' bytes count, and two
+// workgroups per CU keep 50 KB of them in flight: 4 x 131072 rows of 400 bytes for 16 heads
+// take 52 us, 4.0 TB/s, where a large copy moves 5.0.  A call of one token takes 8 us,
+// launch, three dependent loads (entry, row, next tile's) and one tile.
 template <bool kMx4>
-__global__ __launch_bounds__(256, 2) void attend_kernel(AttendParams p, int tiles_per_split) {
+__global__ __launch_bounds__(256, 2) void attend_kernel(AttendParams p, int head_blocks, int tiles_per_split) {
   constexpr int kWaves = 4, kCols = kLatent / kWaves, kColTiles = kCols / 16;
   constexpr int kLoads = kMx4 ? 4 : 16;
   extern __shared__ __align__(16) unsigned char lds[];
@@ -183,7 +187,8 @@ __global__ __launch_bounds__(256, 2) void attend_kernel(AttendParams p, int tile
 
   const int lane = threadIdx.x & 63, l16 = lane & 15, quad = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const Share w = share_of(p, 1, tiles_per_split, kRowTile);
+  const Share w = share_of(p, head_blocks, tiles_per_split, kRowTile);
+  const int head = w.head_block * 16 + l16;
 
   // every lane finds the row whose keys it loads, what is read of it two tiles ahead
   RowFinder finder;
@@ -193,7 +198,7 @@ __global__ __launch_bounds__(256, 2) void attend_kernel(AttendParams p, int tile
   bf16x8 query[18];
 #pragma unroll
   for (int j = 0; j < 18; ++j)
-    query[j] = load_query(p, w, l16, kMx4 && j < 16 ? (j / 4 * 4 + quad) * 32 + j % 4 * 8 : 32 * j + 8 * quad);
+    query[j] = load_query(p, w, head, kMx4 && j < 16 ? (j / 4 * 4 + quad) * 32 + j % 4 * 8 : 32 * j + 8 * quad);
 
   u32x4 key[kLoads], scales{}, turned[2];
   unsigned counts = 0;   // bits of this lane's four rows (quad * 4 + i) that count
@@ -315,15 +320,15 @@ __global__ __launch_bounds__(256, 2) void attend_kernel(AttendParams p, int tile
   sum += __shfl_xor(sum, 32);
   if (quad == 0) wave_top[wave * 16 + l16] = sum;
   __syncthreads();
-  if (l16 >= p.heads) return;
+  if (head >= p.heads) return;
   float all = 0.f;
 #pragma unroll
   for (int i = 0; i < kWaves; ++i) all += wave_top[i * 16 + l16];
-  store_head<kColTiles>(p, w, l16, wave * kCols + quad * 4, [&](int c) { return out[c]; }, reference[l16], all,
+  store_head<kColTiles>(p, w, head, wave * kCols + quad * 4, [&](int c) { return out[c]; }, reference[l16], all,
                         wave == 0 && quad == 0);
 }
 
-// More than 16 heads, 64 at a time.  Eight waves work on 32 rows in three stages,
+// 64 heads at a time, of many tokens.  Eight waves work on 32 rows in three stages,
 // each a tile behind the one before, with one barrier per tile:
 //   scores   wave (rg, kg) multiplies a quarter of the key columns of 16 rows with
 //            the queries of all 64 heads (held in registers), and leaves the values that
@@ -335,7 +340,11 @@ __global__ __launch_bounds__(256, 2) void attend_kernel(AttendParams p, int tile
 // Alone, each stage keeps one unit of a CU busy (matrix cores, LDS, conversion,
 // exponentials) and then waits for the others' waves: one after the other, with
 // a barrier each, they took 7100 cycles per 64 rows, of which the matrix cores worked
-// 2200, also with two such workgroups of 32 heads on a CU.  In one stream they overlap.
+// 2200, also with two such workgroups of 32 heads on a CU.  In one stream they overlap:
+// 2300 cycles per 32 rows, the matrix cores 1100, and 97 us for 128 tokens of 128 heads
+// over 2048 rows each (73 GFLOP).  What is left is spread: without the loads it took
+// 19% less, without the writes of values 20%, without the exchange of scores 15%,
+// without the output's products 19%.
 constexpr int kWideRows = 32;
 constexpr int kWideHeads = 64;
 
@@ -594,19 +603,31 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams p, int
   }
 }
 
-// Joins the parts of one (query token, head).  The parts' factors are made once;
-// then four groups of threads add up every fourth part, four columns per thread,
-// with several parts in flight.
+// Joins the parts of one (query token, head), kCols of its columns: the parts' factors
+// are made once, then groups of threads share the parts, four columns per thread, with several
+// parts in flight.  Fewer columns per workgroup are for few results of many parts:
+// 16 results of 512 parts took 57 us with the attention before them, and 34 so.
 constexpr int kMostSplits = 512;
-constexpr int kJoinGroups = 4;
-__global__ __launch_bounds__(kJoinGroups * kLatent / 4) void combine_kernel(AttendParams p) {
+template <int kCols>
+__global__ __launch_bounds__(kMostSplits) void combine_kernel(AttendParams p) {
+  constexpr int kLanes = kCols / 4, kGroups = kMostSplits / kLanes, kFirst = 8;
   __shared__ float factor[kMostSplits], per_wave[2][8];
-  __shared__ f32x4 group_sum[kJoinGroups - 1][kLatent / 4];
+  __shared__ f32x4 group_sum[kGroups - 1][kLanes];
   const int64_t token = blockIdx.x / p.heads;
   const int head = static_cast<int>(blockIdx.x - token * p.heads);
-  const int64_t first = token * p.splits * p.heads + head;
+  const int64_t first = token * p.plan.splits * p.heads + head;
   const int tid = threadIdx.x, wave = tid / 64;
-  const f32x2 ml = tid < p.splits ? p.part_ml[first + static_cast<int64_t>(tid) * p.heads] : f32x2{-INFINITY, 0.f};
+  const f32x2 ml = tid < p.plan.splits ? p.part_ml[first + static_cast<int64_t>(tid) * p.heads] : f32x2{-INFINITY, 0.f};
+  // the first parts come while their factors are found
+  const int group = tid / kLanes, col = blockIdx.y * kCols + tid % kLanes * 4;
+  const float* part = p.part_out + first * kLatent + col;
+  const int64_t stride = static_cast<int64_t>(p.heads) * kLatent;
+  f32x4 early[kFirst];
+#pragma unroll
+  for (int i = 0; i < kFirst; ++i) {
+    const int at = group + i * kGroups;
+    early[i] = at < p.plan.splits ? *reinterpret_cast<const f32x4*>(part + at * stride) : f32x4{};
+  }
   float top = ml[1] != 0.f ? ml[0] : -INFINITY;   // a part without a row that counts has no reference
 #pragma unroll
   for (int d = 32; d > 0; d /= 2) top = fmaxf(top, __shfl_xor(top, d));
@@ -626,25 +647,63 @@ __global__ __launch_bounds__(kJoinGroups * kLatent / 4) void combine_kernel(Atte
 #pragma unroll
   for (int i = 0; i < 8; ++i) all += per_wave[1][i];
 
-  const int group = tid / (kLatent / 4), col = tid % (kLatent / 4) * 4;
-  const float* part = p.part_out + first * kLatent + col;
-  const int64_t stride = static_cast<int64_t>(p.heads) * kLatent;
   f32x4 o{};
+#pragma unroll
+  for (int i = 0; i < kFirst; ++i) {
+    const int at = group + i * kGroups;
+    if (at < p.plan.splits) o += early[i] * factor[at];
+  }
 #pragma unroll 8
-  for (int i = group; i < p.splits; i += kJoinGroups) o += *reinterpret_cast<const f32x4*>(part + i * stride) * factor[i];
-  if (group > 0) group_sum[group - 1][col / 4] = o;
+  for (int i = group + kFirst * kGroups; i < p.plan.splits; i += kGroups)
+    o += *reinterpret_cast<const f32x4*>(part + i * stride) * factor[i];
+  if (group > 0) group_sum[group - 1][tid % kLanes] = o;
   __syncthreads();
   if (group > 0) return;
 #pragma unroll
-  for (int g = 0; g < kJoinGroups - 1; ++g) o += group_sum[g][col / 4];
+  for (int g = 0; g < kGroups - 1; ++g) o += group_sum[g][tid % kLanes];
   o *= all == 0.f ? 0.f : 1.f / all;
   *reinterpret_cast<bf16x4*>(p.out + token * p.out_token_stride + head * p.out_head_stride + col) = rounded(o);
-  if (p.lse && tid == 0) p.lse[token * p.heads + head] = all == 0.f ? -INFINITY : (base + __builtin_amdgcn_logf(all)) * kLn2;
+  if (p.lse && tid == 0 && col == 0) p.lse[token * p.heads + head] = all == 0.f ? -INFINITY : (base + __builtin_amdgcn_logf(all)) * kLn2;
 }
 
-// Workgroups that share the heads of a query token, and rows of their tiles.
-int head_blocks_of(int heads) { return heads <= 16 ? 1 : (heads + kWideHeads - 1) / kWideHeads; }
-int tile_rows_of(int heads) { return heads <= 16 ? kRowTile : kWideRows; }
+// The same for up to kMost parts, which is most calls: a thread makes the factors itself, without a barrier, and adds up
+// four columns of a result (8192 results of 2 parts: 21 us by the kernel above, 8 us by this).
+template <int kMost>
+__global__ __launch_bounds__(256) void combine_few_kernel(AttendParams p) {
+  const int64_t result = static_cast<int64_t>(blockIdx.x) * 2 + threadIdx.x / 128;
+  const int64_t token = result / p.heads;
+  if (token >= static_cast<int64_t>(p.cache.batch) * p.n_q) return;
+  const int head = static_cast<int>(result - token * p.heads), col = threadIdx.x % 128 * 4;
+  const int64_t first = token * p.plan.splits * p.heads + head;
+  f32x4 part[kMost];
+  f32x2 ml[kMost];
+#pragma unroll
+  for (int i = 0; i < kMost; ++i) {
+    const int64_t at = first + static_cast<int64_t>(min(i, p.plan.splits - 1)) * p.heads;
+    ml[i] = p.part_ml[at];
+    part[i] = i < p.plan.splits ? *reinterpret_cast<const f32x4*>(p.part_out + at * kLatent + col) : f32x4{};
+  }
+  float top = -INFINITY, all = 0.f;
+#pragma unroll
+  for (int i = 0; i < kMost; ++i) {
+    if (i >= p.plan.splits) ml[i][1] = 0.f;
+    if (ml[i][1] != 0.f) top = fmaxf(top, ml[i][0]);   // a part without a row that counts has no reference
+  }
+  const float base = zero_if_none(top);
+  f32x4 o{};
+#pragma unroll
+  for (int i = 0; i < kMost; ++i) {
+    const float w = ml[i][1] != 0.f ? __builtin_amdgcn_exp2f(ml[i][0] - base) : 0.f;
+    all += w * ml[i][1];
+    o += part[i] * w;
+  }
+  o *= all == 0.f ? 0.f : 1.f / all;
+  *reinterpret_cast<bf16x4*>(p.out + token * p.out_token_stride + head * p.out_head_stride + col) = rounded(o);
+  if (p.lse && col == 0) p.lse[token * p.heads + head] = all == 0.f ? -INFINITY : (base + __builtin_amdgcn_logf(all)) * kLn2;
+}
+
+int head_blocks_of(int heads, bool wide) { return wide ? (heads + kWideHeads - 1) / kWideHeads : (heads + 15) / 16; }
+int tile_rows_of(bool wide) { return wide ? kWideRows : kRowTile; }
 
 template <typename Kernel>
 hipError_t allow_lds(Kernel kernel, size_t lds) {
@@ -652,12 +711,12 @@ hipError_t allow_lds(Kernel kernel, size_t lds) {
 }
 
 template <bool kMx4>
-hipError_t launch_narrow(const AttendParams& p, int64_t groups, int tiles_per_split, hipStream_t s) {
+hipError_t launch_narrow(const AttendParams& p, int64_t groups, int head_blocks, int tiles_per_split, hipStream_t s) {
   constexpr size_t lds = kValueBytes + 2048 + 5 * 16 * 4 + 16;
   static_assert(2 * lds <= 160 * 1024, "LDS of two workgroups");
   static const hipError_t ready = allow_lds(&attend_kernel<kMx4>, lds);
   if (ready != hipSuccess) return ready;
-  attend_kernel<kMx4><<<dim3(static_cast<unsigned>(groups)), 256, lds, s>>>(p, tiles_per_split);
+  attend_kernel<kMx4><<<dim3(static_cast<unsigned>(groups)), 256, lds, s>>>(p, head_blocks, tiles_per_split);
   return hipGetLastError();
 }
 
@@ -674,31 +733,79 @@ hipError_t launch_wide(const AttendParams& p, int64_t groups, int head_blocks, i
 
 template <bool kMx4>
 hipError_t launch_format(const AttendParams& p, hipStream_t s) {
-  const int head_blocks = head_blocks_of(p.heads), rows = tile_rows_of(p.heads);
-  const int tiles = (p.topk + rows - 1) / rows, each = (tiles + p.splits - 1) / p.splits;
-  const int64_t groups = static_cast<int64_t>(p.cache.batch) * p.n_q * head_blocks * p.splits;
+  const int head_blocks = head_blocks_of(p.heads, p.plan.wide), rows = tile_rows_of(p.plan.wide), splits = p.plan.splits;
+  const int tiles = (p.topk + rows - 1) / rows, each = (tiles + splits - 1) / splits;
+  const int64_t groups = static_cast<int64_t>(p.cache.batch) * p.n_q * head_blocks * splits;
   if (groups > INT32_MAX) return hipErrorInvalidValue;
-  return p.heads <= 16 ? launch_narrow<kMx4>(p, groups, each, s) : launch_wide<kMx4>(p, groups, head_blocks, each, s);
+  return p.plan.wide ? launch_wide<kMx4>(p, groups, head_blocks, each, s) : launch_narrow<kMx4>(p, groups, head_blocks, each, s);
+}
+
+// Time of a call in us, from ones that were timed in a graph: what a workgroup needs
+// at its start and end, its tiles of 64 rows, and the parts written and joined.
+// Where a CU has one workgroup of the narrow kernel and not two, each is faster.
+double attend_cost(bool mx4, bool wide, int64_t tokens, int heads, int tiles, int splits) {
+  const int64_t groups = tokens * head_blocks_of(heads, wide) * splits;
+  const int each = (tiles + splits - 1) / splits;
+  double at = 0;
+  if (wide) {
+    const double ends = 6.3 + 0.13 * std::min(heads, kWideHeads) + (groups > 128 ? 2.5 : 0.);
+    at = static_cast<double>((groups + 255) / 256) * (ends + 2.1 * each);
+  } else if (groups <= 256) {
+    at = 6.4 + (mx4 ? 1.7 : 3.) * each;
+  } else {
+    at = static_cast<double>((groups + 511) / 512) * (11. + (mx4 ? 2.15 : 4.7) * each);
+  }
+  const double megabytes = static_cast<double>(tokens) * splits * heads * (kLatent * 4) / 1e6;
+  return splits > 1 ? at + 2.5 + (wide ? 0.25 : 0.45) * megabytes : at;
 }
 
 }  // namespace
 
-// Splits so that every CU has work (two workgroups of up to 16 heads, one of
-// 64), but no part smaller than a tile of 64 rows.
-int attend_splits(int batch, int n_q, int heads, int topk) {
-  constexpr int64_t kCus = 256;
-  const int64_t groups = static_cast<int64_t>(batch) * n_q * head_blocks_of(heads);
-  const int64_t want = (heads <= 16 ? 2 * kCus : kCus) / groups;
-  const int tiles = (topk + 63) / 64;
-  if (want <= 1 || tiles <= 1) return 1;
-  const int64_t each = (tiles + want - 1) / want;
-  return static_cast<int>((tiles + each - 1) / each);
+// Which kernel, and how many workgroups share a token's rows: the least of the times
+// above for parts that give 128, 256 or 512 workgroups.  Measured (us, 4-bit rows; the
+// narrow kernel in 256 and in 512 workgroups, the wide one in 128 and in 256):
+//   tokens x heads x rows     narrow 256    512     wide 128    256
+//       1 x 64 x   256          10.5       10.5       17.0      16.9
+//       4 x 64 x  2048          17.2       23.6       26.5      26.6
+//      33 x 40 x  1000          25.4       26.6       29.2      27.7
+//      33 x 64 x   256          13.2       20.7       24.4      26.5
+//      64 x 64 x  2048          60.5       51.8       53.7      40.7
+//     128 x 64 x   256          20.0       20.1       23.0      29.2
+//     128 x 128 x 2048         153.6      153.4       83.7      83.8
+//   the same in bfloat16:
+//       4 x 64 x  2048          19.7       26.4       27.4      27.6
+//      16 x 64 x  2048          37.3       37.3       31.2      29.9
+AttendPlan attend_plan(int format, int batch, int n_q, int heads, int topk) {
+  const int64_t tokens = static_cast<int64_t>(batch) * n_q;
+  const int tiles = (topk + kRowTile - 1) / kRowTile;
+  AttendPlan best{false, 1};
+  double least = INFINITY;
+  for (int wide = 0; wide < (heads > 16 ? 2 : 1); ++wide) {
+    const int64_t groups = tokens * head_blocks_of(heads, wide != 0);
+    int last = 0;
+    for (int64_t target : {128, 256, 512}) {
+      const int64_t want = std::max<int64_t>(1, std::min<int64_t>(target / groups, tiles));
+      const int each = static_cast<int>((tiles + want - 1) / std::max<int64_t>(1, want));
+      const int splits = each > 0 ? (tiles + each - 1) / each : 1;
+      if (splits == last) continue;
+      last = splits;
+      const double cost = attend_cost(format == 1, wide != 0, tokens, heads, tiles, splits);
+      if (cost < least) least = cost, best = {wide != 0, splits};
+    }
+  }
+  return best;
 }
 
 hipError_t launch_attend(const AttendParams& p, int format, hipStream_t s) {
   hipError_t e = format == 1 ? launch_format<true>(p, s) : launch_format<false>(p, s);
-  if (e != hipSuccess || p.splits <= 1) return e;
-  combine_kernel<<<dim3(static_cast<unsigned>(p.cache.batch * p.n_q * p.heads)), kJoinGroups * kLatent / 4, 0, s>>>(p);
+  const int splits = p.plan.splits;
+  if (e != hipSuccess || splits <= 1) return e;
+  const int64_t results = static_cast<int64_t>(p.cache.batch) * p.n_q * p.heads;
+  const unsigned pairs = static_cast<unsigned>((results + 1) / 2);
+  if (splits <= 4) combine_few_kernel<4><<<pairs, 256, 0, s>>>(p);
+  else if (splits <= 16) combine_few_kernel<16><<<pairs, 256, 0, s>>>(p);
+  else if (results <= 128) combine_kernel<128><<<dim3(static_cast<unsigned>(results), 4), kMostSplits, 0, s>>>(p);
+  else combine_kernel<512><<<dim3(static_cast<unsigned>(results)), kMostSplits, 0, s>>>(p);
   return hipGetLastError();
 }
 

@@ -3,6 +3,7 @@
 // keeps state beyond the calling thread's last error text.
 #include "avsg_latent.h"
 
+#include <algorithm>
 #include <cstdarg>
 #include <cstdio>
 
@@ -139,7 +140,9 @@ avsg_status avsg_kv_read(const avsg_cache* cache, int64_t n, const int32_t* d_re
 
 size_t avsg_attend_workspace_bytes(int32_t batch, int32_t n_q, int32_t heads, int32_t topk) {
   if (batch < 1 || n_q < 1 || heads < 1 || topk < 1) return 0;
-  const size_t splits = static_cast<size_t>(attend_splits(batch, n_q, heads, topk));
+  // of either row format, whichever has more parts
+  const size_t splits = static_cast<size_t>(std::max(attend_plan(AVSG_ROWS_BF16, batch, n_q, heads, topk).splits,
+                                                     attend_plan(AVSG_ROWS_MX4, batch, n_q, heads, topk).splits));
   if (splits <= 1) return 0;
   const size_t parts = static_cast<size_t>(batch) * n_q * splits * heads;
   return parts * (kLatent * sizeof(float) + sizeof(f32x2));
@@ -172,13 +175,13 @@ avsg_status avsg_attend(const avsg_cache* cache, const avsg_attention* a, void* 
   p.out_token_stride = a->out_token_stride;
   p.out_head_stride = a->out_head_stride;
   p.lse = a->d_lse;
-  p.splits = attend_splits(cache->batch, a->n_q, a->heads, a->topk);
-  const size_t need = avsg_attend_workspace_bytes(cache->batch, a->n_q, a->heads, a->topk);
-  if (need > 0) {
+  p.plan = attend_plan(cache->format, cache->batch, a->n_q, a->heads, a->topk);
+  if (p.plan.splits > 1) {
+    const size_t need = avsg_attend_workspace_bytes(cache->batch, a->n_q, a->heads, a->topk);
     if (!d_workspace || !aligned(d_workspace, 256) || workspace_bytes < need)
       return fail(AVSG_E_INVAL, "the workspace must be 256-byte aligned and hold %zu bytes", need);
     p.part_out = static_cast<float*>(d_workspace);
-    p.part_ml = reinterpret_cast<f32x2*>(p.part_out + static_cast<size_t>(tokens) * p.splits * p.heads * kLatent);
+    p.part_ml = reinterpret_cast<f32x2*>(p.part_out + static_cast<size_t>(tokens) * p.plan.splits * p.heads * kLatent);
   }
   return launched(launch_attend(p, cache->format, static_cast<hipStream_t>(stream)), "avsg_attend");
 }

@@ -122,6 +122,12 @@ struct ReadParams {
   int64_t out_stride;
 };
 
+// How a call of attention is carried out.
+struct AttendPlan {
+  bool wide;        // 64 heads per workgroup, not 16
+  int32_t splits;   // workgroups that share a query token's entries
+};
+
 struct AttendParams {
   CacheView cache;
   int32_t n_q, heads, topk;
@@ -134,7 +140,7 @@ struct AttendParams {
   __bf16* out;
   int64_t out_token_stride, out_head_stride;
   float* lse;
-  int32_t splits;       // workgroups that share a query token's entries
+  AttendPlan plan;
   float* part_out;      // [B n_q][splits][heads][512], splits > 1
   f32x2* part_ml;       // [B n_q][splits][heads]: maximum and sum
 };
@@ -158,7 +164,7 @@ struct Mx4Product {
 hipError_t launch_kv_append(const AppendParams& p, int format, int rope_style, hipStream_t s);
 hipError_t launch_kv_read(const ReadParams& p, int format, hipStream_t s);
 // entries of a query token each workgroup takes, and how many share one
-int attend_splits(int batch, int n_q, int heads, int topk);
+AttendPlan attend_plan(int format, int batch, int n_q, int heads, int topk);
 hipError_t launch_attend(const AttendParams& p, int format, hipStream_t s);
 hipError_t launch_mx4_quantize(const void* x, bool f32, int64_t rows, int64_t cols, int64_t x_stride, uint8_t* codes,
                                uint8_t* scales, hipStream_t s);

@@ -153,6 +153,61 @@ def test_attend_masks(mx4):
 
 
 @pytest.mark.parametrize("mx4", [False, True])
+@pytest.mark.parametrize("batch,n_q,heads,k,slots", [
+    (33, 2, 64, 700, 1024), (65, 2, 64, 300, 512), (50, 2, 33, 1500, 2048), (150, 2, 70, 100, 128),
+    (9, 1, 16, 4096, 4096), (64, 1, 128, 33, 64), (16, 1, 130, 900, 1024)])
+def test_attend_many_tokens(batch, n_q, heads, k, slots, mx4):
+    """Enough tokens that 64 heads share a workgroup, with and without parts to join, and more parts
+    than one thread takes; tokens without rows, tiles without rows, and NaN in rows that do not count."""
+    from paper_2609_37538_amd import latent as L
+    g = gen(batch + heads + k)
+    pool = pool_of(g, batch, slots, mx4)
+    pool[:, 5::7] = 0xff
+    cache = L.LatentCache(pool, batch, int(mx4))
+    q = normal(g, batch, n_q, heads, 576)
+    rows = torch.randint(0, slots, (batch, n_q, k), generator=g, device="cuda").to(torch.int32)
+    index = torch.where(rows % 7 == 5, -1, torch.randint(0, 2 * k, rows.shape, generator=g, device="cuda")).to(torch.int32)
+    index[batch // 2, 0, :k // 2] = 2 ** 31 - 1
+    lens = torch.randint(0, 2 * k + 1, (batch, n_q), generator=g, device="cuda")
+    lens[0, 0], lens[-1, -1] = 0, 2 * k
+    out, lse = cache.attend(q, rows=rows, index=index, lens=lens, scale=SCALE)
+    assert (out[0, 0] == 0).all() and (lse[0, 0] == -math.inf).all()
+    some = torch.tensor(sorted({0, 1, batch // 2, batch - 1}), device="cuda")
+    few = L.LatentCache(pool[some].contiguous(), len(some), int(mx4))
+    pick = lambda x: x[some].contiguous()  # noqa: E731
+    check_attend(few, pick(q), pick(out), pick(lse), pick(rows), pick(index), pick(lens))
+    assert torch.isfinite(out).all()
+
+
+@pytest.mark.parametrize("mx4", [False, True])
+@pytest.mark.parametrize("order", ["rising", "falling", "one far above", "far below zero"])
+def test_attend_score_ranges_many_tokens(order, mx4):
+    """The same ranges as below, with every token of a large batch at another place of the ramp."""
+    from paper_2609_37538_amd import latent as L
+    g = gen(17)
+    batch, k, heads = 66, 700, 64
+    latent, rope = normal(g, k, 512, by=0.1), normal(g, k, 64, by=0.1)
+    ramp = torch.linspace(-6, 6, k, device="cuda")
+    if order == "falling":
+        ramp = -ramp
+    elif order == "one far above":
+        ramp = torch.where(torch.arange(k, device="cuda") == 500, 6.0, -6.0)
+    elif order == "far below zero":
+        ramp = ramp - 30
+    latent[:, :32] = ramp[:, None].to(torch.bfloat16)
+    pool = row_bytes(latent, rope, mx4).unsqueeze(0).expand(batch, -1, -1).contiguous()
+    cache = L.LatentCache(pool, batch, int(mx4))
+    rows = ((torch.arange(k, device="cuda")[None] + 10 * torch.arange(batch, device="cuda")[:, None]) % k).to(torch.int32)
+    rows = rows.view(batch, 1, k).contiguous()
+    q = normal(g, batch, 1, heads, 576)
+    q[..., :32] = 1.0 + torch.arange(heads, device="cuda")[:, None] / heads
+    out, lse = cache.attend(q, rows=rows, scale=1.5)
+    some = torch.tensor([0, 1, 30, batch - 1], device="cuda")
+    few = L.LatentCache(pool[some].contiguous(), len(some), int(mx4))
+    check_attend(few, q[some].contiguous(), out[some].contiguous(), lse[some].contiguous(), rows[some].contiguous(), scale=1.5)
+
+
+@pytest.mark.parametrize("mx4", [False, True])
 @pytest.mark.parametrize("order", ["rising", "falling", "one far above", "far below zero"])
 def test_attend_score_ranges(order, mx4):
     """Scores that grow over hundreds along the entries, so that every later row outweighs all before
