@@ -331,48 +331,84 @@ class Mx4:
     """A matrix or a batch of them in 4-bit microscaled form: codes uint8 [..., K/2] (column 2i in
     the low half of byte i) and scales uint8 [..., K/32]."""
 
-    __slots__ = ("codes", "scales", "_view")
+    # Small calls cost more time on the host than on the GPU, so what mx4_quantize makes is
+    # one allocation, and its tensors are made where they are asked for.
+    __slots__ = ("device", "_shape", "_codes", "_scales", "_base", "_code_strides", "_scale_strides", "_view")
 
     def __init__(self, codes, scales):
         torch = _torch()
         _need(codes.dtype == torch.uint8 and scales.dtype == torch.uint8 and codes.is_cuda
               and codes.device == scales.device, "codes and scales must be uint8 tensors on one GPU")
-        _need(codes.dim() in (2, 3) and codes.shape[:-1] == scales.shape[:-1]
-              and codes.shape[-1] == scales.shape[-1] * (AVSG_MX4_BLOCK // 2),
+        cs, ss = codes.shape, scales.shape
+        _need(len(cs) in (2, 3) and cs[:-1] == ss[:-1] and cs[-1] == ss[-1] * (AVSG_MX4_BLOCK // 2),
               "codes [..., K/2] and scales [..., K/32] must belong together and have two or three dimensions")
-        self.codes, self.scales, self._view = codes, scales, None
+        self.device, self._shape = codes.device, (*cs[:-1], cs[-1] * 2)
+        self._codes, self._scales, self._base, self._view = codes, scales, None, None
 
     @property
     def shape(self):
         """Of the matrix it stands for."""
-        return (*self.codes.shape[:-1], self.codes.shape[-1] * 2)
+        return self._shape
+
+    @property
+    def codes(self):
+        if self._codes is None:
+            k = self._shape[-1]
+            self._codes = self._base.as_strided((*self._shape[:-1], k // 2), (*self._code_strides, 1), 0)
+        return self._codes
+
+    @property
+    def scales(self):
+        if self._scales is None:
+            k, n = self._shape[-1], self._base.shape[0]
+            self._scales = self._base.as_strided((*self._shape[:-1], k // AVSG_MX4_BLOCK), (*self._scale_strides, 1), n // 17 * 16)
+        return self._scales
 
     def transpose(self, i: int, j: int) -> "Mx4":
         """With two leading dimensions exchanged (the columns stay in place)."""
-        n = self.codes.dim()
+        n = len(self._shape)
         _need(i % n != n - 1 and j % n != n - 1, "columns cannot be exchanged: blocks lie along them")
-        return _mx4(self.codes.transpose(i, j), self.scales.transpose(i, j))
+        if self._base is None:
+            return Mx4(self._codes.transpose(i, j), self._scales.transpose(i, j))
+        if i % n == j % n:
+            return self
+        s, c, b = self._shape, self._code_strides, self._scale_strides
+        return _mx4(self.device, self._base, (s[1], s[0], s[2]), (c[1], c[0]), (b[1], b[0]))
 
     def _c(self) -> AvsgMx4:
         """The matrix as the library takes it; made once, for codes and scales do not move."""
-        if self._view is None:
-            c, s = self.codes, self.scales
-            if not c.numel():
-                self._view = AvsgMx4(c.data_ptr(), s.data_ptr(), 0, 0, 0, 0)
-                return self._view
-            cs = [0 if n == 1 else st for st, n in zip(c.stride(), c.shape)]
-            ss = [0 if n == 1 else st for st, n in zip(s.stride(), s.shape)]
-            _need(c.stride(-1) == 1 and ss[-1] <= 1 and c.data_ptr() & 15 == 0 and all(st % 16 == 0 for st in cs[:-1]),
-                  "rows of codes must be contiguous and 16-byte aligned")
-            three = len(cs) == 3
-            self._view = AvsgMx4(c.data_ptr(), s.data_ptr(), cs[-2], cs[0] if three else 0, ss[-2], ss[0] if three else 0)
-        return self._view
+        view = self._view
+        if view is not None:
+            return view
+        if self._base is not None:
+            at, n = self._base.data_ptr(), self._base.shape[0]
+            cs, ss = self._code_strides, self._scale_strides
+            view = (AvsgMx4(at, at + n // 17 * 16, cs[-1], cs[0], ss[-1], ss[0]) if len(cs) == 2
+                    else AvsgMx4(at, at + n // 17 * 16, cs[0], 0, ss[0], 0))
+        else:
+            c, s = self._codes, self._scales
+            at, cs, ss = c.data_ptr(), c.stride(), s.stride()
+            if 0 in self._shape:
+                cs = ss = (0,) * (len(cs) - 1) + (1,)
+            elif 1 in self._shape or s.shape[-1] == 1:     # strides of dimensions of one entry do not matter
+                cs = tuple(0 if n == 1 else st for st, n in zip(cs[:-1], c.shape)) + cs[-1:]
+                ss = tuple(0 if n == 1 else st for st, n in zip(ss[:-1], s.shape)) + (1 if s.shape[-1] == 1 else ss[-1],)
+            if len(cs) == 2:
+                _need(cs[1] == 1 and ss[1] == 1 and not (at | cs[0]) & 15, "rows of codes must be contiguous and 16-byte aligned")
+                view = AvsgMx4(at, s.data_ptr(), cs[0], 0, ss[0], 0)
+            else:
+                _need(cs[2] == 1 and ss[2] == 1 and not (at | cs[0] | cs[1]) & 15,
+                      "rows of codes must be contiguous and 16-byte aligned")
+                view = AvsgMx4(at, s.data_ptr(), cs[1], cs[0], ss[1], ss[0])
+        self._view = view
+        return view
 
 
-def _mx4(codes, scales) -> Mx4:
-    """An Mx4 of tensors that are known to belong together."""
+def _mx4(device, base, shape, code_strides, scale_strides) -> Mx4:
+    """An Mx4 in one allocation: the codes, then the scales, a seventeenth of it."""
     m = Mx4.__new__(Mx4)
-    m.codes, m.scales, m._view = codes, scales, None
+    m.device, m._base, m._shape, m._code_strides, m._scale_strides = device, base, shape, code_strides, scale_strides
+    m._codes = m._scales = m._view = None
     return m
 
 
@@ -401,31 +437,40 @@ def mx4_quantize(x) -> Mx4:
               "x: rows must be contiguous and 16-byte aligned")
     at = x.data_ptr()
     _need(at & 15 == 0, "x: rows must be 16-byte aligned")
-    codes = torch.empty((*shape[:-1], k // 2), dtype=torch.uint8, device=dev)
-    scales = torch.empty((*shape[:-1], k // AVSG_MX4_BLOCK), dtype=torch.uint8, device=dev)
-    _run(_lib.avsg_mx4_quantize, "avsg_mx4_quantize", dev.index, at, dtype, rows, k, stride, codes.data_ptr(),
-         scales.data_ptr())
-    return _mx4(codes, scales)
+    code_bytes, blocks = rows * (k // 2), k // AVSG_MX4_BLOCK
+    base = torch.empty(code_bytes + rows * blocks, dtype=torch.uint8, device=dev)
+    to = base.data_ptr()
+    _run(_lib.avsg_mx4_quantize, "avsg_mx4_quantize", dev.index, at, dtype, rows, k, stride, to, to + code_bytes)
+    if dims == 2:
+        return _mx4(dev, base, (rows, k), (k // 2,), (blocks,))
+    r = shape[1]
+    return _mx4(dev, base, (shape[0], r, k), (r * (k // 2), k // 2), (r * blocks, blocks))
 
 
 def mx4_dequantize(m: Mx4, dtype=None):
     """The values that a contiguous Mx4 stands for, in bfloat16 (the default) or float32."""
-    codes, scales = m.codes, m.scales
-    _need(codes.is_contiguous() and scales.is_contiguous(), "codes and scales must be contiguous")
-    out = _t.empty(m.shape, dtype=dtype or _t.bfloat16, device=codes.device)
-    kind, k = _plain_type(out, "dtype"), out.shape[-1]
-    _run(_lib.avsg_mx4_dequantize, "avsg_mx4_dequantize", codes.device.index,
-         AvsgMx4(codes.data_ptr(), scales.data_ptr(), k // 2, 0, k // AVSG_MX4_BLOCK, 0),
-         out.numel() // k if k else 0, k, out.data_ptr(), kind, k)
+    shape, dev, k = m._shape, m.device, m._shape[-1]
+    strides = m._code_strides if m._base is not None else ()
+    if strides and strides[-1] == k // 2 and (len(strides) == 1 or strides[0] == shape[1] * strides[1]):
+        at = m._base.data_ptr()
+        scales_at = at + m._base.shape[0] // 17 * 16
+    else:
+        codes, scales = m.codes, m.scales
+        _need(codes.is_contiguous() and scales.is_contiguous(), "codes and scales must be contiguous")
+        at, scales_at = codes.data_ptr(), scales.data_ptr()
+    out = _t.empty(shape, dtype=dtype or _t.bfloat16, device=dev)
+    kind, rows = _plain_type(out, "dtype"), shape[0] * (shape[1] if len(shape) == 3 else 1)
+    _run(_lib.avsg_mx4_dequantize, "avsg_mx4_dequantize", dev.index,
+         AvsgMx4(at, scales_at, k // 2, 0, k // AVSG_MX4_BLOCK, 0), rows if k else 0, k, out.data_ptr(), kind, k)
     return out
 
 
 def mx4_matmul(a: Mx4, b: Mx4, out=None, dtype=None):
     """a b^T for a [M][K] and b [N][K], or for batches of both; `out` ([M][N] or [batch][M][N],
     bfloat16 or float32, rows contiguous) or a new tensor of `dtype` (bfloat16)."""
-    sa, sb, dev = a.shape, b.shape, a.codes.device
+    sa, sb, dev = a._shape, b._shape, a.device
     three = len(sa) == 3
-    if len(sa) != len(sb) or sa[-1] != sb[-1] or dev != b.codes.device or (three and sa[0] != sb[0]):
+    if len(sa) != len(sb) or sa[-1] != sb[-1] or dev != b.device or (three and sa[0] != sb[0]):
         raise ValueError("a and b must have the same dimensions, batch, columns and GPU")
     shape = (*sa[:-1], sb[-2])
     if out is None:
