@@ -13,14 +13,12 @@
 namespace avsg {
 namespace {
 
-constexpr int kRowTile = 64;                  // rows of one pass through the narrow kernel's loop
 // Values in LDS: rows of 1024 bytes.  Of every 256 bytes (all banks) row x has
 // its 32-byte pieces exchanged by x mod 8 and the halves of a piece by bit 3 of
 // x.  Sixteen lanes that write 16 bytes each of the same columns of 16 rows, and
 // groups of 16 lanes that read 32 bytes each of four rows, then meet every
 // bank equally often.
 constexpr int kValueStride = kLatent * 2;
-constexpr int kValueBytes = kRowTile * kValueStride;
 // Byte of a row's 256 at which 16-byte part `part` lies.
 __device__ __forceinline__ unsigned value_part(unsigned row, unsigned part) {
   return ((part ^ ((row & 7) * 2 + ((row >> 3) & 1))) & 15) * 16;
@@ -173,26 +171,29 @@ __device__ __forceinline__ void store_head(const AttendParams& p, const Share& w
 // columns each of the output.  So few heads make the rows' bytes count, and two
 // workgroups per CU keep 50 KB of them in flight: 4 x 131072 rows of 400 bytes for 16 heads
 // take 52 us, 4.0 TB/s, where a large copy moves 5.0.  A call of one token takes 8 us,
-// launch, three dependent loads (entry, row, next tile's) and one tile.
-template <bool kMx4>
-__global__ __launch_bounds__(256, 2) void attend_kernel(AttendParams p, int head_blocks, int tiles_per_split) {
-  constexpr int kWaves = 4, kCols = kLatent / kWaves, kColTiles = kCols / 16;
+// launch, three dependent loads (entry, row, next tile's) and one tile.  Or eight waves
+// and tiles of 128 rows: 2.4 to 2.6 us each where a lone workgroup of four takes 1.7 for 64,
+// and half the parts of two workgroups.
+template <bool kMx4, int kWaves>
+__global__ __launch_bounds__(kWaves * 64, 2) void attend_kernel(AttendParams p, int head_blocks, int tiles_per_split) {
+  constexpr int kRows = kWaves * 16, kCols = kLatent / kWaves, kColTiles = kCols / 16;
+  constexpr int kPairs = kWaves / 2;   // of 16-row tiles, as the output product takes them
   constexpr int kLoads = kMx4 ? 4 : 16;
   extern __shared__ __align__(16) unsigned char lds[];
   unsigned char* const values = lds;
-  unsigned char* const weights = lds + kValueBytes;                              // [2][64 lanes] 16 bytes
-  float* const wave_top = reinterpret_cast<float*>(weights + 2048);              // [4][16]
+  unsigned char* const weights = lds + kRows * kValueStride;                              // [kPairs][64 lanes] 16 bytes
+  float* const wave_top = reinterpret_cast<float*>(weights + kPairs * 1024);     // [kWaves][16]
   float* const reference = wave_top + kWaves * 16;                               // [16]
-  int* const raised = reinterpret_cast<int*>(reference + 16);                    // [4]
+  int* const raised = reinterpret_cast<int*>(reference + 16);                    // [2]
 
   const int lane = threadIdx.x & 63, l16 = lane & 15, quad = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const Share w = share_of(p, head_blocks, tiles_per_split, kRowTile);
+  const Share w = share_of(p, head_blocks, tiles_per_split, kRows);
   const int head = w.head_block * 16 + l16;
 
   // every lane finds the row whose keys it loads, what is read of it two tiles ahead
   RowFinder finder;
-  finder.look(p, w, wave * 16 + l16, kRowTile);
+  finder.look(p, w, wave * 16 + l16, kRows);
   if (threadIdx.x < 16) reference[threadIdx.x] = -INFINITY;
   if (threadIdx.x < 4) raised[threadIdx.x] = 0;
   bf16x8 query[18];
@@ -205,7 +206,7 @@ __global__ __launch_bounds__(256, 2) void attend_kernel(AttendParams p, int head
   auto load_keys = [&](int t) {
     const unsigned x = lane_here();
     uint64_t at = finder.address(p, w);
-    finder.look(p, w, (t + 1) * kRowTile + wave * 16 + (x & 15), kRowTile);
+    finder.look(p, w, (t + 1) * kRows + wave * 16 + (x & 15), kRows);
     counts = static_cast<unsigned>(__ballot(at != 0) >> (x / 16 * 4)) & 15u;
     if (at == 0) at = reinterpret_cast<uint64_t>(zero_row);
     if constexpr (kMx4) scales = load_global<u32x4>(at + kMx4CodeBytes);
@@ -291,7 +292,9 @@ __global__ __launch_bounds__(256, 2) void attend_kernel(AttendParams p, int head
 
     const unsigned from = values_from(lane_here(), wave * kCols);
     const unsigned char* const weight_from = weights + lane_here() * 16;
-    const bf16x8 e[2] = {*reinterpret_cast<const bf16x8*>(weight_from), *reinterpret_cast<const bf16x8*>(weight_from + 1024)};
+    bf16x8 e[kPairs];
+#pragma unroll
+    for (int i = 0; i < kPairs; ++i) e[i] = *reinterpret_cast<const bf16x8*>(weight_from + i * 1024);
     // operands are read four products ahead: left to itself the compiler waits for each
     auto load_step = [&](int n) {   // column tile n % kColTiles of rows n / kColTiles * 32 .. + 31
       return load_values(values, (from ^ (n % kColTiles * 32)) + n / kColTiles * 32 * kValueStride);
@@ -301,14 +304,14 @@ __global__ __launch_bounds__(256, 2) void attend_kernel(AttendParams p, int head
 #pragma unroll
     for (int n = 0; n < kAhead; ++n) v[n] = load_step(n);
 #pragma unroll
-    for (int n = 0; n < 2 * kColTiles; ++n) {
+    for (int n = 0; n < kPairs * kColTiles; ++n) {
       const bf16x8 x = v[n % kAhead];
-      if (n + kAhead < 2 * kColTiles) v[n % kAhead] = load_step(n + kAhead);
+      if (n + kAhead < kPairs * kColTiles) v[n % kAhead] = load_step(n + kAhead);
       out[n % kColTiles] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, e[n / kColTiles], out[n % kColTiles], 0, 0, 0);
     }
-    kSchedule(kLdsRead, 2 + 2 * kAhead);
+    kSchedule(kLdsRead, kPairs + 2 * kAhead);
 #pragma unroll
-    for (int n = 0; n < 2 * kColTiles; ++n) {
+    for (int n = 0; n < kPairs * kColTiles; ++n) {
       kSchedule(kMatrix, 1);
       kSchedule(kLdsRead, 2);
     }
@@ -702,21 +705,20 @@ __global__ __launch_bounds__(256) void combine_few_kernel(AttendParams p) {
   if (p.lse && col == 0) p.lse[token * p.heads + head] = all == 0.f ? -INFINITY : (base + __builtin_amdgcn_logf(all)) * kLn2;
 }
 
-int head_blocks_of(int heads, bool wide) { return wide ? (heads + kWideHeads - 1) / kWideHeads : (heads + 15) / 16; }
-int tile_rows_of(bool wide) { return wide ? kWideRows : kRowTile; }
+int head_blocks_of(int heads, AttendKernel kernel) { return (heads + heads_of(kernel) - 1) / heads_of(kernel); }
 
 template <typename Kernel>
 hipError_t allow_lds(Kernel kernel, size_t lds) {
   return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lds));
 }
 
-template <bool kMx4>
+template <bool kMx4, int kWaves>
 hipError_t launch_narrow(const AttendParams& p, int64_t groups, int head_blocks, int tiles_per_split, hipStream_t s) {
-  constexpr size_t lds = kValueBytes + 2048 + 5 * 16 * 4 + 16;
-  static_assert(2 * lds <= 160 * 1024, "LDS of two workgroups");
-  static const hipError_t ready = allow_lds(&attend_kernel<kMx4>, lds);
+  constexpr size_t lds = kWaves * 16 * kValueStride + kWaves / 2 * 1024 + (kWaves + 1) * 16 * 4 + 16;
+  static_assert(8 / kWaves * lds <= 160 * 1024, "LDS of a CU's workgroups");
+  static const hipError_t ready = allow_lds(&attend_kernel<kMx4, kWaves>, lds);
   if (ready != hipSuccess) return ready;
-  attend_kernel<kMx4><<<dim3(static_cast<unsigned>(groups)), 256, lds, s>>>(p, head_blocks, tiles_per_split);
+  attend_kernel<kMx4, kWaves><<<dim3(static_cast<unsigned>(groups)), kWaves * 64, lds, s>>>(p, head_blocks, tiles_per_split);
   return hipGetLastError();
 }
 
@@ -733,64 +735,72 @@ hipError_t launch_wide(const AttendParams& p, int64_t groups, int head_blocks, i
 
 template <bool kMx4>
 hipError_t launch_format(const AttendParams& p, hipStream_t s) {
-  const int head_blocks = head_blocks_of(p.heads, p.plan.wide), rows = tile_rows_of(p.plan.wide), splits = p.plan.splits;
-  const int tiles = (p.topk + rows - 1) / rows, each = (tiles + splits - 1) / splits;
-  const int64_t groups = static_cast<int64_t>(p.cache.batch) * p.n_q * head_blocks * splits;
+  const AttendKernel kernel = p.plan.kernel;
+  const int head_blocks = head_blocks_of(p.heads, kernel), rows = kernel == AttendKernel::k64Heads ? kWideRows : rows_of(kernel);
+  const int tiles = (p.topk + rows - 1) / rows, each = (tiles + p.plan.splits - 1) / p.plan.splits;
+  const int64_t groups = static_cast<int64_t>(p.cache.batch) * p.n_q * head_blocks * p.plan.splits;
   if (groups > INT32_MAX) return hipErrorInvalidValue;
-  return p.plan.wide ? launch_wide<kMx4>(p, groups, head_blocks, each, s) : launch_narrow<kMx4>(p, groups, head_blocks, each, s);
+  switch (kernel) {
+    case AttendKernel::k16Heads: return launch_narrow<kMx4, 4>(p, groups, head_blocks, each, s);
+    case AttendKernel::k16HeadsAlone: return launch_narrow<kMx4, 8>(p, groups, head_blocks, each, s);
+    default: return launch_wide<kMx4>(p, groups, head_blocks, each, s);
+  }
 }
 
 // Time of a call in us, from ones that were timed in a graph: what a workgroup needs
-// at its start and end, its tiles of 64 rows, and the parts written and joined.
-// Where a CU has one workgroup of the narrow kernel and not two, each is faster.
-double attend_cost(bool mx4, bool wide, int64_t tokens, int heads, int tiles, int splits) {
-  const int64_t groups = tokens * head_blocks_of(heads, wide) * splits;
+// at its start and end, its tiles, and the parts written and joined.  916 calls
+// of 1 to 128 tokens, 8 to 128 heads, 150 to 2048 rows and of long contexts took 6%
+// more or less than this says, and the choices made by it 0.4% more than the best.
+double attend_cost(bool mx4, AttendKernel kernel, int64_t tokens, int heads, int tiles, int splits) {
+  const int64_t groups = tokens * head_blocks_of(heads, kernel) * splits;
   const int each = (tiles + splits - 1) / splits;
+  auto rounds = [&](int64_t at_once) { return static_cast<double>((groups + at_once - 1) / at_once); };
   double at = 0;
-  if (wide) {
-    const double ends = 6.3 + 0.13 * std::min(heads, kWideHeads) + (groups > 128 ? 2.5 : 0.);
-    at = static_cast<double>((groups + 255) / 256) * (ends + 2.1 * each);
-  } else if (groups <= 256) {
-    at = 6.4 + (mx4 ? 1.7 : 3.) * each;
-  } else {
-    at = static_cast<double>((groups + 511) / 512) * (11. + (mx4 ? 2.15 : 4.7) * each);
-  }
+  if (kernel == AttendKernel::k64Heads) at = rounds(256) * (6.3 + 0.13 * std::min(heads, 64) + (mx4 ? 2.1 : 2.4) * each);
+  else if (kernel == AttendKernel::k16HeadsAlone) at = rounds(256) * (9. + (mx4 ? 2.55 : 5.) * each);
+  else if (groups <= 256) at = 6.4 + (mx4 ? 1.7 : 3.05) * each;   // a CU has one workgroup and not two
+  else at = rounds(512) * (11. + (mx4 ? 2.15 : 4.75) * each);
+  if (splits == 1) return at;
   const double megabytes = static_cast<double>(tokens) * splits * heads * (kLatent * 4) / 1e6;
-  return splits > 1 ? at + 2.5 + (wide ? 0.25 : 0.45) * megabytes : at;
+  return at + 2.5 + 0.45 * std::min(megabytes, 17.) + 0.2 * std::max(megabytes - 17., 0.);
 }
 
 }  // namespace
 
 // Which kernel, and how many workgroups share a token's rows: the least of the times
-// above for parts that give 128, 256 or 512 workgroups.  Measured (us, 4-bit rows; the
-// narrow kernel in 256 and in 512 workgroups, the wide one in 128 and in 256):
-//   tokens x heads x rows     narrow 256    512     wide 128    256
-//       1 x 64 x   256          10.5       10.5       17.0      16.9
-//       4 x 64 x  2048          17.2       23.6       26.5      26.6
-//      33 x 40 x  1000          25.4       26.6       29.2      27.7
-//      33 x 64 x   256          13.2       20.7       24.4      26.5
-//      64 x 64 x  2048          60.5       51.8       53.7      40.7
-//     128 x 64 x   256          20.0       20.1       23.0      29.2
-//     128 x 128 x 2048         153.6      153.4       83.7      83.8
+// above for parts that give 128, 256 or 512 workgroups.  Measured (us, 4-bit rows; 16 heads
+// with 64-row tiles in 256 and 512 workgroups, with 128-row tiles in 256, 64 heads
+// in 128 and 256):
+//   tokens x heads x rows    64 rows: 256    512    128 rows    64 heads: 128    256
+//       1 x  64 x   256         10.5        10.5      13.3          16.8        16.8
+//       4 x  64 x  2048         17.5        23.1      18.7          27.1        27.2
+//      33 x  40 x  1000         25.7        26.8      23.6          29.4        27.8
+//      33 x  64 x  1000         33.2        30.8      27.9          33.9        31.5
+//      64 x  64 x  2048         60.6        52.0      47.7          54.5        40.7
+//     128 x  64 x   256         20.1        20.1      27.5          23.2        29.2
+//     128 x 128 x  2048        153.5       153.8     183.7          83.6        83.5
+//       4 x  16 x 131072        66.3        53.7      53.5
 //   the same in bfloat16:
-//       4 x 64 x  2048          19.7       26.4       27.4      27.6
-//      16 x 64 x  2048          37.3       37.3       31.2      29.9
+//       4 x  64 x  2048         20.1        25.6      21.5          28.2        28.5
+//      16 x  64 x  2048         37.4        37.5      35.0          31.5        30.2
 AttendPlan attend_plan(int format, int batch, int n_q, int heads, int topk) {
   const int64_t tokens = static_cast<int64_t>(batch) * n_q;
-  const int tiles = (topk + kRowTile - 1) / kRowTile;
-  AttendPlan best{false, 1};
+  AttendPlan best{AttendKernel::k16Heads, 1};
   double least = INFINITY;
-  for (int wide = 0; wide < (heads > 16 ? 2 : 1); ++wide) {
-    const int64_t groups = tokens * head_blocks_of(heads, wide != 0);
+  for (AttendKernel kernel : {AttendKernel::k16Heads, AttendKernel::k16HeadsAlone, AttendKernel::k64Heads}) {
+    if (kernel == AttendKernel::k64Heads && heads <= 16) break;
+    const int64_t groups = tokens * head_blocks_of(heads, kernel);
+    const int tiles = (topk + rows_of(kernel) - 1) / rows_of(kernel);
     int last = 0;
     for (int64_t target : {128, 256, 512}) {
+      if (target == 512 && kernel != AttendKernel::k16Heads) break;   // one workgroup per CU
       const int64_t want = std::max<int64_t>(1, std::min<int64_t>(target / groups, tiles));
-      const int each = static_cast<int>((tiles + want - 1) / std::max<int64_t>(1, want));
+      const int each = static_cast<int>((tiles + want - 1) / want);
       const int splits = each > 0 ? (tiles + each - 1) / each : 1;
       if (splits == last) continue;
       last = splits;
-      const double cost = attend_cost(format == 1, wide != 0, tokens, heads, tiles, splits);
-      if (cost < least) least = cost, best = {wide != 0, splits};
+      const double cost = attend_cost(format == 1, kernel, tokens, heads, tiles, splits);
+      if (cost < least) least = cost, best = {kernel, splits};
     }
   }
   return best;

@@ -123,8 +123,17 @@ struct ReadParams {
 };
 
 // How a call of attention is carried out.
+enum class AttendKernel {
+  k16Heads,        // 16 heads per workgroup, tiles of 64 rows, two workgroups per CU
+  k16HeadsAlone,   // 16 heads, tiles of 128 rows, one workgroup per CU
+  k64Heads,        // 64 heads, one workgroup per CU
+};
+constexpr int heads_of(AttendKernel k) { return k == AttendKernel::k64Heads ? 64 : 16; }
+// the least part of a token's rows that a workgroup takes
+constexpr int rows_of(AttendKernel k) { return k == AttendKernel::k16HeadsAlone ? 128 : 64; }
+
 struct AttendPlan {
-  bool wide;        // 64 heads per workgroup, not 16
+  AttendKernel kernel;
   int32_t splits;   // workgroups that share a query token's entries
 };
 

@@ -231,6 +231,35 @@ def test_attend_score_ranges(order, mx4):
     check_attend(cache, q, out, lse, scale=1.5)
 
 
+@pytest.mark.parametrize("batch,heads,k,mx4", [(132, 64, 700, True), (33, 40, 1000, True), (66, 32, 600, True),
+                                               (130, 16, 500, False), (128, 16, 600, False), (40, 40, 1000, False)])
+@pytest.mark.parametrize("order", ["rising", "falling"])
+def test_attend_rising_and_masked(order, batch, heads, k, mx4):
+    """Scores that grow or fall along the entries, of which some do not count and hold NaN, in batches of
+    the sizes between few tokens and many: tiles of every kind, whole and in parts."""
+    from paper_2609_37538_amd import latent as L
+    g = gen(batch + heads)
+    slots = k + 50
+    latent, rope = normal(g, slots, 512, by=0.1), normal(g, slots, 64, by=0.1)
+    ramp = torch.linspace(-6, 6, slots, device="cuda")
+    latent[:, :32] = (ramp if order == "rising" else -ramp)[:, None].to(torch.bfloat16)
+    pool = row_bytes(latent, rope, mx4).unsqueeze(0).expand(batch, -1, -1).contiguous()
+    pool[:, 3::11] = 0xff
+    cache = L.LatentCache(pool, batch, int(mx4))
+    first = torch.arange(batch, device="cuda") % 50
+    rows = (first[:, None] + torch.arange(k, device="cuda")).to(torch.int32).view(batch, 1, k).contiguous()
+    index = torch.where(rows % 11 == 3, -1, rows).contiguous()
+    lens = torch.randint(0, slots + 1, (batch, 1), generator=g, device="cuda")
+    lens[0], lens[1], lens[batch - 1] = 0, 1, slots
+    q = normal(g, batch, 1, heads, 576)
+    q[..., :32] = 1.0 + torch.arange(heads, device="cuda")[:, None] / heads
+    out, lse = cache.attend(q, rows=rows, index=index, lens=lens, scale=1.5)
+    assert torch.isfinite(out).all() and (out[0] == 0).all() and (lse[0] == -math.inf).all()
+    some = torch.tensor([0, 1, 2, batch // 2, batch - 1], device="cuda")
+    few, pick = L.LatentCache(pool[some].contiguous(), len(some), int(mx4)), lambda x: x[some].contiguous()
+    check_attend(few, pick(q), pick(out), pick(lse), pick(rows), pick(index), pick(lens), scale=1.5)
+
+
 def test_attend_scale_extremes():
     """Scales of zero and below zero."""
     from paper_2609_37538_amd import latent as L
