@@ -707,17 +707,11 @@ __global__ __launch_bounds__(256) void combine_few_kernel(AttendParams p) {
 
 int head_blocks_of(int heads, AttendKernel kernel) { return (heads + heads_of(kernel) - 1) / heads_of(kernel); }
 
-template <typename Kernel>
-hipError_t allow_lds(Kernel kernel, size_t lds) {
-  return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lds));
-}
-
 template <bool kMx4, int kWaves>
 hipError_t launch_narrow(const AttendParams& p, int64_t groups, int head_blocks, int tiles_per_split, hipStream_t s) {
   constexpr size_t lds = kWaves * 16 * kValueStride + kWaves / 2 * 1024 + (kWaves + 1) * 16 * 4 + 16;
   static_assert(8 / kWaves * lds <= 160 * 1024, "LDS of a CU's workgroups");
-  static const hipError_t ready = allow_lds(&attend_kernel<kMx4, kWaves>, lds);
-  if (ready != hipSuccess) return ready;
+  if (const hipError_t e = allow_lds<&attend_kernel<kMx4, kWaves>>(lds); e != hipSuccess) return e;
   attend_kernel<kMx4, kWaves><<<dim3(static_cast<unsigned>(groups)), kWaves * 64, lds, s>>>(p, head_blocks, tiles_per_split);
   return hipGetLastError();
 }
@@ -727,8 +721,7 @@ hipError_t launch_wide(const AttendParams& p, int64_t groups, int head_blocks, i
   constexpr size_t lds = 3 * kWideRows * kValueStride + 2 * (kWideHeads / 16) * 1024 + 2 * 2 * 4 * 3 * 1024 + 4 * kWideRows * 8 +
                          3 * kWideHeads * 4 + 8;
   static_assert(lds <= 160 * 1024, "LDS of a workgroup");
-  static const hipError_t ready = allow_lds(&attend_wide_kernel<kMx4>, lds);
-  if (ready != hipSuccess) return ready;
+  if (const hipError_t e = allow_lds<&attend_wide_kernel<kMx4>>(lds); e != hipSuccess) return e;
   attend_wide_kernel<kMx4><<<dim3(static_cast<unsigned>(groups)), 512, lds, s>>>(p, head_blocks, tiles_per_split);
   return hipGetLastError();
 }

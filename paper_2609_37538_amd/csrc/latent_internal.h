@@ -2,6 +2,7 @@
 // (include/avsg_latent.h): cache addressing, the 4-bit format, launchers.
 #pragma once
 
+#include <atomic>
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -170,9 +171,23 @@ struct Mx4Product {
   int64_t out_stride, out_batch_stride;
 };
 
+// Lets a kernel have `bytes` of dynamic LDS, once on each GPU that is current in a call.
+template <auto kKernel>
+hipError_t allow_lds(size_t bytes) {
+  static std::atomic<uint64_t> done{0};
+  int gpu = 0;
+  if (const hipError_t e = hipGetDevice(&gpu); e != hipSuccess) return e;
+  const uint64_t bit = gpu < 64 ? uint64_t{1} << gpu : 0;
+  if (done.load(std::memory_order_relaxed) & bit) return hipSuccess;
+  const hipError_t e =
+      hipFuncSetAttribute(reinterpret_cast<const void*>(kKernel), hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
+  if (e == hipSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+  return e;
+}
+
 hipError_t launch_kv_append(const AppendParams& p, int format, int rope_style, hipStream_t s);
 hipError_t launch_kv_read(const ReadParams& p, int format, hipStream_t s);
-// entries of a query token each workgroup takes, and how many share one
+// the kernel of a call of attention, and how many workgroups share a token
 AttendPlan attend_plan(int format, int batch, int n_q, int heads, int topk);
 hipError_t launch_attend(const AttendParams& p, int format, hipStream_t s);
 hipError_t launch_mx4_quantize(const void* x, bool f32, int64_t rows, int64_t cols, int64_t x_stride, uint8_t* codes,

@@ -400,10 +400,8 @@ template <int kTile, int kWavesM, int kWavesN, int kGroups, bool kF32>
 hipError_t launch_staged(const Mx4Product& p, int64_t tiles_m, int64_t tiles_n, hipStream_t s) {
   constexpr int kLds = kGroups * 2 * 2 * kTile * 136;
   static_assert(kLds <= 160 * 1024, "LDS of a workgroup");
-  const auto kernel = &staged_kernel<kTile, kTile, kWavesM, kWavesN, kGroups, kF32>;
-  static const hipError_t ready =
-      hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
-  if (ready != hipSuccess) return ready;
+  constexpr auto kernel = &staged_kernel<kTile, kTile, kWavesM, kWavesN, kGroups, kF32>;
+  if (const hipError_t e = allow_lds<kernel>(kLds); e != hipSuccess) return e;
   kernel<<<dim3(static_cast<unsigned>(tiles_m * tiles_n), p.batch), kGroups * kWavesM * kWavesN * 64, kLds, s>>>(
       p, static_cast<int>(tiles_m), static_cast<int>(tiles_n));
   return hipGetLastError();
