@@ -141,15 +141,16 @@ def avsg_latent_last_error() -> str:
 # ---------------------------------------------------------------------------
 _t = None            # torch, once a wrapper is used
 _stream_of = None    # current stream of a GPU's index
+_current = None      # index of the current GPU (of a process that has tensors on one)
 
 
 def _torch():
     """torch, with the signatures of the library set."""
-    global _t, _stream_of
+    global _t, _stream_of, _current
     if _t is None:
         import torch
         load()
-        _stream_of = torch._C._cuda_getCurrentRawStream
+        _stream_of, _current = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
         _t = torch
     return _t
 
@@ -161,7 +162,7 @@ def _need(ok: bool, what: str) -> None:
 
 def _run(f, where: str, index: int, *args) -> None:
     """Calls f on the current stream of GPU `index`, with that GPU current."""
-    if _t.cuda.current_device() == index:
+    if _current() == index:
         rc = f(*args, _stream_of(index))
     else:
         with _t.cuda.device(index):
@@ -314,10 +315,14 @@ class LatentCache:
         lens_at = None if lens is None else _ints(lens, _t.int64, (b, n_q), dev, "lens")
         if out is None:
             out = _t.empty((b, n_q, heads, AVSG_LATENT_DIM), dtype=_t.bfloat16, device=dev)
-        oa, ot, oh = _tokens(out, (b, n_q, heads, AVSG_LATENT_DIM), dev, "out")
+            oa, ot, oh = out.data_ptr(), heads * AVSG_LATENT_DIM, AVSG_LATENT_DIM
+        else:
+            oa, ot, oh = _tokens(out, (b, n_q, heads, AVSG_LATENT_DIM), dev, "out")
         if lse is None:
             lse = _t.empty((b, n_q, heads), dtype=_t.float32, device=dev)
-        lse_at = _ints(lse, _t.float32, (b, n_q, heads), dev, "lse")
+            lse_at = lse.data_ptr()
+        else:
+            lse_at = _ints(lse, _t.float32, (b, n_q, heads), dev, "lse")
         need = self._workspace.get((n_q, heads, k))
         if need is None:
             need = self._workspace[n_q, heads, k] = avsg_attend_workspace_bytes(b, n_q, heads, k)
