@@ -126,13 +126,16 @@ __device__ __forceinline__ unsigned values_from(int lane, int col) {
   return row * kValueStride + (col * 2 & ~255) + value_part(row, col / 8 % 16 + (lane & 3) / 2) + (lane & 1) * 8;
 }
 
+// Eight columns of a head's query (of head 0 in place of one that does not exist).
+__device__ __forceinline__ u32x4 load_query(const AttendParams& p, const Share& w, int head, int col) {
+  return *reinterpret_cast<const u32x4*>(p.q + w.token * p.q_token_stride + (head < p.heads ? head : 0) * p.q_head_stride + col);
+}
 // Queries take the scale's sign (or its zero), so that with a positive scale
-// products compare like scores.
-__device__ __forceinline__ bf16x8 load_query(const AttendParams& p, const Share& w, int head, int col) {
-  const bool there = head < p.heads;
-  bf16x8 x = *reinterpret_cast<const bf16x8*>(p.q + w.token * p.q_token_stride + (there ? head : 0) * p.q_head_stride + col);
-  if (!there || p.scale == 0.f) x = bf16x8{};
-  return p.scale < 0.f ? -x : x;
+// products compare like scores.  In bits, without a branch: behind one, every load of a
+// kernel's eighteen would be waited for by itself.
+__device__ __forceinline__ bf16x8 signed_query(const AttendParams& p, int head, u32x4 x) {
+  const uint32_t keep = head < p.heads && p.scale != 0.f ? ~0u : 0u, sign = p.scale < 0.f ? 0x80008000u : 0u;
+  return __builtin_bit_cast(bf16x8, (x & keep) ^ sign);
 }
 
 // Result of one head: four columns of every column tile of a wave, whose sum
@@ -196,10 +199,10 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_kernel(AttendParams p, 
   finder.look(p, w, wave * 16 + l16, kRows);
   if (threadIdx.x < 16) reference[threadIdx.x] = -INFINITY;
   if (threadIdx.x < 4) raised[threadIdx.x] = 0;
-  bf16x8 query[18];
+  u32x4 raw[18];
 #pragma unroll
   for (int j = 0; j < 18; ++j)
-    query[j] = load_query(p, w, head, kMx4 && j < 16 ? (j / 4 * 4 + quad) * 32 + j % 4 * 8 : 32 * j + 8 * quad);
+    raw[j] = load_query(p, w, head, kMx4 && j < 16 ? (j / 4 * 4 + quad) * 32 + j % 4 * 8 : 32 * j + 8 * quad);
 
   u32x4 key[kLoads], scales{}, turned[2];
   unsigned counts = 0;   // bits of this lane's four rows (quad * 4 + i) that count
@@ -217,6 +220,10 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_kernel(AttendParams p, 
     for (int j = 0; j < 2; ++j) turned[j] = load_global<u32x4>(at + (kMx4 ? kMx4RopeAt : kLatent * 2) + 64 * j);
   };
   load_keys(0);
+  __builtin_amdgcn_sched_barrier(0);   // the first keys are on their way before the queries are waited for
+  bf16x8 query[18];
+#pragma unroll
+  for (int j = 0; j < 18; ++j) query[j] = signed_query(p, head, raw[j]);
 
   const float scale = p.scale == 0.f ? 1.f : fabsf(p.scale) * kLog2e;   // scores in powers of two
   const float per_scale = 1.f / scale;
@@ -371,6 +378,17 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams p, int
   const Share w = share_of(p, head_blocks, tiles_per_split, kWideRows);
   const int head0 = w.head_block * kWideHeads;
 
+  // The head tile whose weights the wave makes comes first.  Of the two steps of
+  // rotated columns it takes step kg % 2 for that one and the next.
+  auto head_of = [&](int h) { return head0 + (h + kg) % kTiles * 16 + l16; };
+  u32x4 raw[kTiles][4], raw_turned[2];
+#pragma unroll
+  for (int h = 0; h < kTiles; ++h)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) raw[h][j] = load_query(p, w, head_of(h), kg * 128 + (kMx4 ? 32 * quad + 8 * j : 32 * j + 8 * quad));
+#pragma unroll
+  for (int h = 0; h < 2; ++h) raw_turned[h] = load_query(p, w, head_of(h), kLatent + kg % 2 * 32 + 8 * quad);
+
   // the first wave finds the rows of two tiles at a time, one per lane; their
   // addresses go to LDS, and all waves fetch their keys a tile ahead
   RowFinder finder{};
@@ -385,18 +403,6 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams p, int
   }
   if (threadIdx.x < kWideHeads) reference[threadIdx.x] = -INFINITY;
   if (threadIdx.x < 2) raised[threadIdx.x] = 0;
-
-  // The head tile whose weights the wave makes comes first.  Of the two steps of
-  // rotated columns it takes step kg % 2 for that one and the next.
-  bf16x8 query[kTiles][4], query_turned[2];
-#pragma unroll
-  for (int h = 0; h < kTiles; ++h)
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      query[h][j] = load_query(p, w, head0 + (h + kg) % kTiles * 16 + l16, kg * 128 + (kMx4 ? 32 * quad + 8 * j : 32 * j + 8 * quad));
-#pragma unroll
-  for (int h = 0; h < 2; ++h)
-    query_turned[h] = load_query(p, w, head0 + (h + kg) % kTiles * 16 + l16, kLatent + kg % 2 * 32 + 8 * quad);
 
   u32x4 key[kLoads], turned;
   uint32_t scales = 0;
@@ -418,6 +424,14 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams p, int
 #pragma unroll
     for (int n = 0; n < kLoads + 2; ++n) load_part(at, n);
   }
+  __builtin_amdgcn_sched_barrier(0);   // the first keys are on their way before the queries are waited for
+  bf16x8 query[kTiles][4], query_turned[2];
+#pragma unroll
+  for (int h = 0; h < kTiles; ++h)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) query[h][j] = signed_query(p, head_of(h), raw[h][j]);
+#pragma unroll
+  for (int h = 0; h < 2; ++h) query_turned[h] = signed_query(p, head_of(h), raw_turned[h]);
 
   const float scale = p.scale == 0.f ? 1.f : fabsf(p.scale) * kLog2e;   // scores in powers of two
   const float per_scale = 1.f / scale;
