@@ -173,9 +173,9 @@ __device__ __forceinline__ void store_head(const AttendParams& p, const Share& w
 // all 576 columns, leave weights and expanded values in LDS, and take 128 of the 512
 // columns each of the output.  So few heads make the rows' bytes count, and two
 // workgroups per CU keep 50 KB of them in flight: 4 x 131072 rows of 400 bytes for 16 heads
-// take 52 us, 4.0 TB/s, where a large copy moves 5.0.  A call of one token takes 8 us,
+// take 51 us, 4.1 TB/s, where a large copy moves 5.0.  A call of one token takes 7 us,
 // launch, three dependent loads (entry, row, next tile's) and one tile.  Or eight waves
-// and tiles of 128 rows: 2.4 to 2.6 us each where a lone workgroup of four takes 1.7 for 64,
+// and tiles of 128 rows: 2.3 us each where a lone workgroup of four takes 1.7 for 64,
 // and half the parts of two workgroups.
 template <bool kMx4, int kWaves>
 __global__ __launch_bounds__(kWaves * 64, 2) void attend_kernel(AttendParams p, int head_blocks, int tiles_per_split) {
@@ -351,7 +351,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_kernel(AttendParams p, 
 // exponentials) and then waits for the others' waves: one after the other, with
 // a barrier each, they took 7100 cycles per 64 rows, of which the matrix cores worked
 // 2200, also with two such workgroups of 32 heads on a CU.  In one stream they overlap:
-// 2300 cycles per 32 rows, the matrix cores 1100, and 97 us for 128 tokens of 128 heads
+// 2300 cycles per 32 rows, the matrix cores 1100, and 96 us for 128 tokens of 128 heads
 // over 2048 rows each (73 GFLOP).  What is left is spread: without the loads it took
 // 19% less, without the writes of values 20%, without the exchange of scores 15%,
 // without the output's products 19%.
