@@ -351,7 +351,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_kernel(AttendParams p, 
 // exponentials) and then waits for the others' waves: one after the other, with
 // a barrier each, they took 7100 cycles per 64 rows, of which the matrix cores worked
 // 2200, also with two such workgroups of 32 heads on a CU.  In one stream they overlap:
-// 2300 cycles per 32 rows, the matrix cores 1100, and 96 us for 128 tokens of 128 heads
+// 2200 cycles per 32 rows, the matrix cores 1100, and 92 us for 128 tokens of 128 heads
 // over 2048 rows each (73 GFLOP).  What is left is spread: without the loads it took
 // 19% less, without the writes of values 20%, without the exchange of scores 15%,
 // without the output's products 19%.
@@ -530,10 +530,15 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams p, int
         for (int h = 0; h < kTiles; ++h) part[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, query[h][j], part[h], 0, 0, 0);
         k = following;
       }
+      counted = counts;
+      // the next keys' loads start where registers are free, two here and the rest one by
+      // one between the products below (all of them below: 5% longer)
+      take_keys(next_at);
+      load_part(next_at, 0);
+      load_part(next_at, kMx4 ? 2 : 1);
 #pragma unroll
       for (int h = 0; h < 2; ++h)
         part[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, turned), query_turned[h], part[h], 0, 0, 0);
-      counted = counts;
     }
     if constexpr (kOutput) {
       if (high == t + 1) {
@@ -549,7 +554,6 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams p, int
 #pragma unroll
       for (int n = 0; n < 3; ++n) theirs[n] = *reinterpret_cast<const f32x4*>(from + n * 1024);
     }
-    if constexpr (kScores) take_keys(next_at);
     unsigned char* const parts_to = reinterpret_cast<unsigned char*>(parts) + (((t + 2) & 1) * 8 + rg * 4) * 3 * 1024 + lane16;
 #pragma unroll
     for (int c = 0; c < kColTiles; ++c) {
@@ -559,8 +563,8 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams p, int
         for (int h = 0; h < kTiles; ++h) out[c][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[c], e[h], out[c][h], 0, 0, 0);
       }
       if constexpr (kScores) {
-        // the next keys' loads and the scores' way to the others, one by one between products
-        for (int n = c * (kLoads + 2) / 4; n < (c + 1) * (kLoads + 2) / 4; ++n) load_part(next_at, n);
+        // the rest of the loads and the scores' way to the others, one by one between products
+        if (kMx4 ? c == 0 : c < 3) load_part(next_at, kMx4 ? 1 : c + 2);
         if (c > 0) *reinterpret_cast<f32x4*>(parts_to + (kg + c) % 4 * 3 * 1024 + (c - 1) * 1024) = part[c];
       }
     }
