@@ -135,8 +135,9 @@ size_t avsg_attend_workspace_bytes(int32_t batch, int32_t n_q, int32_t heads, in
  * query token that count: their position lies in [0, len) and their row exists.
  * Rows of entries that do not count are not read.  A token without any gets
  * zeros, and minus infinity in d_lse.  Products take bfloat16 operands (4-bit
- * rows are expanded exactly; probabilities are rounded once to bfloat16) and
- * add up in float32, as do maxima and sums. */
+ * rows are expanded exactly; a probability is a sum of two operands and keeps 12
+ * bits at least, or is off by 2^-19 of its token's largest) and add up in float32,
+ * as do maxima and sums. */
 avsg_status avsg_attend(const avsg_cache *cache, const avsg_attention *a, void *d_workspace,
                         size_t workspace_bytes, void *stream);
 

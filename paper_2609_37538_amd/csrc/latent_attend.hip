@@ -24,10 +24,16 @@ __device__ __forceinline__ unsigned value_part(unsigned row, unsigned part) {
   return ((part ^ ((row & 7) * 2 + ((row >> 3) & 1))) & 15) * 16;
 }
 // Weights are kept relative to a reference that need not be the maximum: it is
-// raised only when a score passes it by this much (in powers of two), which in
-// float32 and bfloat16 costs no accuracy and saves the exchange of maxima
-// between waves for nearly every tile.
-constexpr float kSlack = 40.f;
+// raised only when a score passes it by this much (in powers of two), which
+// saves the exchange of maxima between waves for nearly every tile.
+constexpr float kSlack = 8.f;
+// A weight takes part in the output product as a sum of two bfloat16, its eight highest bits and the
+// rest: one alone would be off by up to 2^-8, as much as the result's own rounding.  Where LDS has no
+// room for both, the rest is kept in 8 bits (e4m3: 4 significant ones, so the weight has 12), in units that fit
+// the largest weight, 2^kSlack, whose rest is at most 2^(kSlack - 9): 256 units.  Below 2^-6 of the reference's
+// weight the rest has fewer bits, and is off by at most 2^-19 of that weight.
+constexpr float kRestUnit = 0x1p-9f;
+static_assert(kSlack == 8.f, "kRestUnit is 2^(kSlack - 17)");
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 // The order in which the compiler is to issue what stands before in a block:
@@ -42,6 +48,28 @@ __device__ __forceinline__ float zero_if_none(float reference) { return referenc
 
 __device__ __forceinline__ bf16x4 rounded(f32x4 x) {
   return bf16x4{static_cast<__bf16>(x[0]), static_cast<__bf16>(x[1]), static_cast<__bf16>(x[2]), static_cast<__bf16>(x[3])};
+}
+
+// What `rounded` leaves of x.
+__device__ __forceinline__ f32x4 rest_of(f32x4 x, bf16x4 high) {
+  return f32x4{x[0] - static_cast<float>(high[0]), x[1] - static_cast<float>(high[1]), x[2] - static_cast<float>(high[2]),
+               x[3] - static_cast<float>(high[3])};
+}
+
+typedef short s16x2 __attribute__((ext_vector_type(2)));
+// Four rests in 8 bits each, and eight of them in bfloat16.
+__device__ __forceinline__ uint32_t rest_encode(f32x4 x) {
+  s16x2 c{};
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(c, x[0], x[1], kRestUnit, false);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(c, x[2], x[3], kRestUnit, true);
+  return __builtin_bit_cast(uint32_t, c);
+}
+__device__ __forceinline__ bf16x8 rest_decode(u32x2 c) {
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[0], kRestUnit, false);
+  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[0], kRestUnit, true);
+  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[1], kRestUnit, false);
+  const bf16x2 e = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[1], kRestUnit, true);
+  return bf16x8{a[0], a[1], b[0], b[1], d[0], d[1], e[0], e[1]};
 }
 
 // A lane's number that the compiler takes for a new value: what is derived from
@@ -184,8 +212,8 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_kernel(AttendParams p, 
   constexpr int kLoads = kMx4 ? 4 : 16;
   extern __shared__ __align__(16) unsigned char lds[];
   unsigned char* const values = lds;
-  unsigned char* const weights = lds + kRows * kValueStride;                              // [kPairs][64 lanes] 16 bytes
-  float* const wave_top = reinterpret_cast<float*>(weights + kPairs * 1024);     // [kWaves][16]
+  unsigned char* const weights = lds + kRows * kValueStride;                     // [high, rest][kPairs][64 lanes] 16 bytes
+  float* const wave_top = reinterpret_cast<float*>(weights + 2 * kPairs * 1024); // [kWaves][16]
   float* const reference = wave_top + kWaves * 16;                               // [16]
   int* const raised = reinterpret_cast<int*>(reference + 16);                    // [2]
 
@@ -265,9 +293,10 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_kernel(AttendParams p, 
 #pragma unroll
       for (int i = 0; i < 4; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], scale, -base));
       add = (e[0] + e[1]) + (e[2] + e[3]);
-      // rounded once; the sum keeps float32 weights, so the rounding errors
-      // of many rows cancel in the output and do not touch the sum
-      *reinterpret_cast<bf16x4*>(weights + (wave >> 1) * 1024 + lane * 16 + (wave & 1) * 8) = rounded(e);
+      bf16x4* const to = reinterpret_cast<bf16x4*>(weights + (wave >> 1) * 1024 + lane * 16 + (wave & 1) * 8);
+      const bf16x4 high = rounded(e);
+      to[0] = high;
+      to[kPairs * 128] = rounded(rest_of(e, high));
     };
     const float top = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
     weigh();
@@ -299,9 +328,9 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_kernel(AttendParams p, 
 
     const unsigned from = values_from(lane_here(), wave * kCols);
     const unsigned char* const weight_from = weights + lane_here() * 16;
-    bf16x8 e[kPairs];
+    bf16x8 e[2][kPairs];
 #pragma unroll
-    for (int i = 0; i < kPairs; ++i) e[i] = *reinterpret_cast<const bf16x8*>(weight_from + i * 1024);
+    for (int i = 0; i < 2 * kPairs; ++i) e[i / kPairs][i % kPairs] = *reinterpret_cast<const bf16x8*>(weight_from + i * 1024);
     // operands are read four products ahead: left to itself the compiler waits for each
     auto load_step = [&](int n) {   // column tile n % kColTiles of rows n / kColTiles * 32 .. + 31
       return load_values(values, (from ^ (n % kColTiles * 32)) + n / kColTiles * 32 * kValueStride);
@@ -314,12 +343,14 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_kernel(AttendParams p, 
     for (int n = 0; n < kPairs * kColTiles; ++n) {
       const bf16x8 x = v[n % kAhead];
       if (n + kAhead < kPairs * kColTiles) v[n % kAhead] = load_step(n + kAhead);
-      out[n % kColTiles] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, e[n / kColTiles], out[n % kColTiles], 0, 0, 0);
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        out[n % kColTiles] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, e[i][n / kColTiles], out[n % kColTiles], 0, 0, 0);
     }
-    kSchedule(kLdsRead, kPairs + 2 * kAhead);
+    kSchedule(kLdsRead, 2 * kPairs + 2 * kAhead);
 #pragma unroll
     for (int n = 0; n < kPairs * kColTiles; ++n) {
-      kSchedule(kMatrix, 1);
+      kSchedule(kMatrix, 2);
       kSchedule(kLdsRead, 2);
     }
   }
@@ -366,7 +397,8 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams p, int
   extern __shared__ __align__(16) unsigned char lds[];
   unsigned char* const values = lds;                                                        // [3] tiles
   unsigned char* const weights = lds + 3 * kBufferBytes;                                    // [2][head tiles][64 lanes] 16 bytes
-  f32x4* const parts = reinterpret_cast<f32x4*>(weights + 2 * kTiles * 1024);               // [2][2][4][3][64]
+  unsigned char* const rests = weights + 2 * kTiles * 1024;                                 // [2][head tiles][64 lanes] 8 bytes
+  f32x4* const parts = reinterpret_cast<f32x4*>(rests + 2 * kTiles * 512);                  // [2][2][4][3][64]
   uint64_t* const row_at = reinterpret_cast<uint64_t*>(parts + 2 * 2 * 4 * 3 * 64);         // [4] tiles: rows, 0 = none
   float* const group_top = reinterpret_cast<float*>(row_at + 4 * kWideRows);                // [2][heads]
   float* const reference = group_top + 2 * kWideHeads;                                      // [heads]
@@ -451,9 +483,10 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams p, int
 #pragma unroll
     for (int j = 0; j < 4; ++j) e[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[j], scale, -base));
     add = (e[0] + e[1]) + (e[2] + e[3]);
-    // rounded once; the sum keeps float32 weights, so the rounding errors
-    // of many rows cancel in the output and do not touch the sum
-    *reinterpret_cast<bf16x4*>(weights + (t & 1) * kTiles * 1024 + kg * 1024 + lane_here() * 16 + rg * 8) = rounded(e);
+    const bf16x4 high = rounded(e);
+    const unsigned to = (t & 1) * kTiles * 64 + kg * 64 + lane_here();
+    *reinterpret_cast<bf16x4*>(weights + to * 16 + rg * 8) = high;
+    *reinterpret_cast<uint32_t*>(rests + to * 8 + rg * 4) = rest_encode(rest_of(e, high));
   };
   // some score of tile t lies far above the reference: all waves agree on new
   // ones and bring what they hold to them
@@ -566,6 +599,16 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams p, int
         // the rest of the loads and the scores' way to the others, one by one between products
         if (kMx4 ? c == 0 : c < 3) load_part(next_at, kMx4 ? 1 : c + 2);
         if (c > 0) *reinterpret_cast<f32x4*>(parts_to + (kg + c) % 4 * 3 * 1024 + (c - 1) * 1024) = part[c];
+      }
+    }
+    if constexpr (kOutput) {
+      // the weights' rests, whose products run beside what follows
+      const unsigned char* const rest_from = rests + (t & 1) * kTiles * 512 + lane16 / 2;
+#pragma unroll
+      for (int h = 0; h < kTiles; ++h) {
+        const bf16x8 rest = rest_decode(*reinterpret_cast<const u32x2*>(rest_from + h * 512));
+#pragma unroll
+        for (int c = 0; c < kColTiles; ++c) out[c][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[c], rest, out[c][h], 0, 0, 0);
       }
     }
     if constexpr (kWeights) {
@@ -727,7 +770,7 @@ int head_blocks_of(int heads, AttendKernel kernel) { return (heads + heads_of(ke
 
 template <bool kMx4, int kWaves>
 hipError_t launch_narrow(const AttendParams& p, int64_t groups, int head_blocks, int tiles_per_split, hipStream_t s) {
-  constexpr size_t lds = kWaves * 16 * kValueStride + kWaves / 2 * 1024 + (kWaves + 1) * 16 * 4 + 16;
+  constexpr size_t lds = kWaves * 16 * kValueStride + kWaves * 1024 + (kWaves + 1) * 16 * 4 + 16;
   static_assert(8 / kWaves * lds <= 160 * 1024, "LDS of a CU's workgroups");
   if (const hipError_t e = allow_lds<&attend_kernel<kMx4, kWaves>>(lds); e != hipSuccess) return e;
   attend_kernel<kMx4, kWaves><<<dim3(static_cast<unsigned>(groups)), kWaves * 64, lds, s>>>(p, head_blocks, tiles_per_split);
@@ -736,7 +779,7 @@ hipError_t launch_narrow(const AttendParams& p, int64_t groups, int head_blocks,
 
 template <bool kMx4>
 hipError_t launch_wide(const AttendParams& p, int64_t groups, int head_blocks, int tiles_per_split, hipStream_t s) {
-  constexpr size_t lds = 3 * kWideRows * kValueStride + 2 * (kWideHeads / 16) * 1024 + 2 * 2 * 4 * 3 * 1024 + 4 * kWideRows * 8 +
+  constexpr size_t lds = 3 * kWideRows * kValueStride + 2 * (kWideHeads / 16) * (1024 + 512) + 2 * 2 * 4 * 3 * 1024 + 4 * kWideRows * 8 +
                          3 * kWideHeads * 4 + 8;
   static_assert(lds <= 160 * 1024, "LDS of a workgroup");
   if (const hipError_t e = allow_lds<&attend_wide_kernel<kMx4>>(lds); e != hipSuccess) return e;
