@@ -137,7 +137,8 @@ size_t avsg_attend_workspace_bytes(int32_t batch, int32_t n_q, int32_t heads, in
  * zeros, and minus infinity in d_lse.  Products take bfloat16 operands (4-bit
  * rows are expanded exactly; a probability is a sum of two operands and keeps 12
  * bits at least, or is off by 2^-19 of its token's largest) and add up in float32,
- * as do maxima and sums. */
+ * as do maxima and sums.  No sum exceeds the rows' largest value, so what is finite
+ * in the rows is finite in the result. */
 avsg_status avsg_attend(const avsg_cache *cache, const avsg_attention *a, void *d_workspace,
                         size_t workspace_bytes, void *stream);
 

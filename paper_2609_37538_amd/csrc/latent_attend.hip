@@ -23,17 +23,19 @@ constexpr int kValueStride = kLatent * 2;
 __device__ __forceinline__ unsigned value_part(unsigned row, unsigned part) {
   return ((part ^ ((row & 7) * 2 + ((row >> 3) & 1))) & 15) * 16;
 }
-// Weights are kept relative to a reference that need not be the maximum: it is
-// raised only when a score passes it by this much (in powers of two), which
-// saves the exchange of maxima between waves for nearly every tile.
+// Weights are kept relative to a reference, the largest score so far raised by `above` powers of two.  It need
+// not follow the maximum: only a score that passes the one it was made of by kSlack raises it, which saves the
+// exchange of maxima between waves for nearly every tile.  `above` is kSlack and the logarithm of the number of
+// entries, so that however many weights there are, they add up to 1 at most and their products with values to
+// the largest value at most: what is finite in the rows stays finite in every sum.  A token's largest weight is
+// never less than 2^-above, 2^-39 at most, and weights down to 2^-87 of that do not vanish.
 constexpr float kSlack = 8.f;
 // A weight takes part in the output product as a sum of two bfloat16, its eight highest bits and the
 // rest: one alone would be off by up to 2^-8, as much as the result's own rounding.  Where LDS has no
-// room for both, the rest is kept in 8 bits (e4m3: 4 significant ones, so the weight has 12), in units that fit
-// the largest weight, 2^kSlack, whose rest is at most 2^(kSlack - 9): 256 units.  Below 2^-6 of the reference's
-// weight the rest has fewer bits, and is off by at most 2^-19 of that weight.
-constexpr float kRestUnit = 0x1p-9f;
-static_assert(kSlack == 8.f, "kRestUnit is 2^(kSlack - 17)");
+// room for both, the rest is kept in 8 bits (e4m3: 4 significant ones, so that the weight has 12), in units that
+// fit the largest weight, 2^(kSlack - above), whose rest is at most 2^-9 of it: 256 units.  Below 2^-6 of the weight
+// that the reference's own score has, the rest has fewer bits, and is off by at most 2^-19 of that weight.
+constexpr float kRestUnit = 0x1p-17f;   // of the largest weight
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 // The order in which the compiler is to issue what stands before in a block:
@@ -58,17 +60,17 @@ __device__ __forceinline__ f32x4 rest_of(f32x4 x, bf16x4 high) {
 
 typedef short s16x2 __attribute__((ext_vector_type(2)));
 // Four rests in 8 bits each, and eight of them in bfloat16.
-__device__ __forceinline__ uint32_t rest_encode(f32x4 x) {
+__device__ __forceinline__ uint32_t rest_encode(f32x4 x, float unit) {
   s16x2 c{};
-  c = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(c, x[0], x[1], kRestUnit, false);
-  c = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(c, x[2], x[3], kRestUnit, true);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(c, x[0], x[1], unit, false);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(c, x[2], x[3], unit, true);
   return __builtin_bit_cast(uint32_t, c);
 }
-__device__ __forceinline__ bf16x8 rest_decode(u32x2 c) {
-  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[0], kRestUnit, false);
-  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[0], kRestUnit, true);
-  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[1], kRestUnit, false);
-  const bf16x2 e = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[1], kRestUnit, true);
+__device__ __forceinline__ bf16x8 rest_decode(u32x2 c, float unit) {
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[0], unit, false);
+  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[0], unit, true);
+  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[1], unit, false);
+  const bf16x2 e = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[1], unit, true);
   return bf16x8{a[0], a[1], b[0], b[1], d[0], d[1], e[0], e[1]};
 }
 
@@ -166,6 +168,11 @@ __device__ __forceinline__ bf16x8 signed_query(const AttendParams& p, int head, 
   return __builtin_bit_cast(bf16x8, (x & keep) ^ sign);
 }
 
+// The logarithm of the sum of exp(score) where weights relative to `reference` add up to `all`, 0 if there are none.
+__device__ __forceinline__ float log_sum(const AttendParams& p, float reference, float all) {
+  return all == 0.f ? -INFINITY : (zero_if_none(reference) - p.above + __builtin_amdgcn_logf(all * __builtin_amdgcn_exp2f(p.above))) * kLn2;
+}
+
 // Result of one head: four columns of every column tile of a wave, whose sum
 // of weights is `all` relative to `reference`.
 template <int kColTiles, typename Out>
@@ -183,7 +190,7 @@ __device__ __forceinline__ void store_head(const AttendParams& p, const Share& w
 #pragma unroll
   for (int c = 0; c < kColTiles; ++c) *reinterpret_cast<bf16x4*>(to + c * 16) = rounded(out(c) * by);
   if (p.lse && first)
-    p.lse[w.token * p.heads + head] = all == 0.f ? -INFINITY : (zero_if_none(reference) + __builtin_amdgcn_logf(all)) * kLn2;
+    p.lse[w.token * p.heads + head] = log_sum(p, reference, all);
 }
 
 // Operands of the products, in both kernels below:
@@ -285,7 +292,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_kernel(AttendParams p, 
 #pragma unroll
     for (int i = 0; i < 4; ++i)
       if (!((now >> i) & 1)) s[i] = -INFINITY;
-    // weights relative to the reference as it is; a score far above it is noted
+    // weights relative to the reference as it is; a score that raises it is noted
     float add;
     auto weigh = [&]() {
       const float base = zero_if_none(ref);
@@ -300,12 +307,12 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_kernel(AttendParams p, 
     };
     const float top = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
     weigh();
-    if (__any(top > (ref + kSlack) * per_scale) && lane == 0) raised[t & 1] = t + 1;
+    if (__any(top > (ref - p.above + kSlack) * per_scale) && lane == 0) raised[t & 1] = t + 1;
     __syncthreads();
     if (raised[t & 1] == t + 1) {
-      // some score lies far above the reference: all waves agree on new ones and
+      // some score raises its reference: all waves agree on new ones and
       // bring what they hold to them
-      float high = top * scale;
+      float high = top * scale + p.above;
       high = fmaxf(high, __shfl_xor(high, 16));
       high = fmaxf(high, __shfl_xor(high, 32));
       if (quad == 0) wave_top[wave * 16 + l16] = high;
@@ -486,13 +493,13 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams p, int
     const bf16x4 high = rounded(e);
     const unsigned to = (t & 1) * kTiles * 64 + kg * 64 + lane_here();
     *reinterpret_cast<bf16x4*>(weights + to * 16 + rg * 8) = high;
-    *reinterpret_cast<uint32_t*>(rests + to * 8 + rg * 4) = rest_encode(rest_of(e, high));
+    *reinterpret_cast<uint32_t*>(rests + to * 8 + rg * 4) = rest_encode(rest_of(e, high), p.rest_unit);
   };
-  // some score of tile t lies far above the reference: all waves agree on new
+  // some score of tile t raises its reference: all waves agree on new
   // ones and bring what they hold to them
   auto raise = [&](int t) {
     const int x = lane_here(), x16 = x & 15;
-    float high = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])) * scale;
+    float high = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])) * scale + p.above;
     high = fmaxf(high, __shfl_xor(high, 16));
     high = fmaxf(high, __shfl_xor(high, 32));
     if (x < 16) group_top[rg * kWideHeads + kg * 16 + x16] = high;
@@ -606,7 +613,7 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams p, int
       const unsigned char* const rest_from = rests + (t & 1) * kTiles * 512 + lane16 / 2;
 #pragma unroll
       for (int h = 0; h < kTiles; ++h) {
-        const bf16x8 rest = rest_decode(*reinterpret_cast<const u32x2*>(rest_from + h * 512));
+        const bf16x8 rest = rest_decode(*reinterpret_cast<const u32x2*>(rest_from + h * 512), p.rest_unit);
 #pragma unroll
         for (int c = 0; c < kColTiles; ++c) out[c][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[c], rest, out[c][h], 0, 0, 0);
       }
@@ -622,9 +629,9 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams p, int
     }
     if constexpr (kWeights) {
       weigh(t + 1);
-      // a score far above the reference is noted
+      // a score that raises the reference is noted
       const float top = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
-      if (__any(top > (ref + kSlack) * per_scale)) raised[(t + 1) & 1] = t + 2;
+      if (__any(top > (ref - p.above + kSlack) * per_scale)) raised[(t + 1) & 1] = t + 2;
     }
     if constexpr (kScores) {
       if (wave == 0 && t >= 0 && (t & 1) == 0) {
@@ -727,7 +734,7 @@ __global__ __launch_bounds__(kMostSplits) void combine_kernel(AttendParams p) {
   for (int g = 0; g < kGroups - 1; ++g) o += group_sum[g][tid % kLanes];
   o *= all == 0.f ? 0.f : 1.f / all;
   *reinterpret_cast<bf16x4*>(p.out + token * p.out_token_stride + head * p.out_head_stride + col) = rounded(o);
-  if (p.lse && tid == 0 && col == 0) p.lse[token * p.heads + head] = all == 0.f ? -INFINITY : (base + __builtin_amdgcn_logf(all)) * kLn2;
+  if (p.lse && tid == 0 && col == 0) p.lse[token * p.heads + head] = log_sum(p, top, all);
 }
 
 // The same for up to kMost parts, which is most calls: a thread makes the factors itself, without a barrier, and adds up
@@ -763,7 +770,7 @@ __global__ __launch_bounds__(256) void combine_few_kernel(AttendParams p) {
   }
   o *= all == 0.f ? 0.f : 1.f / all;
   *reinterpret_cast<bf16x4*>(p.out + token * p.out_token_stride + head * p.out_head_stride + col) = rounded(o);
-  if (p.lse && col == 0) p.lse[token * p.heads + head] = all == 0.f ? -INFINITY : (base + __builtin_amdgcn_logf(all)) * kLn2;
+  if (p.lse && col == 0) p.lse[token * p.heads + head] = log_sum(p, top, all);
 }
 
 int head_blocks_of(int heads, AttendKernel kernel) { return (heads + heads_of(kernel) - 1) / heads_of(kernel); }
@@ -861,7 +868,12 @@ AttendPlan attend_plan(int format, int batch, int n_q, int heads, int topk) {
   return best;
 }
 
-hipError_t launch_attend(const AttendParams& p, int format, hipStream_t s) {
+hipError_t launch_attend(const AttendParams& call, int format, hipStream_t s) {
+  AttendParams p = call;
+  int bits = 0;   // of the number of entries
+  while (bits < 31 && (int64_t{1} << bits) < p.topk) ++bits;
+  p.above = kSlack + static_cast<float>(bits);
+  p.rest_unit = std::ldexp(kRestUnit, -bits);
   hipError_t e = format == 1 ? launch_format<true>(p, s) : launch_format<false>(p, s);
   const int splits = p.plan.splits;
   if (e != hipSuccess || splits <= 1) return e;

@@ -152,7 +152,8 @@ struct AttendParams {
   float* lse;
   AttendPlan plan;
   float* part_out;      // [B n_q][splits][heads][512], splits > 1
-  f32x2* part_ml;       // [B n_q][splits][heads]: maximum and sum
+  f32x2* part_ml;       // [B n_q][splits][heads]: reference and sum
+  float above, rest_unit;   // of the weights; the launch sets them
 };
 
 struct Mx4View {
