@@ -86,8 +86,12 @@ __device__ __forceinline__ int lane_here() {
 // run of tiles of its entries.
 struct Share {
   int64_t token, len;
-  int request, head_block, split, tile0, tiles, limit;
+  int request, head_block, split, first, tiles;   // `first` of its entries (where it has any)
+  unsigned count;                                 // that can count
 };
+
+// Tiles of `entries`, which may be as many as 31 bits hold.
+__host__ __device__ constexpr int tiles_of(int entries, int rows) { return entries / rows + (entries % rows != 0); }
 
 __device__ __forceinline__ Share share_of(const AttendParams& p, int head_blocks, int tiles_per_split, int tile_rows) {
   Share w;
@@ -102,9 +106,11 @@ __device__ __forceinline__ Share share_of(const AttendParams& p, int head_blocks
   w.request = static_cast<int>(w.token / p.n_q);
   w.len = p.lens ? p.lens[w.token] : INT64_MAX;
   // entries that can count: with their positions given, any
-  w.limit = p.index ? p.topk : static_cast<int>(w.len < 0 ? 0 : w.len < p.topk ? w.len : p.topk);
-  w.tile0 = w.split * tiles_per_split;
-  w.tiles = min(tiles_per_split, (w.limit + tile_rows - 1) / tile_rows - w.tile0);
+  const int limit = p.index ? p.topk : static_cast<int>(w.len < 0 ? 0 : w.len < p.topk ? w.len : p.topk);
+  const int64_t most = static_cast<int64_t>(tiles_per_split) * tile_rows, first = w.split * most;
+  w.first = static_cast<int>(first);
+  w.count = static_cast<unsigned>(max(int64_t{0}, min(most, limit - first)));
+  w.tiles = static_cast<int>((w.count + tile_rows - 1) / tile_rows);
   return w;
 }
 
@@ -114,10 +120,10 @@ struct RowFinder {
   int row, pos, page;   // of this lane's row of those looked at last
 
   // entry `n` of the share
-  __device__ __forceinline__ void look(const AttendParams& p, const Share& w, int n, int tile_rows) {
+  __device__ __forceinline__ void look(const AttendParams& p, const Share& w, unsigned n) {
     row = pos = page = -1;
-    const int i = w.tile0 * tile_rows + n;
-    if (i >= w.limit || n >= w.tiles * tile_rows) return;
+    if (n >= w.count) return;
+    const int i = w.first + static_cast<int>(n);
     row = p.rows ? p.rows[w.token * p.topk + i] : i;
     pos = p.index ? p.index[w.token * p.topk + i] : i;
     if (!p.rows && p.cache.table && i < p.cache.capacity)
@@ -231,7 +237,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_kernel(AttendParams p, 
 
   // every lane finds the row whose keys it loads, what is read of it two tiles ahead
   RowFinder finder;
-  finder.look(p, w, wave * 16 + l16, kRows);
+  finder.look(p, w, wave * 16 + l16);
   if (threadIdx.x < 16) reference[threadIdx.x] = -INFINITY;
   if (threadIdx.x < 4) raised[threadIdx.x] = 0;
   u32x4 raw[18];
@@ -244,7 +250,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_kernel(AttendParams p, 
   auto load_keys = [&](int t) {
     const unsigned x = lane_here();
     uint64_t at = finder.address(p, w);
-    finder.look(p, w, (t + 1) * kRows + wave * 16 + (x & 15), kRows);
+    finder.look(p, w, (t + 1u) * kRows + wave * 16 + (x & 15));
     counts = static_cast<unsigned>(__ballot(at != 0) >> (x / 16 * 4)) & 15u;
     if (at == 0) at = reinterpret_cast<uint64_t>(zero_row);
     if constexpr (kMx4) scales = load_global<u32x4>(at + kMx4CodeBytes);
@@ -434,10 +440,10 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams p, int
   auto leave = [&](const RowFinder& f, int t) { row_at[(t & 3) * kWideRows + lane_here()] = f.address(p, w); };
   if (wave == 0) {
     RowFinder second;
-    finder.look(p, w, lane, kWideRows);
-    second.look(p, w, 2 * kWideRows + lane, kWideRows);
+    finder.look(p, w, lane);
+    second.look(p, w, 2 * kWideRows + lane);
     leave(finder, 0);
-    finder.look(p, w, 4 * kWideRows + lane, kWideRows);
+    finder.look(p, w, 4 * kWideRows + lane);
     leave(second, 2);
   }
   if (threadIdx.x < kWideHeads) reference[threadIdx.x] = -INFINITY;
@@ -636,7 +642,7 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams p, int
     if constexpr (kScores) {
       if (wave == 0 && t >= 0 && (t & 1) == 0) {
         leave(finder, t + 4);
-        finder.look(p, w, (t + 6) * kWideRows + lane_here(), kWideRows);
+        finder.look(p, w, (t + 6u) * kWideRows + lane_here());
       }
     }
     __syncthreads();
@@ -798,7 +804,7 @@ template <bool kMx4>
 hipError_t launch_format(const AttendParams& p, hipStream_t s) {
   const AttendKernel kernel = p.plan.kernel;
   const int head_blocks = head_blocks_of(p.heads, kernel), rows = kernel == AttendKernel::k64Heads ? kWideRows : rows_of(kernel);
-  const int tiles = (p.topk + rows - 1) / rows, each = (tiles + p.plan.splits - 1) / p.plan.splits;
+  const int tiles = tiles_of(p.topk, rows), each = tiles_of(tiles, p.plan.splits);
   const int64_t groups = static_cast<int64_t>(p.cache.batch) * p.n_q * head_blocks * p.plan.splits;
   if (groups > INT32_MAX) return hipErrorInvalidValue;
   switch (kernel) {
@@ -852,7 +858,7 @@ AttendPlan attend_plan(int format, int batch, int n_q, int heads, int topk) {
   for (AttendKernel kernel : {AttendKernel::k16Heads, AttendKernel::k16HeadsAlone, AttendKernel::k64Heads}) {
     if (kernel == AttendKernel::k64Heads && heads <= 16) break;
     const int64_t groups = tokens * head_blocks_of(heads, kernel);
-    const int tiles = (topk + rows_of(kernel) - 1) / rows_of(kernel);
+    const int tiles = tiles_of(topk, rows_of(kernel));
     int last = 0;
     for (int64_t target : {128, 256, 512}) {
       if (target == 512 && kernel != AttendKernel::k16Heads) break;   // one workgroup per CU

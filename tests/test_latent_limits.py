@@ -1,0 +1,32 @@
+"""The latent-cache operators at the ends of what their arguments can say."""
+import pytest
+import torch
+
+from paper_2609_37538_amd import latent as L
+
+MOST = 2 ** 31 - 1
+
+
+@pytest.mark.parametrize("batch,n_q,heads", [(1, 1, 16), (4, 1, 16), (1, 1, 64), (2, 3, 40), (16, 1, 128)])
+def test_plans_of_the_longest_contexts(batch, n_q, heads):
+    """The last counts of entries that 32 bits hold are shared by as many workgroups as those before them."""
+    want = L.avsg_attend_workspace_bytes(batch, n_q, heads, 2 ** 31 - 4096)
+    assert want > 0
+    for k in [MOST - i for i in (0, 1, 30, 31, 62, 63, 64, 126, 127, 128, 200)]:
+        assert L.avsg_attend_workspace_bytes(batch, n_q, heads, k) == want, k
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("mx4", [False, True])
+@pytest.mark.parametrize("batch,n_q,heads", [(1, 1, 16), (2, 2, 64), (3, 1, 40)])
+@pytest.mark.parametrize("longest", [MOST, MOST - 63])
+def test_attend_without_a_limit(longest, batch, n_q, heads, mx4):
+    """Contexts bounded by their lengths alone, and by the rows that exist."""
+    from test_latent import SCALE, check_attend, gen, normal, pool_of
+    g = gen(batch + heads)
+    cache = L.LatentCache(pool_of(g, batch, 500, mx4), batch, int(mx4))
+    q = normal(g, batch, n_q, heads, 576)
+    lens = torch.randint(1, 501, (batch, n_q), generator=g, device="cuda")
+    lens[0, 0] = 700       # 200 of them are not there
+    out, lse = cache.attend(q, lens=lens, longest=longest, scale=SCALE)
+    check_attend(cache, q, out, lse, lens=lens, longest=700)
