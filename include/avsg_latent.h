@@ -102,12 +102,13 @@ typedef struct avsg_append {
  * A token whose request, position or page is out of range writes no row; one
  * whose position lies outside [0, positions) writes no row either and gets
  * queries of zeros (padding tokens have position -1).  d_q_out may be d_q.  Two
- * tokens of one call with the same row race. */
+ * tokens of one call with the same row race.  tokens * (1 + heads / 8, rounded up) is
+ * at most 67108860, what a launch takes, or AVSG_E_RANGE. */
 avsg_status avsg_kv_append(const avsg_cache *cache, const avsg_append *a, void *stream);
 
 /* Read n rows back as bfloat16 [n][576] (latent, then rotated part; 16-byte
  * aligned, out_stride elements from row to row, a multiple of 8).  Rows out of
- * range read as zeros. */
+ * range read as zeros.  n is at most 67108860, or AVSG_E_RANGE. */
 avsg_status avsg_kv_read(const avsg_cache *cache, int64_t n, const int32_t *d_request,
                          const int64_t *d_position, void *d_out, int64_t out_stride, void *stream);
 
@@ -138,7 +139,8 @@ size_t avsg_attend_workspace_bytes(int32_t batch, int32_t n_q, int32_t heads, in
  * rows are expanded exactly; a probability is a sum of two operands and keeps 12
  * bits at least, or is off by 2^-19 of its token's largest) and add up in float32,
  * as do maxima and sums.  No sum exceeds the rows' largest value, so what is finite
- * in the rows is finite in the result. */
+ * in the rows is finite in the result.  batch * n_q is at most 2^19, heads at most
+ * 4096, and batch * n_q * heads at most what one launch takes (2^26 always), or AVSG_E_RANGE. */
 avsg_status avsg_attend(const avsg_cache *cache, const avsg_attention *a, void *d_workspace,
                         size_t workspace_bytes, void *stream);
 
@@ -148,7 +150,8 @@ avsg_status avsg_attend(const avsg_cache *cache, const avsg_attention *a, void *
  * that brings its largest magnitude into [3.5, 7), values are rounded to the
  * nearest code, ties to the even code; scales are at least 2^-125, and at most
  * 2^125 (magnitudes above 7 * 2^125 become 6 * 2^125).  A block that holds an
- * infinity or a NaN gets scale 255. */
+ * infinity or a NaN gets scale 255.  rows * cols is at most 2^35 - 2048 here
+ * and in avsg_mx4_dequantize, or AVSG_E_RANGE. */
 avsg_status avsg_mx4_quantize(const void *d_x, int32_t type, int64_t rows, int64_t cols, int64_t x_stride,
                               void *d_codes, void *d_scales, void *stream);
 
@@ -168,7 +171,8 @@ avsg_status avsg_mx4_dequantize(const avsg_mx4 *x, int64_t rows, int64_t cols, v
 /* out[i] = a[i] b[i]^T for i in [0, batch): a[i] is [m][k], b[i] is [n][k], both
  * mx4, out[i] [m][n] of out_type with out_stride elements from row to row and
  * out_batch_stride from product to product.  k is a multiple of 32.  Products
- * are exact and add up in float32. */
+ * are exact and add up in float32.  m, n and k are below 2^30, out[i] has fewer than 2^24
+ * tiles of 128 x 128 and batch is at most 65535, or AVSG_E_RANGE. */
 avsg_status avsg_mx4_matmul(const avsg_mx4 *a, const avsg_mx4 *b, int32_t batch, int64_t m, int64_t n,
                             int64_t k, void *d_out, int32_t out_type, int64_t out_stride,
                             int64_t out_batch_stride, void *stream);

@@ -806,7 +806,6 @@ hipError_t launch_format(const AttendParams& p, hipStream_t s) {
   const int head_blocks = head_blocks_of(p.heads, kernel), rows = kernel == AttendKernel::k64Heads ? kWideRows : rows_of(kernel);
   const int tiles = tiles_of(p.topk, rows), each = tiles_of(tiles, p.plan.splits);
   const int64_t groups = static_cast<int64_t>(p.cache.batch) * p.n_q * head_blocks * p.plan.splits;
-  if (groups > INT32_MAX) return hipErrorInvalidValue;
   switch (kernel) {
     case AttendKernel::k16Heads: return launch_narrow<kMx4, 4>(p, groups, head_blocks, each, s);
     case AttendKernel::k16HeadsAlone: return launch_narrow<kMx4, 8>(p, groups, head_blocks, each, s);
@@ -833,6 +832,10 @@ double attend_cost(bool mx4, AttendKernel kernel, int64_t tokens, int heads, int
 }
 
 }  // namespace
+
+int64_t attend_threads(const AttendPlan& plan, int64_t tokens, int heads) {
+  return tokens * head_blocks_of(heads, plan.kernel) * plan.splits * (plan.kernel == AttendKernel::k16Heads ? 256 : 512);
+}
 
 // Which kernel, and how many workgroups share a token's rows: the least of the times
 // above for parts that give 128, 256 or 512 workgroups.  Measured (us, 4-bit rows; 16 heads

@@ -13,6 +13,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 constexpr int kGroup = 8;   // lanes that share one vector of 64 values to rotate
+static_assert(kWaves == 4 && kGroup == kHeadsPerWave, "kMostRowWaves");
 
 // Lane s of eight turns four pairs (a, b) of a 64-vector by the angles of its
 // pairs 4s..4s+3: (a cos - b sin, a sin + b cos) in float32, rounded once.

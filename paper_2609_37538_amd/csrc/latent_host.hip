@@ -70,9 +70,6 @@ avsg_status view_of(const avsg_cache* c, CacheView* v) {
   return AVSG_OK;
 }
 
-// Launch grids are 32 bits wide.
-constexpr int64_t kMostItems = int64_t{1} << 31;
-
 }  // namespace
 
 extern "C" {
@@ -99,8 +96,9 @@ avsg_status avsg_kv_append(const avsg_cache* cache, const avsg_append* a, void* 
   if (a->heads > 0 && (!rows16(a->d_q, a->q_token_stride) || (a->q_head_stride & 7) != 0 ||
                        !rows16(a->d_q_out, a->q_out_token_stride) || (a->q_out_head_stride & 7) != 0))
     return fail(AVSG_E_INVAL, "d_q and d_q_out must be 16-byte aligned with strides in multiples of 8 elements");
-  if (a->heads > 65536 || a->tokens > kMostItems / (1 + a->heads))
-    return fail(AVSG_E_RANGE, "tokens * (1 + heads) must be at most 2^31, heads at most 65536");
+  if (a->heads > 65536 || a->tokens > kMostRowWaves / (1 + (a->heads + kHeadsPerWave - 1) / kHeadsPerWave))
+    return fail(AVSG_E_RANGE, "tokens * (1 + heads / 8, rounded up) must be at most %lld, heads at most 65536",
+                static_cast<long long>(kMostRowWaves));
   p.tokens = a->tokens;
   p.positions = a->positions;
   p.latent = static_cast<const __bf16*>(a->d_latent);
@@ -126,7 +124,7 @@ avsg_status avsg_kv_read(const avsg_cache* cache, int64_t n, const int32_t* d_re
   if (avsg_status st = view_of(cache, &p.cache); st != AVSG_OK) return st;
   if (n < 0) return fail(AVSG_E_INVAL, "n must not be negative");
   if (n == 0) return AVSG_OK;
-  if (n > kMostItems) return fail(AVSG_E_RANGE, "n must be at most 2^31");
+  if (n > kMostRowWaves) return fail(AVSG_E_RANGE, "n must be at most %lld", static_cast<long long>(kMostRowWaves));
   if (!d_request || !d_position) return fail(AVSG_E_INVAL, "d_request and d_position are needed");
   if (!rows16(d_out, out_stride))
     return fail(AVSG_E_INVAL, "d_out must be 16-byte aligned with a stride in multiples of 8 elements");
@@ -159,7 +157,7 @@ avsg_status avsg_attend(const avsg_cache* cache, const avsg_attention* a, void* 
       (a->out_head_stride & 7) != 0)
     return fail(AVSG_E_INVAL, "d_q and d_out must be 16-byte aligned with strides in multiples of 8 elements");
   const int64_t tokens = static_cast<int64_t>(cache->batch) * a->n_q;
-  if (tokens > kMostItems / 4096 || a->heads > 4096)
+  if (tokens > (1 << 19) || a->heads > 4096)
     return fail(AVSG_E_RANGE, "batch * n_q must be at most 2^19 and heads at most 4096");
   p.n_q = a->n_q;
   p.heads = a->heads;
@@ -176,6 +174,8 @@ avsg_status avsg_attend(const avsg_cache* cache, const avsg_attention* a, void* 
   p.out_head_stride = a->out_head_stride;
   p.lse = a->d_lse;
   p.plan = attend_plan(cache->format, cache->batch, a->n_q, a->heads, a->topk);
+  if (attend_threads(p.plan, tokens, a->heads) > kMostThreads)
+    return fail(AVSG_E_RANGE, "batch * n_q * heads is more than a launch takes");
   if (p.plan.splits > 1) {
     const size_t need = avsg_attend_workspace_bytes(cache->batch, a->n_q, a->heads, a->topk);
     if (!d_workspace || !aligned(d_workspace, 256) || workspace_bytes < need)
@@ -195,7 +195,7 @@ avsg_status avsg_mx4_quantize(const void* d_x, int32_t type, int64_t rows, int64
   if (!d_x || !aligned(d_x, 16) || (x_stride & (type == AVSG_F32 ? 3 : 7)) != 0)
     return fail(AVSG_E_INVAL, "d_x and its rows must be 16-byte aligned");
   if (!d_codes || !aligned(d_codes, 16) || !d_scales) return fail(AVSG_E_INVAL, "d_codes (16-byte aligned) and d_scales are needed");
-  if (cols > INT32_MAX || rows > INT64_MAX / cols / 16) return fail(AVSG_E_RANGE, "too many values");
+  if (cols > INT32_MAX || rows > kMostChunks / (cols / 8)) return fail(AVSG_E_RANGE, "rows * cols must be at most 2^35 - 2048");
   return launched(launch_mx4_quantize(d_x, type == AVSG_F32, rows, cols, x_stride, static_cast<uint8_t*>(d_codes),
                                       static_cast<uint8_t*>(d_scales), static_cast<hipStream_t>(stream)),
                   "avsg_mx4_quantize");
@@ -212,7 +212,7 @@ avsg_status avsg_mx4_dequantize(const avsg_mx4* x, int64_t rows, int64_t cols, v
     return fail(AVSG_E_INVAL, "codes and their rows must be 16-byte aligned");
   if (!d_out || !aligned(d_out, 16) || (out_stride & (type == AVSG_F32 ? 3 : 7)) != 0)
     return fail(AVSG_E_INVAL, "d_out and its rows must be 16-byte aligned");
-  if (cols > INT32_MAX || rows > INT64_MAX / cols / 16) return fail(AVSG_E_RANGE, "too many values");
+  if (cols > INT32_MAX || rows > kMostChunks / (cols / 8)) return fail(AVSG_E_RANGE, "rows * cols must be at most 2^35 - 2048");
   const Mx4View v{static_cast<const uint8_t*>(x->d_codes), static_cast<const uint8_t*>(x->d_scales), x->code_stride,
                   x->code_batch_stride, x->scale_stride, x->scale_batch_stride};
   return launched(launch_mx4_dequantize(v, rows, cols, d_out, type == AVSG_F32, out_stride,
@@ -227,6 +227,8 @@ avsg_status avsg_mx4_matmul(const avsg_mx4* a, const avsg_mx4* b, int32_t batch,
   if (k % kMx4Block != 0) return fail(AVSG_E_RANGE, "k must be a multiple of %d", kMx4Block);
   if (m > INT32_MAX / 2 || n > INT32_MAX / 2 || k > INT32_MAX / 2 || batch > 65535)
     return fail(AVSG_E_RANGE, "m, n and k must be below 2^30 and batch at most 65535");
+  if ((m + 127) / 128 * ((n + 127) / 128) > kMostThreads / 256)
+    return fail(AVSG_E_RANGE, "m x n must have fewer than 2^24 tiles of 128 x 128");
   if (batch == 0 || m == 0 || n == 0) return AVSG_OK;
   if (!d_out || !aligned(d_out, out_type == AVSG_F32 ? 4 : 2)) return fail(AVSG_E_INVAL, "d_out is null or misaligned");
   const avsg_mx4* both[2] = {a, b};

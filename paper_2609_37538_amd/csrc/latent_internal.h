@@ -10,6 +10,8 @@
 
 namespace avsg {
 
+constexpr int64_t kMostThreads = (int64_t{1} << 32) - 1;   // of a launch, along a dimension
+
 constexpr int kLatent = 512;           // latent values of a row: key and value
 constexpr int kRope = 64;              // rotated values of a row: key only
 constexpr int kKeyDim = kLatent + kRope;
@@ -123,6 +125,13 @@ struct ReadParams {
   int64_t out_stride;
 };
 
+// Rows that a launch of append or read takes: a wave each, four to a workgroup.
+constexpr int64_t kMostRowWaves = kMostThreads / 256 * 4;
+// Eight columns of a matrix that a launch of quantise or dequantise takes, a thread each.
+constexpr int64_t kMostChunks = kMostThreads / 256 * 256;
+// Heads' queries that one wave of append rotates.
+constexpr int kHeadsPerWave = 8;
+
 // How a call of attention is carried out.
 enum class AttendKernel {
   k16Heads,        // 16 heads per workgroup, tiles of 64 rows, two workgroups per CU
@@ -188,6 +197,8 @@ hipError_t allow_lds(size_t bytes) {
 
 hipError_t launch_kv_append(const AppendParams& p, int format, int rope_style, hipStream_t s);
 hipError_t launch_kv_read(const ReadParams& p, int format, hipStream_t s);
+// threads of a call's attention kernel
+int64_t attend_threads(const AttendPlan& plan, int64_t tokens, int heads);
 // the kernel of a call of attention, and how many workgroups share a token
 AttendPlan attend_plan(int format, int batch, int n_q, int heads, int topk);
 hipError_t launch_attend(const AttendParams& p, int format, hipStream_t s);

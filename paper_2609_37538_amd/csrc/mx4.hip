@@ -8,6 +8,7 @@ namespace avsg {
 namespace {
 
 constexpr int kThreads = 256;
+static_assert(kMostChunks % kThreads == 0);
 
 // Eight columns per thread: 16 bytes of bfloat16 (32 of float32) in, one word of
 // codes out; four neighbouring lanes hold a block of 32 and agree on its scale.
@@ -63,8 +64,7 @@ __global__ __launch_bounds__(kThreads) void dequantize_kernel(Mx4View x, int64_t
 hipError_t launch_mx4_quantize(const void* x, bool f32, int64_t rows, int64_t cols, int64_t x_stride, uint8_t* codes,
                                uint8_t* scales, hipStream_t s) {
   const int64_t chunks = rows * (cols / 8);
-  const int64_t blocks = (chunks + kThreads - 1) / kThreads;
-  if (blocks > INT32_MAX) return hipErrorInvalidValue;
+  const int64_t blocks = (chunks + kThreads - 1) / kThreads;   // chunks <= kMostChunks
   const uint32_t per_row = static_cast<uint32_t>(cols / 8);
   const dim3 grid(static_cast<unsigned>(blocks));
   if (f32) quantize_kernel<true><<<grid, kThreads, 0, s>>>(x, chunks, per_row, x_stride, codes, scales);
@@ -75,8 +75,7 @@ hipError_t launch_mx4_quantize(const void* x, bool f32, int64_t rows, int64_t co
 hipError_t launch_mx4_dequantize(const Mx4View& x, int64_t rows, int64_t cols, void* out, bool f32, int64_t out_stride,
                                  hipStream_t s) {
   const int64_t chunks = rows * (cols / 8);
-  const int64_t blocks = (chunks + kThreads - 1) / kThreads;
-  if (blocks > INT32_MAX) return hipErrorInvalidValue;
+  const int64_t blocks = (chunks + kThreads - 1) / kThreads;   // chunks <= kMostChunks
   const uint32_t per_row = static_cast<uint32_t>(cols / 8);
   const dim3 grid(static_cast<unsigned>(blocks));
   if (f32) dequantize_kernel<true><<<grid, kThreads, 0, s>>>(x, chunks, per_row, out, out_stride);

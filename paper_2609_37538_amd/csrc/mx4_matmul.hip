@@ -433,7 +433,6 @@ hipError_t launch(const Mx4Product& p, hipStream_t s) {
   auto tiles = [](int64_t rows, int64_t by) { return (rows + by - 1) / by; };
   const int64_t tiles_m = tiles(p.m, 128), tiles_n = tiles(p.n, 128), wide_m = tiles(p.m, 256), wide_n = tiles(p.n, 256);
   const int64_t small_m = tiles(p.m, 64), small_n = tiles(p.n, 64);
-  if (small_m * small_n > INT32_MAX) return hipErrorInvalidValue;
   // offsets within a tile's rows are held in 32 bits
   const int64_t longest = std::max(p.a.code_stride, p.b.code_stride);
   const bool staged = p.k >= 256 && p.a.code_stride >= 0 && p.b.code_stride >= 0 && longest * 256 + p.k < (int64_t{1} << 31);

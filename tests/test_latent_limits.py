@@ -2,6 +2,7 @@
 import pytest
 import torch
 
+from paper_2609_37538_amd import avsg as A
 from paper_2609_37538_amd import latent as L
 
 MOST = 2 ** 31 - 1
@@ -30,3 +31,22 @@ def test_attend_without_a_limit(longest, batch, n_q, heads, mx4):
     lens[0, 0] = 700       # 200 of them are not there
     out, lse = cache.attend(q, lens=lens, longest=longest, scale=SCALE)
     check_attend(cache, q, out, lse, lens=lens, longest=700)
+
+
+def test_more_than_a_launch_takes():
+    """Counts that no launch takes are refused by the checks, with the status that says so."""
+    from test_latent_abi import append, attention, cache, status
+    rng, rows = A.AVSG_E_RANGE, 67108860
+    for heads, per in ((0, 1), (8, 2), (9, 3), (128, 17)):
+        q = dict(heads=heads, d_q=4096, q_token_stride=64 * heads, q_head_stride=64, d_q_out=4096, q_out_token_stride=64 * heads,
+                 q_out_head_stride=64)
+        assert status(L.avsg_kv_append, cache(), append(tokens=rows // per + 1, **q)) == rng
+    assert status(L.avsg_kv_read, cache(), rows + 1, 4096, 4096, 4096, 576) == rng
+    many = cache(batch=2 ** 19, pages=2 ** 19, pages_per_request=1)
+    assert status(L.avsg_attend, many, attention(heads=4096, topk=0), None, 0) == rng
+    assert status(L.avsg_mx4_quantize, 4096, 0, 2 ** 30, 32, 32, 4096, 4096) == rng
+    assert status(L.avsg_mx4_quantize, 4096, 1, 2 ** 20, 2 ** 15, 2 ** 15, 4096, 4096) == rng
+    x = L.AvsgMx4(4096, 4096, 16, 16, 1, 1)
+    assert status(L.avsg_mx4_dequantize, x, 2 ** 30, 32, 4096, 0, 32) == rng
+    assert status(L.avsg_mx4_matmul, x, x, 1, 2 ** 19, 2 ** 19, 32, 4096, 0, 2 ** 19, 0) == rng
+    assert status(L.avsg_mx4_matmul, x, x, 1, 129, 2 ** 30 - 1, 32, 4096, 0, 2 ** 30, 0) == rng
