@@ -245,7 +245,7 @@ class LatentCache:
             per = pages // batch
         self.rows_per_request = per * page_rows
         self.c = AvsgCache(base, pages, page_stride, row_stride, row_format, batch, page_rows, per, table)
-        self._workspace = {}     # bytes by (n_q, heads, entries)
+        self._workspace = (None, 0)     # the last call's (n_q, heads, entries), and its bytes
 
     @classmethod
     def of_slots(cls, operator, row_format: Optional[int] = None) -> "LatentCache":
@@ -323,9 +323,10 @@ class LatentCache:
             lse_at = lse.data_ptr()
         else:
             lse_at = _ints(lse, _t.float32, (b, n_q, heads), dev, "lse")
-        need = self._workspace.get((n_q, heads, k))
-        if need is None:
-            need = self._workspace[n_q, heads, k] = avsg_attend_workspace_bytes(b, n_q, heads, k)
+        last, need = self._workspace
+        if last != (n_q, heads, k):
+            need = avsg_attend_workspace_bytes(b, n_q, heads, k)
+            self._workspace = ((n_q, heads, k), need)
         ws = _t.empty(need, dtype=_t.uint8, device=dev) if need else None
         a = AvsgAttention(n_q, heads, k, scale, qa, qt, qh, rows_at, index_at, lens_at, oa, ot, oh, lse_at)
         _run(_lib.avsg_attend, "avsg_attend", dev.index, self.c, a, ws.data_ptr() if need else None, need)

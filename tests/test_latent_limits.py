@@ -50,3 +50,22 @@ def test_more_than_a_launch_takes():
     assert status(L.avsg_mx4_dequantize, x, 2 ** 30, 32, 4096, 0, 32) == rng
     assert status(L.avsg_mx4_matmul, x, x, 1, 2 ** 19, 2 ** 19, 32, 4096, 0, 2 ** 19, 0) == rng
     assert status(L.avsg_mx4_matmul, x, x, 1, 129, 2 ** 30 - 1, 32, 4096, 0, 2 ** 30, 0) == rng
+
+
+@pytest.mark.gpu
+def test_cache_keeps_nothing_of_past_calls():
+    """Contexts that grow by a position per step, as a decode over whole contexts has them."""
+    from test_latent import SCALE, check_attend, gen, normal, pool_of
+    g = gen(31)
+    cache = L.LatentCache(pool_of(g, 1, 400, True), 1, 1)
+    q = normal(g, 1, 1, 16, 576)
+
+    def held():
+        return sum(len(x) for x in vars(cache).values() if isinstance(x, (dict, list, set, tuple)))
+
+    cache.attend(q, longest=300, scale=SCALE)
+    before = held()
+    for longest in (301, 302, 40, 303, 40, 399, 400, 1):
+        out, lse = cache.attend(q, longest=longest, scale=SCALE)
+        check_attend(cache, q, out, lse, longest=longest)
+    assert held() == before
