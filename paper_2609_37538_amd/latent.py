@@ -7,7 +7,8 @@ tensors.
 appends to, reads and attends over them; :class:`Mx4` is a matrix in 4-bit
 microscaled form, made by :func:`mx4_quantize`.  The wrappers run on the current
 stream of their tensors' GPU and raise ValueError for tensors the kernels do not
-take (they copy nothing behind the caller's back).
+take (they copy nothing behind the caller's back).  None of them has a backward
+pass: with gradients enabled they raise ValueError for tensors that require one.
 """
 from __future__ import annotations
 
@@ -160,6 +161,13 @@ def _need(ok: bool, what: str) -> None:
         raise ValueError(what)
 
 
+def _no_gradient(what: str) -> None:
+    """For a tensor that requires a gradient: there is none, so with gradients enabled it would be lost."""
+    if _t.is_grad_enabled():
+        raise ValueError(f"{what} requires a gradient, which this operator does not have: "
+                         "detach it, or call under torch.no_grad()")
+
+
 def _run(f, where: str, index: int, *args) -> None:
     """Calls f on the current stream of GPU `index`, with that GPU current."""
     if _current() == index:
@@ -172,6 +180,8 @@ def _run(f, where: str, index: int, *args) -> None:
 
 
 def _ints(x, dtype, shape, device, what) -> int:
+    if x.requires_grad:
+        _no_gradient(what)
     if x.dtype is not dtype or x.shape != shape or x.device != device or not x.is_contiguous():
         raise ValueError(f"{what} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {device}")
     return x.data_ptr()
@@ -179,6 +189,8 @@ def _ints(x, dtype, shape, device, what) -> int:
 
 def _vectors(x, shape, device, what):
     """(address, strides) of a bfloat16 tensor whose vectors (last dimension) are read 16 bytes at a time."""
+    if x.requires_grad:
+        _no_gradient(what)
     if x.dtype is not _t.bfloat16 or x.shape != shape or x.device != device:
         raise ValueError(f"{what} must be a bfloat16 tensor of shape {tuple(shape)} on {device}")
     at, strides = x.data_ptr(), x.stride()
@@ -419,6 +431,8 @@ def _mx4(device, base, shape, code_strides, scale_strides) -> Mx4:
 
 
 def _plain_type(x, what):
+    if x.requires_grad:
+        _no_gradient(what)
     if x.dtype is _t.bfloat16 and x.is_cuda:
         return AVSG_BF16
     _need(x.is_cuda and x.dtype is _t.float32, f"{what} must be a bfloat16 or float32 cuda tensor")

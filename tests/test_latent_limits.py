@@ -69,3 +69,35 @@ def test_cache_keeps_nothing_of_past_calls():
         out, lse = cache.attend(q, longest=longest, scale=SCALE)
         check_attend(cache, q, out, lse, longest=longest)
     assert held() == before
+
+
+@pytest.mark.gpu
+def test_gradients_are_not_lost_silently():
+    """Tensors that require a gradient are refused where gradients are enabled, as torch refuses them for `out`."""
+    from test_latent import angles_of, gen, normal, pool_of
+    g = gen(32)
+    cache = L.LatentCache(pool_of(g, 1, 64, True), 1, 1)
+    q, latent, rope, turn = normal(g, 1, 1, 16, 576), normal(g, 1, 512), normal(g, 1, 64), normal(g, 1, 2, 64)
+    at, angles, w = torch.zeros(1, dtype=torch.int64, device="cuda"), angles_of(64), normal(g, 32, 64)
+    out, plain = torch.empty(1, 1, 16, 512, dtype=torch.bfloat16, device="cuda"), torch.randn(8, 64, device="cuda")
+    lse, rows = torch.empty(1, 1, 16, device="cuda"), torch.empty(1, 576, dtype=torch.bfloat16, device="cuda")
+    product = torch.empty(32, 32, dtype=torch.bfloat16, device="cuda")
+
+    def calls():
+        return [(q, lambda: cache.attend(q, scale=1.0)), (out, lambda: cache.attend(q, scale=1.0, out=out)),
+                (lse, lambda: cache.attend(q, scale=1.0, lse=lse)), (rows, lambda: cache.read(at.int(), at, out=rows))] + [
+            (x, lambda: cache.append(latent, rope, at.int(), at, angles, q_rope=turn, q_out=turn[:, :]))
+            for x in (latent, rope, angles, turn)] + [
+            (w, lambda: L.mx4_quantize(w)), (plain, lambda: L.mx4_quantize(plain)),
+            (product, lambda: L.mx4_matmul(L.mx4_quantize(w), L.mx4_quantize(w), out=product))]
+
+    for i, (x, call) in enumerate(calls()):
+        call()
+        x.requires_grad_()
+        with pytest.raises(ValueError, match="gradient"):
+            call()
+            pytest.fail(f"call {i} lost a gradient")
+        with torch.no_grad():
+            call()
+        x.requires_grad_(False)
+        call()
