@@ -129,7 +129,10 @@ typedef struct avsg_attention {
 } avsg_attention;
 
 /* Bytes of device workspace avsg_attend needs (256-byte aligned; contents do
- * not matter before or after a call), 0 when it needs none. */
+ * not matter before or after a call), 0 when it needs none.  They are those of a call
+ * of exactly these sizes: one of fewer requests, tokens, heads or entries, which more
+ * workgroups share, may need more.  AVSG_ATTEND_WORKSPACE_MOST are enough for any call. */
+#define AVSG_ATTEND_WORKSPACE_MOST 33685504
 size_t avsg_attend_workspace_bytes(int32_t batch, int32_t n_q, int32_t heads, int32_t topk);
 
 /* out = sum_i softmax_i(scale * q . key_i) * value_i over the entries i of a

@@ -141,10 +141,12 @@ size_t avsg_attend_workspace_bytes(int32_t batch, int32_t n_q, int32_t heads, in
   // of either row format, whichever has more parts
   const size_t splits = static_cast<size_t>(std::max(attend_plan(AVSG_ROWS_BF16, batch, n_q, heads, topk).splits,
                                                      attend_plan(AVSG_ROWS_MX4, batch, n_q, heads, topk).splits));
-  if (splits <= 1) return 0;
+  if (splits <= 1) return 0;   // else at most 256 workgroups of 64 heads, or 512 of 16
   const size_t parts = static_cast<size_t>(batch) * n_q * splits * heads;
   return parts * (kLatent * sizeof(float) + sizeof(f32x2));
 }
+
+static_assert(AVSG_ATTEND_WORKSPACE_MOST == kMostParts * (kLatent * sizeof(float) + sizeof(f32x2)));
 
 avsg_status avsg_attend(const avsg_cache* cache, const avsg_attention* a, void* d_workspace, size_t workspace_bytes,
                         void* stream) {

@@ -142,6 +142,9 @@ constexpr int heads_of(AttendKernel k) { return k == AttendKernel::k64Heads ? 64
 // the least part of a token's rows that a workgroup takes
 constexpr int rows_of(AttendKernel k) { return k == AttendKernel::k16HeadsAlone ? 128 : 64; }
 
+// Parts of results, of a head each, that the workgroups of a call leave: tokens * splits * heads
+constexpr int64_t kMostParts = 256 * 64;
+
 struct AttendPlan {
   AttendKernel kernel;
   int32_t splits;   // workgroups that share a query token's entries

@@ -27,6 +27,7 @@ AVSG_ROPE_PAIRS = 0
 AVSG_ROPE_HALVES = 1
 AVSG_BF16 = 0
 AVSG_F32 = 1
+AVSG_ATTEND_WORKSPACE_MOST = 33685504     # bytes, enough for any call of avsg_attend
 KEY_DIM = AVSG_LATENT_DIM + AVSG_ROPE_DIM
 
 _i32, _i64, _sz = ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t

@@ -1,4 +1,6 @@
 """The latent-cache operators at the ends of what their arguments can say."""
+import random
+
 import pytest
 import torch
 
@@ -101,3 +103,15 @@ def test_gradients_are_not_lost_silently():
             call()
         x.requires_grad_(False)
         call()
+
+
+def test_workspace_enough_for_any_call():
+    """A smaller call may need more workspace than a larger one; there is a size that is enough for all."""
+    rng, needs = random.Random(5), {}
+    sizes = [(batch, n_q, heads, k) for batch in (1, 4, 16, 32, 48, 64) for n_q in (1, 2, 4) for heads in (1, 16, 17, 64, 128, 4096)
+             for k in (1, 64, 65, 128, 700, 2048, 4096, 131072, MOST)]
+    sizes += [(rng.randint(1, 300), rng.randint(1, 4), rng.randint(1, 300), int(2 ** rng.uniform(0, 24))) for _ in range(5000)]
+    for s in sizes:
+        needs[s] = L.avsg_attend_workspace_bytes(*s)
+    assert any(needs[batch, 2, 128, 2048] > needs[64, 2, 128, 2048] for batch in (1, 4, 16, 32, 48))
+    assert 0.9 * L.AVSG_ATTEND_WORKSPACE_MOST < max(needs.values()) <= L.AVSG_ATTEND_WORKSPACE_MOST
