@@ -814,21 +814,22 @@ hipError_t launch_format(const AttendParams& p, hipStream_t s) {
 }
 
 // Time of a call in us, from ones that were timed in a graph: what a workgroup needs
-// at its start and end, its tiles, and the parts written and joined.  916 calls
-// of 1 to 128 tokens, 8 to 128 heads, 150 to 2048 rows and of long contexts took 5%
-// more or less than this says, and the choices made by it 0.4% more than the best.
+// at its start and end, its tiles, and the parts written and joined.  920 calls
+// of 1 to 128 tokens, 8 to 128 heads, 150 to 2048 rows and of long contexts, 3992 ways in all, took 5%
+// more or less than this says, and the ways chosen by it 0.1% more than the best
+// (5% at worst); their times are in profiles/latent_attend_choices.csv.
 double attend_cost(bool mx4, AttendKernel kernel, int64_t tokens, int heads, int tiles, int splits) {
   const int64_t groups = tokens * head_blocks_of(heads, kernel) * splits;
   const int each = (tiles + splits - 1) / splits;
   auto rounds = [&](int64_t at_once) { return static_cast<double>((groups + at_once - 1) / at_once); };
   double at = 0;
-  if (kernel == AttendKernel::k64Heads) at = rounds(256) * (5.7 + 0.1 * std::min(heads, 64) + (mx4 ? 2.1 : 2.4) * each);
-  else if (kernel == AttendKernel::k16HeadsAlone) at = rounds(256) * (8.2 + (mx4 ? 2.3 : 4.6) * each);
+  if (kernel == AttendKernel::k64Heads) at = rounds(256) * (5.9 + 0.09 * std::min(heads, 64) + 2.7 * each);
+  else if (kernel == AttendKernel::k16HeadsAlone) at = rounds(256) * (8.2 + (mx4 ? 2.5 : 4.8) * each);
   else if (groups <= 256) at = 6. + (mx4 ? 1.7 : 2.5) * each;   // a CU has one workgroup and not two
-  else at = rounds(512) * (8.1 + (mx4 ? 2.2 : 4.1) * each);
+  else at = rounds(512) * (7.9 + (mx4 ? 2.4 : 4.2) * each);
   if (splits == 1) return at;
   const double megabytes = static_cast<double>(tokens) * splits * heads * (kLatent * 4) / 1e6;
-  return at + 1.9 + 0.6 * std::min(megabytes, 17.) + 0.04 * std::max(megabytes - 17., 0.);
+  return at + 2.0 + 0.6 * std::min(megabytes, 17.) + 0.1 * std::max(megabytes - 17., 0.);
 }
 
 }  // namespace
@@ -842,18 +843,18 @@ int64_t attend_threads(const AttendPlan& plan, int64_t tokens, int heads) {
 // with 64-row tiles in 256 and 512 workgroups, with 128-row tiles in 256, 64 heads
 // in 128 and 256):
 //   tokens x heads x rows    64 rows: 256    512    128 rows    64 heads: 128    256
-//       1 x  64 x   256          9.7         9.7      12.4          15.8        16.0
-//      33 x  40 x  1000         24.8        26.2      23.0          28.1        26.9
-//      33 x  64 x  1000         32.6        31.4      27.4          33.3        30.2
-//      64 x  64 x  2048         60.2        51.3      46.5          53.2        40.1
-//     128 x  64 x   256         20.0        19.8      24.9          21.5        27.7
-//     128 x 128 x  2048        151.5       151.5     179.7          84.2        84.6
-//       4 x  16 x 131072        65.9        52.4      51.9
-//       1 x  16 x 131072        28.6        32.7      27.7
+//       1 x  64 x   256          9.9         9.9      12.7          16.4        16.4
+//      33 x  40 x  1000         25.4        26.9      24.0          31.4        29.1
+//      33 x  64 x  1000         34.2        32.0      28.9          35.9        32.3
+//      64 x  64 x  2048         63.0        55.0      50.0          64.0        47.0
+//     128 x  64 x   256         20.3        20.2      26.1          24.5        29.6
+//     128 x 128 x  2048        161.8       161.8     193.5         109.1       105.5
+//       4 x  16 x 131072        68.5        55.7      55.8
+//       1 x  16 x 131072        28.0        32.4      27.3
 //   the same in bfloat16:
-//       1 x  64 x   256         10.8        10.8      15.3          16.7        16.7
-//      16 x  64 x  2048         31.9        33.8      32.6          29.5        28.1
-//      33 x  40 x  1000         30.3        31.8      31.2          28.2        25.2
+//       1 x  64 x   256         10.9        10.9      15.6          17.3        17.4
+//      16 x  64 x  2048         32.4        34.1      34.1          31.5        29.4
+//      33 x  40 x  1000         31.1        31.8      32.6          30.2        26.8
 AttendPlan attend_plan(int format, int batch, int n_q, int heads, int topk) {
   const int64_t tokens = static_cast<int64_t>(batch) * n_q;
   AttendPlan best{AttendKernel::k16Heads, 1};
