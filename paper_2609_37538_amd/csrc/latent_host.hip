@@ -188,6 +188,11 @@ avsg_status avsg_attend(const avsg_cache* cache, const avsg_attention* a, void* 
   return launched(launch_attend(p, cache->format, static_cast<hipStream_t>(stream)), "avsg_attend");
 }
 
+int64_t avsg_internal_attend_plan(int32_t format, int32_t batch, int32_t n_q, int32_t heads, int32_t topk) {
+  const AttendPlan plan = attend_plan(format, batch, n_q, heads, topk);
+  return static_cast<int64_t>(plan.kernel) | static_cast<int64_t>(plan.splits) << 32;
+}
+
 avsg_status avsg_mx4_quantize(const void* d_x, int32_t type, int64_t rows, int64_t cols, int64_t x_stride, void* d_codes,
                               void* d_scales, void* stream) {
   if (type != AVSG_BF16 && type != AVSG_F32) return fail(AVSG_E_INVAL, "unknown type %d", type);

@@ -212,3 +212,7 @@ hipError_t launch_mx4_dequantize(const Mx4View& x, int64_t rows, int64_t cols, v
 hipError_t launch_mx4_matmul(const Mx4Product& p, hipStream_t s);
 
 }  // namespace avsg
+
+// attend_plan for tests, which assert what their cases run: the kernel in the low half, the parts in the high
+// one.  Not part of the ABI.
+extern "C" int64_t avsg_internal_attend_plan(int32_t format, int32_t batch, int32_t n_q, int32_t heads, int32_t topk);
