@@ -115,3 +115,14 @@ def test_workspace_enough_for_any_call():
         needs[s] = L.avsg_attend_workspace_bytes(*s)
     assert any(needs[batch, 2, 128, 2048] > needs[64, 2, 128, 2048] for batch in (1, 4, 16, 32, 48))
     assert 0.9 * L.AVSG_ATTEND_WORKSPACE_MOST < max(needs.values()) <= L.AVSG_ATTEND_WORKSPACE_MOST
+
+
+def test_workspaces_are_checked():
+    """A long context of one request is shared by several workgroups, so a workspace is asked for, and one that is
+    missing, too small or misaligned is refused."""
+    from test_latent_abi import attention, cache, status
+    need = L.avsg_attend_workspace_bytes(1, 1, 16, 100000)
+    assert need > 0
+    big = cache(batch=1, pages=2000, pages_per_request=2000)
+    for at, size in ((None, need), (None, 0), (4096, need - 1), (4097, need), (4096 + 128, need)):
+        assert status(L.avsg_attend, big, attention(topk=100000), at, size) == A.AVSG_E_INVAL
