@@ -615,14 +615,14 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams p, int
       }
     }
     if constexpr (kOutput) {
-      // the weights' rests, whose products run beside what follows
       const unsigned char* const rest_from = rests + (t & 1) * kTiles * 512 + lane16 / 2;
+      bf16x8 low[kTiles];
 #pragma unroll
-      for (int h = 0; h < kTiles; ++h) {
-        const bf16x8 rest = rest_decode(*reinterpret_cast<const u32x2*>(rest_from + h * 512), p.rest_unit);
+      for (int h = 0; h < kTiles; ++h) low[h] = rest_decode(*reinterpret_cast<const u32x2*>(rest_from + h * 512), p.rest_unit);
 #pragma unroll
-        for (int c = 0; c < kColTiles; ++c) out[c][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[c], rest, out[c][h], 0, 0, 0);
-      }
+      for (int c = 0; c < kColTiles; ++c)
+#pragma unroll
+        for (int h = 0; h < kTiles; ++h) out[c][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[c], low[h], out[c][h], 0, 0, 0);
     }
     if constexpr (kWeights) {
       s = (mine + theirs[0]) + (theirs[1] + theirs[2]);
