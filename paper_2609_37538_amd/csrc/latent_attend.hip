@@ -213,11 +213,11 @@ __device__ __forceinline__ void store_head(const AttendParams& p, const Share& w
 // 16 heads at a time: few heads, or few tokens.  Four waves score 16 rows each against
 // all 576 columns, leave weights and expanded values in LDS, and take 128 of the 512
 // columns each of the output.  So few heads make the rows' bytes count, and two
-// workgroups per CU keep 50 KB of them in flight: 4 x 131072 rows of 400 bytes for 16 heads
-// take 51 us, 4.1 TB/s, where a large copy moves 5.0.  A call of one token takes 7 us,
+// workgroups per CU keep 50 KB of them in flight.  A call of one token takes 7 us,
 // launch, three dependent loads (entry, row, next tile's) and one tile.  Or eight waves
-// and tiles of 128 rows: 2.3 us each where a lone workgroup of four takes 1.7 for 64,
-// and half the parts of two workgroups.
+// and tiles of 128 rows: 2.5 us each where a lone workgroup of four takes 1.7 for 64,
+// and half the parts of two workgroups: 4 x 131072 rows of 400 bytes for 16 heads take
+// 58 us, 3.6 TB/s, where a large copy moves 5.0.
 template <bool kMx4, int kWaves>
 __global__ __launch_bounds__(kWaves * 64, 2) void attend_kernel(AttendParams p, int head_blocks, int tiles_per_split) {
   constexpr int kRows = kWaves * 16, kCols = kLatent / kWaves, kColTiles = kCols / 16;
@@ -392,13 +392,12 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_kernel(AttendParams p, 
 //   output   it multiplies all 32 rows' weights of all heads with 64 of the 512
 //            columns of the values.
 // Alone, each stage keeps one unit of a CU busy (matrix cores, LDS, conversion,
-// exponentials) and then waits for the others' waves: one after the other, with
-// a barrier each, they took 7100 cycles per 64 rows, of which the matrix cores worked
-// 2200, also with two such workgroups of 32 heads on a CU.  In one stream they overlap:
-// 2200 cycles per 32 rows, the matrix cores 1100, and 92 us for 128 tokens of 128 heads
-// over 2048 rows each (73 GFLOP).  What is left is spread: without the loads it took
-// 19% less, without the writes of values 20%, without the exchange of scores 15%,
-// without the output's products 19%.
+// exponentials) and then waits for the others' waves; in one stream they overlap.
+// 128 tokens of 128 heads over 2048 rows each take 104 us, 1.4 us per 32 rows, of which
+// the products take 1600 cycles, about half: 18 matrix instructions of scores per wave, 16 of the
+// output and 16 for the weights' rests, without which it took 81 us.  Of the other half one part is
+// known: every second tile the first wave reads the entries of two tiles at the end of a stage, and
+// waits for them with its keys at the start of the next, where all waves then wait for it.
 constexpr int kWideRows = 32;
 constexpr int kWideHeads = 64;
 
@@ -817,7 +816,7 @@ hipError_t launch_format(const AttendParams& p, hipStream_t s) {
 // at its start and end, its tiles, and the parts written and joined.  920 calls
 // of 1 to 128 tokens, 8 to 128 heads, 150 to 2048 rows and of long contexts, 3992 ways in all, took 5%
 // more or less than this says, and the ways chosen by it 0.1% more than the best
-// (5% at worst); their times are in profiles/latent_attend_choices.csv.
+// (6% at worst); their times are in profiles/latent_attend_choices.csv.
 double attend_cost(bool mx4, AttendKernel kernel, int64_t tokens, int heads, int tiles, int splits) {
   const int64_t groups = tokens * head_blocks_of(heads, kernel) * splits;
   const int each = (tiles + splits - 1) / splits;
@@ -843,18 +842,18 @@ int64_t attend_threads(const AttendPlan& plan, int64_t tokens, int heads) {
 // with 64-row tiles in 256 and 512 workgroups, with 128-row tiles in 256, 64 heads
 // in 128 and 256):
 //   tokens x heads x rows    64 rows: 256    512    128 rows    64 heads: 128    256
-//       1 x  64 x   256          9.9         9.9      12.7          16.4        16.4
-//      33 x  40 x  1000         25.4        26.9      24.0          31.4        29.1
-//      33 x  64 x  1000         34.2        32.0      28.9          35.9        32.3
-//      64 x  64 x  2048         63.0        55.0      50.0          64.0        47.0
-//     128 x  64 x   256         20.3        20.2      26.1          24.5        29.6
-//     128 x 128 x  2048        161.8       161.8     193.5         109.1       105.5
-//       4 x  16 x 131072        68.5        55.7      55.8
-//       1 x  16 x 131072        28.0        32.4      27.3
+//       1 x  64 x    256          9.9         9.8     12.8          16.5        16.4
+//      33 x  40 x   1000         25.8        27.2     24.3          31.0        29.2
+//      33 x  64 x   1000         34.4        32.1     28.9          35.4        32.4
+//      64 x  64 x   2048         63.3        54.9     50.2          62.5        45.8
+//     128 x  64 x    256         20.3        20.3     26.0          24.2        29.6
+//     128 x 128 x   2048        162.0       162.0    193.7         105.2       105.3
+//       4 x  16 x 131072         67.8        55.4     55.8
+//       1 x  16 x 131072         27.6        32.1     27.0
 //   the same in bfloat16:
-//       1 x  64 x   256         10.9        10.9      15.6          17.3        17.4
-//      16 x  64 x  2048         32.4        34.1      34.1          31.5        29.4
-//      33 x  40 x  1000         31.1        31.8      32.6          30.2        26.8
+//       1 x  64 x    256         10.9        10.9     15.5          17.4        17.4
+//      16 x  64 x   2048         32.2        34.0     34.2          31.4        29.4
+//      33 x  40 x   1000         31.1        31.8     32.8          30.4        27.0
 AttendPlan attend_plan(int format, int batch, int n_q, int heads, int topk) {
   const int64_t tokens = static_cast<int64_t>(batch) * n_q;
   AttendPlan best{AttendKernel::k16Heads, 1};

@@ -1,6 +1,6 @@
 // The 4-bit microscaled form: quantisation and its inverse.  A value is read and
 // written once and takes a few operations, so memory bounds large matrices: 8192 x 4096
-// of bfloat16 are quantised in 19 to 20 us (85 MB, 4.3 TB/s; a large copy moves 5.0).
+// of bfloat16 are quantised in 19 to 21 us (85 MB, 4.2 TB/s; a large copy moves 5.0).
 // 16384 x 512, which the caches hold, takes 5.5 us either way, one small matrix 2.
 #include "latent_internal.h"
 

@@ -169,9 +169,10 @@ __global__ __launch_bounds__(kWaves * 64) void thin_kernel(Mx4Product p) {
 
 // Tiles of kTileM x kTileN outputs, kWavesM x kWavesN waves.  Operands come
 // straight from global memory: a lane's 16 bytes are one row's block, so there is
-// nothing to rearrange, and the waves that share rows find them in L1.
-// Steps of 256 columns; the next step's loads are issued before this one's
-// products.
+// nothing to rearrange, and the waves that share rows find them in L1.  Steps of 128
+// columns, loads and then products; nothing is fetched ahead, for with fewer than 256 columns
+// there are one or two steps.  128 products of 128 x 512 x 128 take 9.8 us (22 MB, 17 of them
+// results).
 template <int kTileM, int kTileN, int kWavesM, int kWavesN, bool kF32>
 __global__ __launch_bounds__(kWavesM * kWavesN * 64) void tile_kernel(Mx4Product p, int tiles_m, int tiles_n) {
   constexpr int kM = kTileM / kWavesM / 16, kN = kTileN / kWavesN / 16;
@@ -242,10 +243,11 @@ __device__ __forceinline__ int exchange(int row, bool by_eights) {
 // three bits of the row, so that the sixteen lanes that read one block of sixteen
 // rows meet every bank; eight neighbouring lanes fetch a row's whole line.  kGroups groups
 // of such waves share the columns, a run of steps each, and add up in LDS.
-// 8192 x 4096 x 4096 takes 83 to 97 us, 2.8 to 3.3 PFLOP/s.  Its loop takes 4200 cycles
-// per step where the products take 2048: 2500 without the loads, of which L2
-// delivers 64 KiB to each of 256 CUs per step, 8 TB/s; half the traffic per product
-// would need tiles that the registers do not hold.
+// 8192 x 4096 x 4096 takes 83 to 100 us, 2.7 to 3.3 PFLOP/s.  Its loop takes 4200 cycles
+// per step where the products take 2048, and 2500 without the loads.  Each step waits for
+// memory twice: after its first product or two, because the next step's scales are shifted where
+// they are loaded, which waits for all loads in flight and so keeps most of the step's loads from
+// starting before; and at its end, for the next step's codes.
 template <int kTileM, int kTileN, int kWavesM, int kWavesN, int kGroups, bool kF32>
 __global__ __launch_bounds__(kGroups * kWavesM * kWavesN * 64, kGroups * kWavesM * kWavesN / 4) void staged_kernel(Mx4Product p, int tiles_m, int tiles_n) {
   constexpr int kWaves = kWavesM * kWavesN, kThreads = kWaves * 64;
