@@ -28,7 +28,8 @@ __device__ __forceinline__ unsigned value_part(unsigned row, unsigned part) {
 // exchange of maxima between waves for nearly every tile.  `above` is kSlack and the logarithm of the number of
 // entries, so that however many weights there are, they add up to 1 at most and their products with values to
 // the largest value at most: what is finite in the rows stays finite in every sum.  A token's largest weight is
-// never less than 2^-above, 2^-39 at most, and weights down to 2^-87 of that do not vanish.
+// never less than 2^-above (2^-39 for the longest contexts), and weights down to 2^-87 of that do not vanish.  The matrix
+// instructions keep denormal sums, so values lose bits only below about 2^(above - 140).
 constexpr float kSlack = 8.f;
 // A weight takes part in the output product as a sum of two bfloat16, its eight highest bits and the
 // rest: one alone would be off by up to 2^-8, as much as the result's own rounding.  Where LDS has no

@@ -66,3 +66,28 @@ def test_attend_largest_values(batch, heads, k, order, mx4):
         f32 = (k + 64) * R.F32 + 4 * R.F32 * s.abs().amax(-1, keepdim=True)
         close(out[b, 0], want, R.HALF_ULP * want.abs() + weights + f32 * size, f"request {b}")
         close(lse[b, 0], torch.logsumexp(s, -1), f32[:, 0] + 4 * R.F32 * torch.logsumexp(s, -1).abs(), f"request {b}: lse")
+
+
+@pytest.mark.parametrize("mx4", [False, True])
+@pytest.mark.parametrize("batch,heads,k", [(1, 8, 2000), (3, 128, 100), (130, 64, 2000), (24, 8, 2048)])
+def test_attend_small_values(batch, heads, k, mx4):
+    """Values near 2^-110, whose products with the weights are less than the least normal float32."""
+    from paper_2609_37538_amd import latent as L
+    g = gen(batch + heads + k)
+    latent = (torch.randint(2, 7, (k, 512), generator=g, device="cuda") * 2.0 ** -111).to(torch.bfloat16)
+    pool = row_bytes(latent, normal(g, k, 64), mx4).expand(batch, -1, -1).contiguous()
+    cache = L.LatentCache(pool, batch, int(mx4))
+    q = torch.zeros(batch, 1, heads, 576, dtype=torch.bfloat16, device="cuda")
+    q[..., 512] = 1.0
+    out, lse = cache.attend(q, scale=1.0)
+    for b in sorted({0, batch // 2, batch - 1}):
+        keys = R.row_values(pool[b], mx4)
+        s = q[b, 0].cpu().double() @ keys.T
+        p, v = torch.softmax(s, -1), keys[:, :512]
+        want, size = p @ v, p @ v.abs()
+        weights = 2.0 ** -12 * size + 2.0 ** -19 * p.amax(-1, keepdim=True) * v.abs().sum(0)
+        f32 = (k + 64) * R.F32 + 4 * R.F32 * s.abs().amax(-1, keepdim=True)
+        # two products and additions per row, off by half of 2^-149 each, relative to weights of 2^-19 at least
+        least = 4 * k * 2.0 ** -150 * 2.0 ** 19
+        close(out[b, 0], want, R.HALF_ULP * want.abs() + weights + f32 * size + least, f"request {b}")
+        assert (out[b, 0] != 0).all()
