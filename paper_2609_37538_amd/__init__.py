@@ -4,7 +4,9 @@ The operator lives in the HIP library ``libavsg.so`` (C ABI in
 ``include/avsg.h``); :mod:`paper_2609_37538_amd.avsg` is its ctypes binding.
 :mod:`paper_2609_37538_amd.latent` binds the operators around it
 (``include/avsg_latent.h``): the cache of latent rows, the attention over the
-rows that a step placed, and the 4-bit microscaled form.
+rows that a step placed, and the 4-bit microscaled form; and
+:mod:`paper_2609_37538_amd.selection` what makes a step's selection
+(``include/avsg_select.h``): the cache of index keys and the scores over it.
 """
 from .avsg import (  # noqa: F401
     AVSG_GATHER_BALANCED, AVSG_GATHER_NONE, AVSG_GATHER_PIPELINED, AVSG_GATHER_POSITION,
@@ -20,6 +22,7 @@ from .latent import (  # noqa: F401
     AVSG_BF16, AVSG_F32, AVSG_ROPE_HALVES, AVSG_ROPE_PAIRS, AVSG_ROWS_BF16, AVSG_ROWS_MX4, LatentCache, Mx4,
     mx4_dequantize, mx4_matmul, mx4_quantize,
 )
+from .selection import KeyCache  # noqa: F401
 
 
 def build(verbose: bool = False) -> str:

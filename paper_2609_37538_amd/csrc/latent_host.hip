@@ -15,6 +15,10 @@ namespace {
 
 thread_local char g_error[256] = {0};
 
+}  // namespace
+
+namespace avsg {
+
 avsg_status fail(avsg_status s, const char* fmt, ...) {
   va_list ap;
   va_start(ap, fmt);
@@ -28,14 +32,7 @@ avsg_status launched(hipError_t e, const char* what) {
   return fail(AVSG_E_HIP, "%s: %s", what, hipGetErrorString(e));
 }
 
-bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
-// bfloat16 rows read or written 16 bytes at a time
-bool rows16(const void* p, int64_t stride) { return p && aligned(p, 16) && (stride & 7) == 0; }
-
-avsg_status view_of(const avsg_cache* c, CacheView* v) {
-  if (!c || !c->base) return fail(AVSG_E_INVAL, "null cache or cache base");
-  const size_t row = avsg_row_bytes(c->format);
-  if (row == 0) return fail(AVSG_E_INVAL, "unknown row format %d", c->format);
+avsg_status view_of(const avsg_cache* c, size_t row, int align, CacheView* v) {
   if (c->batch < 1 || c->pages_per_request < 1 || c->page_rows < 1 || c->pages < 1)
     return fail(AVSG_E_INVAL, "batch, pages, pages_per_request and page_rows must be positive");
   if (c->pages > INT32_MAX) return fail(AVSG_E_RANGE, "pages must be below 2^31");
@@ -44,8 +41,8 @@ avsg_status view_of(const avsg_cache* c, CacheView* v) {
     return fail(AVSG_E_NOTPOW2, "page_rows must be a power of two (or pages_per_request 1)");
   const int64_t capacity = static_cast<int64_t>(c->pages_per_request) * c->page_rows;
   if (capacity > INT32_MAX) return fail(AVSG_E_RANGE, "rows of a request must be below 2^31");
-  if (!aligned(c->base, 16) || (c->row_stride & 15) != 0 || (c->page_stride & 15) != 0)
-    return fail(AVSG_E_RANGE, "base, row_stride and page_stride must be multiples of 16 bytes");
+  if (!aligned(c->base, align) || (c->row_stride & (align - 1)) != 0 || (c->page_stride & (align - 1)) != 0)
+    return fail(AVSG_E_RANGE, "base, row_stride and page_stride must be multiples of %d bytes", align);
   if (c->row_stride < static_cast<int64_t>(row)) return fail(AVSG_E_RANGE, "row_stride is less than a row's %zu bytes", row);
   if (c->row_stride > INT64_MAX / c->page_rows || c->page_stride < c->row_stride * c->page_rows ||
       c->page_stride > INT64_MAX / c->pages)
@@ -68,6 +65,17 @@ avsg_status view_of(const avsg_cache* c, CacheView* v) {
     v->page_mask = c->page_rows - 1;
   }
   return AVSG_OK;
+}
+
+}  // namespace avsg
+
+namespace {
+
+avsg_status view_of(const avsg_cache* c, CacheView* v) {
+  if (!c || !c->base) return fail(AVSG_E_INVAL, "null cache or cache base");
+  const size_t row = avsg_row_bytes(c->format);
+  if (row == 0) return fail(AVSG_E_INVAL, "unknown row format %d", c->format);
+  return view_of(c, row, 16, v);
 }
 
 }  // namespace

@@ -7,6 +7,7 @@
 #include <stdint.h>
 
 #include "avsg_internal.h"
+#include "avsg_latent.h"
 
 namespace avsg {
 
@@ -183,6 +184,16 @@ struct Mx4Product {
   bool wide_stores;   // four neighbouring outputs can be stored at once
   int64_t out_stride, out_batch_stride;
 };
+
+// Host side, shared with the other operators around the step: the calling thread's error text, a
+// launch's status, alignments, and a cache's view (its format is not looked at: rows of `row` bytes,
+// addresses and strides in multiples of `align`).
+avsg_status fail(avsg_status s, const char* fmt, ...);
+avsg_status launched(hipError_t e, const char* what);
+inline bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+// bfloat16 rows read or written 16 bytes at a time
+inline bool rows16(const void* p, int64_t stride) { return p && aligned(p, 16) && (stride & 7) == 0; }
+avsg_status view_of(const avsg_cache* c, size_t row, int align, CacheView* v);
 
 // Lets a kernel have `bytes` of dynamic LDS, once on each GPU that is current in a call.
 template <auto kKernel>

@@ -1,0 +1,362 @@
+// Scores of the key cache's positions for a step's query tokens, and the best
+// of them.
+#include <algorithm>
+
+#include "select_internal.h"
+
+namespace avsg {
+namespace {
+
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x4_at_4 __attribute__((ext_vector_type(4), aligned(4)));
+
+constexpr int kWaves = 4;      // of a workgroup of scores
+constexpr int kTileKeys = 16;  // keys that a matrix instruction takes
+
+struct F64Pair {
+  double a, b;
+};
+// Exchanges the odd rows of sixteen lanes of a with the even rows of b, or (kHalf) a's upper half with b's lower one.
+template <bool kHalf>
+__device__ __forceinline__ F64Pair swap_rows(double a, double b) {
+  const uint64_t x = __builtin_bit_cast(uint64_t, a), y = __builtin_bit_cast(uint64_t, b);
+  uint32_t lo[2], hi[2];
+  if constexpr (kHalf) {
+    const auto l = __builtin_amdgcn_permlane32_swap(static_cast<uint32_t>(x), static_cast<uint32_t>(y), false, false);
+    const auto h = __builtin_amdgcn_permlane32_swap(static_cast<uint32_t>(x >> 32), static_cast<uint32_t>(y >> 32), false, false);
+    lo[0] = l[0], lo[1] = l[1], hi[0] = h[0], hi[1] = h[1];
+  } else {
+    const auto l = __builtin_amdgcn_permlane16_swap(static_cast<uint32_t>(x), static_cast<uint32_t>(y), false, false);
+    const auto h = __builtin_amdgcn_permlane16_swap(static_cast<uint32_t>(x >> 32), static_cast<uint32_t>(y >> 32), false, false);
+    lo[0] = l[0], lo[1] = l[1], hi[0] = h[0], hi[1] = h[1];
+  }
+  return {__builtin_bit_cast(double, static_cast<uint64_t>(hi[0]) << 32 | lo[0]),
+          __builtin_bit_cast(double, static_cast<uint64_t>(hi[1]) << 32 | lo[1])};
+}
+
+// Sums over the four rows of sixteen lanes; row i gets that of x[i % kTok].
+template <int kTok>
+__device__ __forceinline__ double row_sums(const double (&x)[kTok]) {
+  const F64Pair u = swap_rows<false>(x[0], x[kTok - 1]);
+  const double s = u.a + u.b;
+  const F64Pair v = swap_rows<true>(s, s);
+  return v.a + v.b;
+}
+
+// The largest over groups of 2^shift lanes (at most 16).
+__device__ __forceinline__ float group_max(float x, int shift) {
+  auto with = [&](auto other) { x = fmaxf(x, __builtin_bit_cast(float, other)); };
+  const auto bits = [&] { return __builtin_bit_cast(int, x); };
+  if (shift > 0) with(__builtin_amdgcn_update_dpp(0, bits(), 0xb1, 0xf, 0xf, true));    // lanes 1 0 3 2
+  if (shift > 1) with(__builtin_amdgcn_update_dpp(0, bits(), 0x4e, 0xf, 0xf, true));    // lanes 2 3 0 1
+  if (shift > 2) with(__builtin_amdgcn_update_dpp(0, bits(), 0x141, 0xf, 0xf, true));   // mirrored within eight
+  if (shift > 3) with(__builtin_amdgcn_update_dpp(0, bits(), 0x140, 0xf, 0xf, true));   // mirrored within sixteen
+  return x;
+}
+
+// A wave scores kTok tokens of a request against a run of keys, sixteen at a time.  The matrix instruction
+// (16 x 64 by 64 x 16, 8-bit) multiplies sixteen heads' queries with sixteen keys: lane l holds head, or
+// key, l % 16 and columns (l / 16) * 32 .. + 31 in two instructions, and gets the products of heads (l / 16) *
+// 4 .. + 3 with key l % 16.  The queries and their weights (in 64 bits) stay in registers.
+template <int kTiles, int kTok>
+__global__ __launch_bounds__(kWaves * 64) void score_kernel(SelectParams p, int run_tiles, int runs, int groups, int waves_on_tokens) {
+  const int lane = threadIdx.x & 63, l16 = lane & 15, quad = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int waves_on_keys = kWaves / waves_on_tokens, run_groups = (runs + waves_on_keys - 1) / waves_on_keys;
+  const int token_groups = (groups + waves_on_tokens - 1) / waves_on_tokens;
+  const int run = static_cast<int>(blockIdx.x % run_groups) * waves_on_keys + wave / waves_on_tokens;
+  const int rest = static_cast<int>(blockIdx.x / run_groups);
+  const int group = rest % token_groups * waves_on_tokens + wave % waves_on_tokens, r = p.r0 + rest / token_groups;
+  if (run >= runs || group >= groups) return;
+  int token[kTok], seen[kTok], most = 0;   // tokens past the last are its copies
+#pragma unroll
+  for (int t = 0; t < kTok; ++t) {
+    token[t] = p.g0 + min(group * kTok + t, p.tokens - 1);
+    seen[t] = seen_by(p, r, token[t]);
+    most = max(most, seen[t]);
+  }
+  const int first_key = run * run_tiles * kTileKeys;
+  const int tiles = min(run_tiles, (most - first_key + kTileKeys - 1) / kTileKeys);
+  if (first_key >= most) return;
+
+  i32x4 q[kTok][kTiles][2];
+  double weight[kTok][kTiles][4];
+#pragma unroll
+  for (int t = 0; t < kTok; ++t) {
+    const int64_t at = static_cast<int64_t>(r) * p.n_q + token[t];
+    const int8_t* from = p.q + at * p.q_token_stride + quad * 32;
+    const float* weights = p.weights + at * p.weight_stride;
+#pragma unroll
+    for (int x = 0; x < kTiles; ++x) {
+      const int8_t* row = from + min(x * 16 + l16, p.heads - 1) * p.q_head_stride;
+      q[t][x][0] = *reinterpret_cast<const i32x4*>(row);
+      q[t][x][1] = *reinterpret_cast<const i32x4*>(row + 16);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int h = x * 16 + quad * 4 + i;
+        const float w = weights[min(h, p.heads - 1)];
+        weight[t][x][i] = h < p.heads ? static_cast<double>(w) : 0.0;
+      }
+    }
+  }
+
+  struct Keys {
+    i32x4 codes[2];
+    float scale;
+  };
+  auto fetch = [&](int tile) {
+    Keys k{};
+    k.scale = __uint_as_float(0x7fc00000u);   // of rows that do not exist
+    const int key = first_key + tile * kTileKeys + l16;
+    const uint64_t row = key < most ? cache_row(p.cache, r, key) : 0;
+    if (row != 0) {
+      k.codes[0] = load_global<i32x4_at_4>(row + quad * 32);
+      k.codes[1] = load_global<i32x4_at_4>(row + quad * 32 + 16);
+      k.scale = load_global<float>(row + kKeyScaleAt);
+    }
+    return k;
+  };
+  const int mine = quad % kTok, my_seen = kTok > 1 && mine ? seen[kTok - 1] : seen[0];
+  const int shift = p.block_shift, in_token = group * kTok + mine;
+  const bool stores = quad < kTok && in_token < p.tokens;
+  float* const out = p.scores + (static_cast<int64_t>(r - p.r0) * p.tokens + min(in_token, p.tokens - 1)) * p.score_stride;
+  float best = -__builtin_inff();   // of a block of more than sixteen positions
+  Keys keys = fetch(0);
+  for (int tile = 0; tile < tiles; ++tile) {
+    const Keys now = keys;
+    if (tile + 1 < tiles) keys = fetch(tile + 1);
+    double sum[kTok] = {};
+#pragma unroll
+    for (int x = 0; x < kTiles; ++x)
+#pragma unroll
+      for (int t = 0; t < kTok; ++t) {
+        i32x4 dot = __builtin_amdgcn_mfma_i32_16x16x64_i8(q[t][x][0], now.codes[0], i32x4{}, 0, 0, 0);
+        dot = __builtin_amdgcn_mfma_i32_16x16x64_i8(q[t][x][1], now.codes[1], dot, 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[t] = __builtin_fma(weight[t][x][i], static_cast<double>(max(dot[i], 0)), sum[t]);
+      }
+    // (zeros of either sign are one)
+    float score = static_cast<float>(row_sums<kTok>(sum) * static_cast<double>(now.scale)) + 0.0f;
+    const int key = first_key + tile * kTileKeys + l16;
+    if (!(score == score)) score = -__builtin_inff();
+    if (key < p.first || key >= my_seen - p.recent) score = __builtin_inff();
+    if (key >= my_seen) score = -__builtin_inff();
+    score = group_max(score, shift);
+    if (shift <= 4) {
+      if (stores && (l16 & ((1 << shift) - 1)) == 0 && key < most) out[key >> shift] = score;
+    } else {
+      best = fmaxf(best, score);
+      if (((tile + 1) & ((1 << (shift - 4)) - 1)) == 0 || tile + 1 == tiles) {
+        if (stores && l16 == 0) out[key >> shift] = best;
+        best = -__builtin_inff();
+      }
+    }
+  }
+}
+
+// Bits that order as the floats do (none of which is NaN), and back.
+__device__ __forceinline__ uint32_t ordered(float x) {
+  const uint32_t u = __float_as_uint(x);
+  return u ^ (u >> 31 ? 0xffffffffu : 0x80000000u);
+}
+__device__ __forceinline__ float unordered(uint32_t u) { return __uint_as_float(u ^ (u >> 31 ? 0x80000000u : 0xffffffffu)); }
+constexpr uint32_t kLowest = 0x007fffffu;   // ordered(-inf)
+
+constexpr int kBins = 2048;
+
+// The best blocks of a token, one workgroup per token.  The threshold is found by histograms of the range
+// that holds it, 2048 bins each, which narrow it down until a bin holds one value or all that is
+// wanted; then the blocks above it, and the lowest of those at it, are written in their order.
+// kResident: the scores stay in registers, else every pass reads them again.
+template <int kThreads, int kPer, bool kResident>
+__global__ __launch_bounds__(kThreads) void best_kernel(SelectParams p) {
+  constexpr int kWavesHere = kThreads / 64, kChunk = kThreads * kPer, kCounts = kPer * kWavesHere;
+  static_assert(kCounts <= kThreads && kBins % kThreads == 0);
+  __shared__ uint32_t hist[kBins];
+  __shared__ uint32_t above_counts[kCounts], equal_counts[kCounts];
+  __shared__ uint32_t parts[3][kWavesHere];
+  __shared__ uint32_t found[3];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int r = p.r0 + static_cast<int>(blockIdx.x) / p.tokens, g = p.g0 + static_cast<int>(blockIdx.x) % p.tokens;
+  const int shift = p.block_shift, want = p.topk >> shift;
+  const uint32_t n = p.longest >> shift, seen = (static_cast<uint32_t>(seen_by(p, r, g)) + (1u << shift) - 1) >> shift;
+  const float* const scores = p.scores + static_cast<int64_t>(blockIdx.x) * p.score_stride;
+  const int chunks = kResident ? 1 : static_cast<int>((n + kChunk - 1) / kChunk);
+  auto load = [&](int chunk, int j) {
+    const uint32_t i = static_cast<uint32_t>(chunk) * kChunk + j * kThreads + tid;
+    return i < seen ? ordered(scores[i]) : i < n ? kLowest : 0u;
+  };
+  uint32_t held[kPer];
+  if constexpr (kResident) {
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) held[j] = load(0, j);
+  }
+  auto each = [&](auto f) {
+    for (int chunk = 0; chunk < chunks; ++chunk)
+#pragma unroll
+      for (int j = 0; j < kPer; ++j) f(kResident ? held[j] : load(chunk, j));
+  };
+
+  // range and number of the scores above minus infinity
+  uint32_t lo = 0xffffffffu, hi = 0, count = 0;
+  each([&](uint32_t k) {
+    if (k > kLowest) lo = min(lo, k), hi = max(hi, k), ++count;
+  });
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) {
+    lo = min(lo, static_cast<uint32_t>(__shfl_xor(static_cast<int>(lo), d)));
+    hi = max(hi, static_cast<uint32_t>(__shfl_xor(static_cast<int>(hi), d)));
+    count += static_cast<uint32_t>(__shfl_xor(static_cast<int>(count), d));
+  }
+  if (lane == 0) parts[0][wave] = lo, parts[1][wave] = hi, parts[2][wave] = count;
+  __syncthreads();
+  lo = 0xffffffffu, hi = 0, count = 0;
+#pragma unroll
+  for (int w = 0; w < kWavesHere; ++w) lo = min(lo, parts[0][w]), hi = max(hi, parts[1][w]), count += parts[2][w];
+
+  // prefix sums over the workgroup of a value per thread, without its own; parts[0] is free between calls
+  auto before_me = [&](uint32_t x) {
+    const uint32_t with_me = wave_inclusive_scan(x);
+    __syncthreads();
+    if (lane == 63) parts[0][wave] = with_me;
+    __syncthreads();
+    uint32_t before = with_me - x;
+    for (int w = 0; w < wave; ++w) before += parts[0][w];
+    return before;
+  };
+
+  uint32_t threshold = kLowest, need = 0;   // taken: all above the threshold, and the first `need` at it
+  if (count <= static_cast<uint32_t>(want)) {
+    need = want - count;
+  } else {
+    need = want;
+    for (;;) {
+      const uint32_t span = hi - lo;
+      const int low_bits = max(0, 32 - 11 - (span ? __builtin_clz(span) : 32));
+      __syncthreads();
+#pragma unroll
+      for (int b = 0; b < kBins / kThreads; ++b) hist[b * kThreads + tid] = 0;
+      __syncthreads();
+      each([&](uint32_t k) {
+        if (k < lo || k > hi) return;
+        const uint32_t bin = (hi - k) >> low_bits;   // the largest scores in the first bins
+        // (many equal scores would queue up at one address)
+        const uint32_t one = __builtin_amdgcn_readfirstlane(bin);
+        const uint64_t all = __ballot(true), same = __ballot(bin == one);
+        if (all == same) {
+          if (lane == __builtin_ctzll(all)) atomicAdd(&hist[one], static_cast<uint32_t>(__popcll(all)));
+        } else {
+          atomicAdd(&hist[bin], 1u);
+        }
+      });
+      __syncthreads();
+      constexpr int kMine = kBins / kThreads;
+      uint32_t bins[kMine], mine = 0;
+#pragma unroll
+      for (int b = 0; b < kMine; ++b) bins[b] = hist[tid * kMine + b], mine += bins[b];
+      uint32_t before = before_me(mine);
+#pragma unroll
+      for (int b = 0; b < kMine; ++b) {
+        if (before < need && need <= before + bins[b]) found[0] = tid * kMine + b, found[1] = before, found[2] = bins[b];
+        before += bins[b];
+      }
+      __syncthreads();
+      const uint32_t top = hi - (found[0] << low_bits), size = (1u << low_bits) - 1;
+      need -= found[1];
+      lo = top - lo > size ? top - size : lo;
+      hi = top;
+      if (need == found[2]) {   // all that is left of the bin
+        threshold = lo - 1, need = 0;
+        break;
+      }
+      if (lo == hi) {
+        threshold = lo;
+        break;
+      }
+    }
+  }
+
+  const int64_t token = static_cast<int64_t>(r) * p.n_q + g;
+  int32_t* const index = p.index + token * p.topk;
+  float* const out = p.out_scores ? p.out_scores + token * want : nullptr;
+  uint32_t above_base = 0, equal_base = 0;
+  for (int chunk = 0; chunk < chunks; ++chunk) {
+    if (chunk > 0) __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      const uint32_t k = kResident ? held[j] : load(chunk, j);
+      const uint64_t above = __ballot(k > threshold), equal = __ballot(k == threshold);
+      if (lane == 0) above_counts[j * kWavesHere + wave] = __popcll(above), equal_counts[j * kWavesHere + wave] = __popcll(equal);
+    }
+    __syncthreads();
+    const uint32_t above_here = tid < kCounts ? above_counts[tid] : 0, equal_here = tid < kCounts ? equal_counts[tid] : 0;
+    const uint32_t above_before = before_me(above_here), equal_before = before_me(equal_here);
+    if (tid < kCounts) above_counts[tid] = above_base + above_before, equal_counts[tid] = equal_base + equal_before;
+    if (tid == kThreads - 1) found[0] = above_base + above_before + above_here, found[1] = equal_base + equal_before + equal_here;
+    __syncthreads();
+    above_base = found[0], equal_base = found[1];
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      const uint32_t k = kResident ? held[j] : load(chunk, j);
+      const uint32_t above_at = above_counts[j * kWavesHere + wave], equal_at = equal_counts[j * kWavesHere + wave];
+      const uint64_t lower = (uint64_t{1} << lane) - 1;
+      const uint64_t equal = __ballot(k == threshold);
+      const bool taken = k > threshold || (k == threshold && equal_at + __popcll(equal & lower) < need);
+      const uint64_t all = __ballot(taken);
+      if (taken) {
+        const uint32_t at = above_at + min(equal_at, need) + __popcll(all & lower);
+        const int block = chunk * kChunk + j * kThreads + tid;
+        for (int i = 0; i < 1 << shift; ++i) index[(static_cast<int64_t>(at) << shift) + i] = (block << shift) + i;
+        if (out) out[at] = unordered(k);
+      }
+    }
+  }
+}
+
+template <int kTiles, int kTok>
+hipError_t run_scores(const SelectParams& p, hipStream_t s) {
+  const int groups = (p.tokens + kTok - 1) / kTok;
+  const int waves_on_tokens = groups >= kWaves ? kWaves : 1;
+  const int64_t tiles = (static_cast<int64_t>(p.longest) + kTileKeys - 1) / kTileKeys;
+  // runs in eights of tiles, the largest block
+  const int64_t waves = 2048, per_group = std::max<int64_t>(1, waves / (static_cast<int64_t>(p.requests) * groups));
+  int64_t run_tiles = std::max<int64_t>(8, (tiles + per_group - 1) / per_group);
+  run_tiles = std::min<int64_t>(64, (run_tiles + 7) / 8 * 8);
+  const int64_t runs = (tiles + run_tiles - 1) / run_tiles;
+  const int64_t run_groups = (runs * waves_on_tokens + kWaves - 1) / kWaves, token_groups = (groups + waves_on_tokens - 1) / waves_on_tokens;
+  const int64_t total = run_groups * token_groups * p.requests;
+  score_kernel<kTiles, kTok><<<dim3(static_cast<unsigned>(total)), kWaves * 64, 0, s>>>(
+      p, static_cast<int>(run_tiles), static_cast<int>(runs), groups, waves_on_tokens);
+  return hipGetLastError();
+}
+
+template <int kThreads, int kPer, bool kResident>
+hipError_t run_best(const SelectParams& p, hipStream_t s) {
+  best_kernel<kThreads, kPer, kResident><<<dim3(static_cast<unsigned>(p.requests) * p.tokens), kThreads, 0, s>>>(p);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_scores(const SelectParams& p, hipStream_t s) {
+  const int tiles = (p.heads + 15) / 16;
+  if (tiles > 4) return run_scores<8, 1>(p, s);
+  if (p.tokens == 1) {
+    if (tiles == 1) return run_scores<1, 1>(p, s);
+    if (tiles == 2) return run_scores<2, 1>(p, s);
+    return run_scores<4, 1>(p, s);
+  }
+  if (tiles == 1) return run_scores<1, 2>(p, s);
+  if (tiles == 2) return run_scores<2, 2>(p, s);
+  return run_scores<4, 2>(p, s);
+}
+
+hipError_t launch_best(const SelectParams& p, hipStream_t s) {
+  const int n = p.longest >> p.block_shift;
+  if (n <= 2048) return run_best<256, 8, true>(p, s);
+  if (n <= 16384) return run_best<512, 32, true>(p, s);
+  if (n <= 65536) return run_best<1024, 64, true>(p, s);
+  return run_best<1024, 64, false>(p, s);
+}
+
+}  // namespace avsg

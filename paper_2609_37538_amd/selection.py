@@ -1,0 +1,277 @@
+"""ctypes binding of what makes a step's selection (include/avsg_select.h): the
+same entry points, argument marshalling only, and :class:`KeyCache`, which takes
+torch tensors.
+
+A :class:`KeyCache` describes rows of 8-bit index keys (a paged pool, the second
+buffers of an :class:`~paper_2609_37538_amd.avsg.Operator`, or host rows); it
+appends to them, reads them back, and selects the positions that an operator's
+step and :meth:`~paper_2609_37538_amd.latent.LatentCache.attend` take.  The methods
+run on the current stream of their tensors' GPU and raise ValueError for tensors
+the kernels do not take.  There is no backward pass: with gradients enabled they
+raise ValueError for tensors that require one.
+"""
+from __future__ import annotations
+
+import ctypes
+from typing import Optional, Tuple
+
+from . import latent as _L
+from .avsg import _P, _vp
+from .latent import AVSG_ROPE_PAIRS, _check, _i32, _i64, _need, _sz
+
+AVSG_KEY_DIM = 128
+AVSG_KEY_ROW_BYTES = 132
+AVSG_SELECT_HEADS_MOST = 128
+
+
+class AvsgKeyCache(ctypes.Structure):
+    _fields_ = [("base", _P), ("pages", _i64), ("page_stride", _i64), ("row_stride", _i64), ("batch", _i32),
+                ("page_rows", _i32), ("pages_per_request", _i32), ("d_page_table", _P)]
+
+
+class AvsgKeyAppend(ctypes.Structure):
+    _fields_ = [("tokens", _i64), ("d_key", _P), ("key_stride", _i64), ("d_request", _P), ("d_position", _P),
+                ("d_angles", _P), ("positions", _i64), ("rope_style", _i32), ("rope_at", _i32), ("heads", _i32), ("d_q", _P),
+                ("q_token_stride", _i64), ("q_head_stride", _i64), ("d_weights", _P), ("weight_stride", _i64), ("d_q_out", _P),
+                ("q_out_token_stride", _i64), ("q_out_head_stride", _i64), ("d_weights_out", _P), ("weight_out_stride", _i64)]
+
+
+class AvsgSelection(ctypes.Structure):
+    _fields_ = [("n_q", _i32), ("heads", _i32), ("longest", _i32), ("topk", _i32), ("block", _i32), ("first", _i32),
+                ("recent", _i32), ("d_q", _P), ("q_token_stride", _i64), ("q_head_stride", _i64), ("d_weights", _P),
+                ("weight_stride", _i64), ("d_lens", _P), ("d_index", _P), ("d_scores", _P)]
+
+
+_lib = None
+
+
+def load():
+    """The library with the signatures of this module's entry points."""
+    global _lib
+    if _lib is not None:
+        return _lib
+    lib = _L.load()
+    ptr = ctypes.POINTER
+    for name, restype, args in (
+            ("avsg_key_append_rows", _i32, [ptr(AvsgKeyCache), ptr(AvsgKeyAppend), _P]),
+            ("avsg_key_read_rows", _i32, [ptr(AvsgKeyCache), _i64, _P, _P, _P, _i64, _P]),
+            ("avsg_select_workspace_bytes", _sz, [_i32, _i32, _i32, _i32]),
+            ("avsg_select_workspace_least", _sz, [_i32, _i32]),
+            ("avsg_select", _i32, [ptr(AvsgKeyCache), ptr(AvsgSelection), _P, _sz, _P])):
+        f = getattr(lib, name)
+        f.restype, f.argtypes = restype, args
+    _lib = lib
+    return lib
+
+
+# ---------------------------------------------------------------------------
+# entry points, same names as the C ABI
+# ---------------------------------------------------------------------------
+def avsg_key_append_rows(cache: AvsgKeyCache, append: AvsgKeyAppend, stream: int = 0) -> None:
+    _check(load().avsg_key_append_rows(cache, append, _vp(stream)), "avsg_key_append_rows")
+
+
+def avsg_key_read_rows(cache: AvsgKeyCache, n: int, d_request: int, d_position: int, d_out: int, out_stride: int,
+                       stream: int = 0) -> None:
+    _check(load().avsg_key_read_rows(cache, n, _vp(d_request), _vp(d_position), _vp(d_out), out_stride, _vp(stream)),
+           "avsg_key_read_rows")
+
+
+def avsg_select_workspace_bytes(batch: int, n_q: int, longest: int, block: int) -> int:
+    return int(load().avsg_select_workspace_bytes(batch, n_q, longest, block))
+
+
+def avsg_select_workspace_least(longest: int, block: int) -> int:
+    return int(load().avsg_select_workspace_least(longest, block))
+
+
+def avsg_select(cache: AvsgKeyCache, selection: AvsgSelection, d_workspace: Optional[int], workspace_bytes: int,
+                stream: int = 0) -> None:
+    _check(load().avsg_select(cache, selection, _vp(d_workspace), workspace_bytes, _vp(stream)), "avsg_select")
+
+
+# ---------------------------------------------------------------------------
+# wrapper
+# ---------------------------------------------------------------------------
+def _torch():
+    torch = _L._torch()
+    load()
+    return torch
+
+
+def _codes(x, shape, device, what):
+    """(address, token stride, head stride) of int8 [...][128] codes, whose vectors are read 16 bytes at a time."""
+    if x.dtype is not _L._t.int8 or x.shape != shape or x.device != device:
+        raise ValueError(f"{what} must be an int8 tensor of shape {tuple(shape)} on {device}")
+    return _strided(x, 15, what)
+
+
+def _strided(x, mask, what):
+    """(address, stride of the tokens, ...) of a tensor whose last dimension is contiguous; its leading dimensions but the
+    last one, [B][n_q] or [T], are tokens at equal distances.  `mask`: of strides and, in bytes, of the address."""
+    at, shape = x.data_ptr(), x.shape
+    st = [0 if n <= 1 else s for s, n in zip(x.stride(), shape)]     # strides of dimensions of one entry do not matter
+    if 0 in shape:
+        return at, 0, 0
+    if len(shape) == 4:
+        if shape[1] == 1:
+            st[1] = st[0]
+        elif shape[0] > 1 and st[0] != shape[1] * st[1]:
+            raise ValueError(f"{what}: tokens must lie at equal distances")
+        st = st[1:]
+    if (shape[-1] > 1 and st[-1] != 1) or any(s & mask for s in st[:-1]) or at & 15:
+        raise ValueError(f"{what}: vectors must be contiguous and 16-byte aligned")
+    return at, st[0], st[1]
+
+
+def _weights(x, shape, device, what):
+    """(address, token stride) of float32 [...][H] weights."""
+    if x.requires_grad:
+        _L._no_gradient(what)
+    if x.dtype is not _L._t.float32 or x.shape != shape or x.device != device:
+        raise ValueError(f"{what} must be a float32 tensor of shape {tuple(shape)} on {device}")
+    st = [0 if n <= 1 else s for s, n in zip(x.stride(), shape)]
+    if 0 in shape:
+        return x.data_ptr(), 0
+    if len(shape) == 3:
+        if shape[1] == 1:
+            st[1] = st[0]
+        elif shape[0] > 1 and st[0] != shape[1] * st[1]:
+            raise ValueError(f"{what}: tokens must lie at equal distances")
+        st = st[1:]
+    if shape[-1] > 1 and st[-1] != 1:
+        raise ValueError(f"{what}: a token's weights must be contiguous")
+    return x.data_ptr(), st[0]
+
+
+class KeyCache:
+    """Index-key rows of `batch` requests.
+
+    pool: uint8 cuda tensor [pages][page_rows][132], the bytes of a row contiguous (rows
+        and pages may lie further apart); an `Operator`'s `buffers[1]` is such a pool.
+    page_table: int32 cuda tensor [batch][pages per request] of page numbers, or
+        None: the pool holds batch equal runs of pages.
+    base: device address to use in place of the pool's (for pinned host rows:
+        pass pages, page_rows and device with it, and no pool).
+    """
+
+    def __init__(self, pool, batch: int, page_table=None, *, base: int = 0, pages: int = 0, page_rows: int = 0,
+                 device=None):
+        torch = _torch()
+        _need(batch >= 1, "batch must be positive")
+        self.batch, self.pool, self.page_table = batch, pool, page_table
+        row = AVSG_KEY_ROW_BYTES
+        if pool is not None:
+            _need(pool.dtype == torch.uint8 and pool.is_cuda and pool.dim() == 3 and pool.shape[2] == row
+                  and pool.stride(2) == 1, f"pool must be a cuda uint8 tensor [pages][page_rows][{row}]")
+            self.device = pool.device
+            pages, page_rows, base = pool.shape[0], pool.shape[1], pool.data_ptr()
+            row_stride = pool.stride(1) if page_rows > 1 else row
+            page_stride = pool.stride(0) if pages > 1 else row_stride * page_rows
+        else:
+            _need(base != 0 and pages > 0 and page_rows > 0, "without a pool, base, pages and page_rows are needed")
+            self.device = torch.device(device or "cuda")
+            if self.device.index is None:
+                self.device = torch.device("cuda", torch.cuda.current_device())
+            row_stride, page_stride = row, row * page_rows
+        table = None
+        if page_table is not None:
+            _need(page_table.dim() == 2, "page_table must be [batch][pages per request]")
+            per = page_table.shape[1]
+            table = _L._ints(page_table, torch.int32, (batch, per), self.device, "page_table")
+        else:
+            _need(pages % batch == 0, "without a page table the pool must hold batch equal runs of pages")
+            per = pages // batch
+        self.rows_per_request = per * page_rows
+        self.c = AvsgKeyCache(base, pages, page_stride, row_stride, batch, page_rows, per, table)
+        self._workspace = (None, 0)     # the last call's (n_q, longest, block), and its bytes
+
+    def append(self, key, request, position, angles=None, *, style: int = AVSG_ROPE_PAIRS, rope_at: int = 0, q=None,
+               weights=None, q_out=None, weights_out=None) -> None:
+        """Rotate 64 of the columns of `key` [T][128] (from rope_at, 0 or 64; with angles=None none) by the
+        tokens' positions, quantise and write the rows (request [T] int32, position [T] int64).
+        angles: float32 [positions][32][2], cosine and sine.  q [T][H][128], treated alike, goes to q_out
+        (int8 [T][H][128]), and weights [T][H] (float32, None: ones) times the queries' scales to weights_out."""
+        t, dev = key.shape[0], self.device
+        torch = _L._t
+        ka, ks = _L._vectors(key, (t, AVSG_KEY_DIM), dev, "key")
+        req = _L._ints(request, torch.int32, (t,), dev, "request")
+        pos = _L._ints(position, torch.int64, (t,), dev, "position")
+        if angles is None:
+            ang, turns, rope_at = None, 0, -1
+        else:
+            turns = angles.shape[0]
+            ang = _L._ints(angles, torch.float32, (turns, 32, 2), dev, "angles")
+            _need(rope_at in (0, 64), "rope_at must be 0 or 64")
+        if q is None:
+            _need(weights is None and q_out is None and weights_out is None, "q, q_out and weights_out go together")
+            a = AvsgKeyAppend(t, ka, ks[0], req, pos, ang, turns, style, rope_at)
+        else:
+            _need(q_out is not None and weights_out is not None and q.dim() == 3, "q [T][H][128], q_out and weights_out go together")
+            shape = (t, q.shape[1], AVSG_KEY_DIM)
+            qa, qs = _L._vectors(q, shape, dev, "q")
+            wa, ws = (None, 0) if weights is None else _weights(weights, shape[:2], dev, "weights")
+            oa, ot, oh = _codes(q_out, shape, dev, "q_out")
+            va, vs = _weights(weights_out, shape[:2], dev, "weights_out")
+            a = AvsgKeyAppend(t, ka, ks[0], req, pos, ang, turns, style, rope_at, shape[1], qa, qs[0], qs[1], wa, ws, oa, ot, oh,
+                              va, vs)
+        _L._run(_lib.avsg_key_append_rows, "avsg_key_append_rows", dev.index, self.c, a)
+
+    def read(self, request, position, out=None):
+        """Rows as bfloat16 [n][128]; rows that do not exist read as zeros."""
+        n, dev = request.shape[0], self.device
+        req = _L._ints(request, _L._t.int32, (n,), dev, "request")
+        pos = _L._ints(position, _L._t.int64, (n,), dev, "position")
+        if out is None:
+            out = _L._t.empty((n, AVSG_KEY_DIM), dtype=_L._t.bfloat16, device=dev)
+        at, st = _L._vectors(out, (n, AVSG_KEY_DIM), dev, "out")
+        _L._run(_lib.avsg_key_read_rows, "avsg_key_read_rows", dev.index, self.c, n, req, pos, at, st[0])
+        return out
+
+    def select(self, q, weights, *, topk: int, block: int = 1, lens=None, longest: Optional[int] = None, first: int = 0,
+               recent: int = 0, index=None, scores=None, workspace=None) -> Tuple:
+        """(index [B][n_q][topk] int32, scores [B][n_q][topk / block] float32): the positions, ascending, of the
+        topk / block best blocks of `block` neighbouring positions for each query token, and the blocks'
+        scores.
+
+        q: int8 [B][n_q][H][128] codes, weights: float32 [B][n_q][H] (append's q_out and weights_out).
+        lens: int64 [B][n_q] positions a query token may see, or None: all.
+        longest: positions [0, longest) are ranked, None: all rows of a request.
+        first, recent: positions [0, first) and [len - recent, len) that are always taken.
+        workspace: uint8 tensor to use in place of a new one (at least avsg_select_workspace_least)."""
+        dev, torch = self.device, _L._t
+        _need(q.dim() == 4, "q must be [batch][n_q][heads][128]")
+        b, n_q, heads, _ = q.shape
+        if b != self.batch or n_q < 1 or heads < 1:
+            raise ValueError(f"q must hold {self.batch} requests, and a token and a head")
+        longest = self.rows_per_request if longest is None else longest
+        _need(0 <= topk <= 0x7fffffff and 0 <= longest <= 0x7fffffff and 1 <= block <= 128,
+              "topk and longest must be counts below 2^31, block from 1 to 128")
+        _need(0 <= first <= 0x7fffffff and 0 <= recent <= 0x7fffffff, "first and recent must be counts below 2^31")
+        _need(topk % block == 0, "topk must be a multiple of block")
+        qa, qt, qh = _codes(q, (b, n_q, heads, AVSG_KEY_DIM), dev, "q")
+        wa, ws = _weights(weights, (b, n_q, heads), dev, "weights")
+        lens_at = None if lens is None else _L._ints(lens, torch.int64, (b, n_q), dev, "lens")
+        if index is None:
+            index = torch.empty((b, n_q, topk), dtype=torch.int32, device=dev)
+            index_at = index.data_ptr()
+        else:
+            index_at = _L._ints(index, torch.int32, (b, n_q, topk), dev, "index")
+        if scores is None:
+            scores = torch.empty((b, n_q, topk // block), dtype=torch.float32, device=dev)
+            scores_at = scores.data_ptr()
+        else:
+            scores_at = _L._ints(scores, torch.float32, (b, n_q, topk // block), dev, "scores")
+        if workspace is None:
+            last, need = self._workspace
+            if last != (n_q, longest, block):
+                need = avsg_select_workspace_bytes(b, n_q, longest, block)
+                self._workspace = ((n_q, longest, block), need)
+            workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+        else:
+            _need(workspace.dtype is torch.uint8 and workspace.device == dev and workspace.is_contiguous(),
+                  f"workspace must be a contiguous uint8 tensor on {dev}")
+            need = workspace.numel()
+        a = AvsgSelection(n_q, heads, longest, topk, block, first, recent, qa, qt, qh, wa, ws, lens_at, index_at, scores_at)
+        _L._run(_lib.avsg_select, "avsg_select", dev.index, self.c, a, workspace.data_ptr() if need else None, need)
+        return index, scores
