@@ -34,12 +34,18 @@ __device__ __forceinline__ F64Pair swap_rows(double a, double b) {
           __builtin_bit_cast(double, static_cast<uint64_t>(hi[1]) << 32 | lo[1])};
 }
 
-// Sums over the four rows of sixteen lanes; row i gets that of x[i % kTok].
-template <int kTok>
-__device__ __forceinline__ double row_sums(const double (&x)[kTok]) {
-  const F64Pair u = swap_rows<false>(x[0], x[kTok - 1]);
-  const double s = u.a + u.b;
-  const F64Pair v = swap_rows<true>(s, s);
+// Sums over the four rows of sixteen lanes; row i gets that of x[i % kCount].
+template <int kCount>
+__device__ __forceinline__ double row_sums(const double (&x)[kCount]) {
+  static_assert(kCount == 2 || kCount == 4);
+  const F64Pair u = swap_rows<false>(x[0], x[1]);
+  const double s = u.a + u.b;   // rows 0 and 2: halves of x[0], rows 1 and 3 of x[1]
+  double t = s;
+  if constexpr (kCount == 4) {
+    const F64Pair w = swap_rows<false>(x[2], x[3]);
+    t = w.a + w.b;
+  }
+  const F64Pair v = swap_rows<true>(s, t);
   return v.a + v.b;
 }
 
@@ -58,8 +64,9 @@ __device__ __forceinline__ float group_max(float x, int shift) {
 // (16 x 64 by 64 x 16, 8-bit) multiplies sixteen heads' queries with sixteen keys: lane l holds head, or
 // key, l % 16 and columns (l / 16) * 32 .. + 31 in two instructions, and gets the products of heads (l / 16) *
 // 4 .. + 3 with key l % 16.  The queries and their weights (in 64 bits) stay in registers.
-template <int kTiles, int kTok>
-__global__ __launch_bounds__(kWaves * 64) void score_kernel(SelectParams p, int run_tiles, int runs, int groups, int waves_on_tokens) {
+// kWhole: a tile's keys lie in one page.
+template <int kTiles, int kTok, bool kWhole>
+__global__ __launch_bounds__(kWaves * 64, 2) void score_kernel(SelectParams p, int run_tiles, int runs, int groups, int waves_on_tokens) {
   const int lane = threadIdx.x & 63, l16 = lane & 15, quad = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int waves_on_keys = kWaves / waves_on_tokens, run_groups = (runs + waves_on_keys - 1) / waves_on_keys;
@@ -103,54 +110,89 @@ __global__ __launch_bounds__(kWaves * 64) void score_kernel(SelectParams p, int 
   struct Keys {
     i32x4 codes[2];
     float scale;
+    bool there;   // or it is not the row's
   };
+  // A run has at most 64 tiles: where a tile lies in one page, lane l holds the page of tile l.
+  const int64_t first_page = static_cast<int64_t>(r) * p.cache.pages_per_request;
+  auto page_of = [&](int key) {
+    const int64_t at = first_page + (key >> p.cache.page_shift);
+    const int page = p.cache.table ? p.cache.table[at] : static_cast<int>(at);
+    return page < p.cache.pages ? page : -1;
+  };
+  const int pages = kWhole ? page_of(min(first_key + lane * kTileKeys, most - 1)) : 0;
+  const int64_t in_row = quad * 32, to_scale = kKeyScaleAt - quad * 32;
+  // (No branch: a wave that may skip a load has to wait for all of them;
+  // and nothing is done with a loaded value here, which would wait for it.  Keys past the last one that is seen read as
+  // it; in place of rows that do not exist the pool's first one is read.)
   auto fetch = [&](int tile) {
-    Keys k{};
-    k.scale = __uint_as_float(0x7fc00000u);   // of rows that do not exist
-    const int key = first_key + tile * kTileKeys + l16;
-    const uint64_t row = key < most ? cache_row(p.cache, r, key) : 0;
-    if (row != 0) {
-      k.codes[0] = load_global<i32x4_at_4>(row + quad * 32);
-      k.codes[1] = load_global<i32x4_at_4>(row + quad * 32 + 16);
-      k.scale = load_global<float>(row + kKeyScaleAt);
-    }
+    Keys k;
+    const int key = min(first_key + tile * kTileKeys + l16, most - 1);
+    const int page = kWhole ? __builtin_amdgcn_readlane(pages, min(tile, tiles - 1)) : page_of(key);
+    const bool there = page >= 0;
+    uint64_t row = p.cache.base + (there ? page * p.cache.page_stride : 0);
+    row += (there ? key & p.cache.page_mask : 0) * p.cache.row_stride + in_row;
+    k.codes[0] = load_global<i32x4_at_4>(row);
+    k.codes[1] = load_global<i32x4_at_4>(row + 16);
+    k.scale = load_global<float>(row + to_scale);
+    k.there = there;
     return k;
   };
-  const int mine = quad % kTok, my_seen = kTok > 1 && mine ? seen[kTok - 1] : seen[0];
+  // Of a pair of tiles, the lanes of row i of sixteen end up with token i % kTok and tile i / kTok % 2.
+  const int mine = quad % kTok, my_tile = quad / kTok & 1, my_seen = kTok > 1 && mine ? seen[kTok - 1] : seen[0];
   const int shift = p.block_shift, in_token = group * kTok + mine;
-  const bool stores = quad < kTok && in_token < p.tokens;
+  const bool stores = quad < 2 * kTok && in_token < p.tokens;
   float* const out = p.scores + (static_cast<int64_t>(r - p.r0) * p.tokens + min(in_token, p.tokens - 1)) * p.score_stride;
   float best = -__builtin_inff();   // of a block of more than sixteen positions
-  Keys keys = fetch(0);
-  for (int tile = 0; tile < tiles; ++tile) {
-    const Keys now = keys;
-    if (tile + 1 < tiles) keys = fetch(tile + 1);
-    double sum[kTok] = {};
+  auto meet = [&](const Keys (&pair)[2], int tile) {
+    double sum[2 * kTok];
 #pragma unroll
-    for (int x = 0; x < kTiles; ++x)
+    for (int u = 0; u < 2; ++u)
 #pragma unroll
       for (int t = 0; t < kTok; ++t) {
-        i32x4 dot = __builtin_amdgcn_mfma_i32_16x16x64_i8(q[t][x][0], now.codes[0], i32x4{}, 0, 0, 0);
-        dot = __builtin_amdgcn_mfma_i32_16x16x64_i8(q[t][x][1], now.codes[1], dot, 0, 0, 0);
+        i32x4 dot[kTiles];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sum[t] = __builtin_fma(weight[t][x][i], static_cast<double>(max(dot[i], 0)), sum[t]);
+        for (int x = 0; x < kTiles; ++x) dot[x] = __builtin_amdgcn_mfma_i32_16x16x64_i8(q[t][x][0], pair[u].codes[0], i32x4{}, 0, 0, 0);
+#pragma unroll
+        for (int x = 0; x < kTiles; ++x) dot[x] = __builtin_amdgcn_mfma_i32_16x16x64_i8(q[t][x][1], pair[u].codes[1], dot[x], 0, 0, 0);
+        double& s = sum[u * kTok + t];
+        s = 0.0;
+#pragma unroll
+        for (int x = 0; x < kTiles; ++x)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s = __builtin_fma(weight[t][x][i], static_cast<double>(max(dot[x][i], 0)), s);
       }
+    const float scale = my_tile ? pair[1].scale : pair[0].scale;
+    const bool there = my_tile ? pair[1].there : pair[0].there;
     // (zeros of either sign are one)
-    float score = static_cast<float>(row_sums<kTok>(sum) * static_cast<double>(now.scale)) + 0.0f;
-    const int key = first_key + tile * kTileKeys + l16;
-    if (!(score == score)) score = -__builtin_inff();
+    float score = static_cast<float>(row_sums<2 * kTok>(sum) * static_cast<double>(scale)) + 0.0f;
+    const int key = first_key + (tile + my_tile) * kTileKeys + l16;
+    if (!there || !(score == score)) score = -__builtin_inff();
     if (key < p.first || key >= my_seen - p.recent) score = __builtin_inff();
     if (key >= my_seen) score = -__builtin_inff();
+    if (shift == 0) {
+      if (stores && key < most) out[key] = score;
+      return;
+    }
     score = group_max(score, shift);
     if (shift <= 4) {
       if (stores && (l16 & ((1 << shift) - 1)) == 0 && key < most) out[key >> shift] = score;
     } else {
       best = fmaxf(best, score);
-      if (((tile + 1) & ((1 << (shift - 4)) - 1)) == 0 || tile + 1 == tiles) {
-        if (stores && l16 == 0) out[key >> shift] = best;
+      if (((tile + 2) & ((1 << (shift - 4)) - 1)) == 0 || tile + 2 >= tiles) {
+        best = fmaxf(best, __shfl_xor(best, 16 * kTok));
+        if (stores && my_tile == 0 && l16 == 0) out[key >> shift] = best;
         best = -__builtin_inff();
       }
     }
+  };
+  Keys one[2], two[2];
+  one[0] = fetch(0), one[1] = fetch(1), two[0] = fetch(2), two[1] = fetch(3);
+  for (int tile = 0; tile < tiles; tile += 4) {
+    meet(one, tile);
+    one[0] = fetch(tile + 4), one[1] = fetch(tile + 5);
+    if (tile + 2 >= tiles) break;
+    meet(two, tile + 2);
+    two[0] = fetch(tile + 6), two[1] = fetch(tile + 7);
   }
 }
 
@@ -160,27 +202,42 @@ __device__ __forceinline__ uint32_t ordered(float x) {
   return u ^ (u >> 31 ? 0xffffffffu : 0x80000000u);
 }
 __device__ __forceinline__ float unordered(uint32_t u) { return __uint_as_float(u ^ (u >> 31 ? 0x80000000u : 0xffffffffu)); }
-constexpr uint32_t kLowest = 0x007fffffu;   // ordered(-inf)
+constexpr uint32_t kLowest = 0x007fffffu, kHighest = 0xff800000u;   // ordered(-inf), ordered(inf)
 
 constexpr int kBins = 2048;
+constexpr int kFew = 512;   // scores of a bin that are compared with each other
 
-// The best blocks of a token, one workgroup per token.  The threshold is found by histograms of the range
-// that holds it, 2048 bins each, which narrow it down until a bin holds one value or all that is
-// wanted; then the blocks above it, and the lowest of those at it, are written in their order.
+// What a workgroup picks from: the scores of a token's blocks; those of a segment of them; or what the
+// segments' workgroups left, in the blocks' order.
+enum class From { kScores, kSegment, kSegments };
+
+// The best blocks of a token, one workgroup per token (or segment).  The threshold lies in one of 2048 bins of
+// equal width between the smallest and the largest finite score, the scores of that bin are compared
+// with each other, and the blocks above the threshold, and the lowest of those at it, are written in
+// their order.  Where the bin holds many, or the scores are too far apart for such bins, histograms of
+// their bits narrow the range down until a bin holds one value or all that is wanted.
 // kResident: the scores stay in registers, else every pass reads them again.
-template <int kThreads, int kPer, bool kResident>
+template <int kThreads, int kPer, bool kResident, From kFrom>
 __global__ __launch_bounds__(kThreads) void best_kernel(SelectParams p) {
   constexpr int kWavesHere = kThreads / 64, kChunk = kThreads * kPer, kCounts = kPer * kWavesHere;
-  static_assert(kCounts <= kThreads && kBins % kThreads == 0);
+  static_assert(kCounts <= kThreads && kBins % kThreads == 0 && kFew <= kBins);
   __shared__ uint32_t hist[kBins];
   __shared__ uint32_t above_counts[kCounts], equal_counts[kCounts];
-  __shared__ uint32_t parts[3][kWavesHere];
+  __shared__ uint32_t parts[4][kWavesHere];
   __shared__ uint32_t found[3];
+  __shared__ uint32_t few_count;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int r = p.r0 + static_cast<int>(blockIdx.x) / p.tokens, g = p.g0 + static_cast<int>(blockIdx.x) % p.tokens;
-  const int shift = p.block_shift, want = p.topk >> shift;
-  const uint32_t n = p.longest >> shift, seen = (static_cast<uint32_t>(seen_by(p, r, g)) + (1u << shift) - 1) >> shift;
-  const float* const scores = p.scores + static_cast<int64_t>(blockIdx.x) * p.score_stride;
+  const int row = kFrom == From::kSegment ? static_cast<int>(blockIdx.x) / p.segments : static_cast<int>(blockIdx.x);
+  const int r = p.r0 + row / p.tokens, g = p.g0 + row % p.tokens;
+  const int shift = p.block_shift, wanted = p.topk >> shift;   // of the token
+  const uint32_t blocks = p.longest >> shift;
+  const uint32_t first = kFrom == From::kSegment ? blockIdx.x % p.segments * p.segment : 0;
+  const uint32_t n = kFrom == From::kSegments ? static_cast<uint32_t>(p.candidates) : kFrom == From::kSegment ? min(blocks - first, p.segment) : blocks;
+  const uint32_t want = kFrom == From::kSegment ? min(n, static_cast<uint32_t>(wanted)) : wanted;
+  const uint32_t in_reach = (static_cast<uint32_t>(seen_by(p, r, g)) + (1u << shift) - 1) >> shift;
+  const uint32_t seen = kFrom == From::kSegments ? n : in_reach > first ? min(in_reach - first, n) : 0;
+  const float* const scores = kFrom == From::kSegments ? p.candidate_scores + static_cast<int64_t>(row) * p.candidates
+                                                       : p.scores + row * p.score_stride + first;
   const int chunks = kResident ? 1 : static_cast<int>((n + kChunk - 1) / kChunk);
   auto load = [&](int chunk, int j) {
     const uint32_t i = static_cast<uint32_t>(chunk) * kChunk + j * kThreads + tid;
@@ -196,25 +253,24 @@ __global__ __launch_bounds__(kThreads) void best_kernel(SelectParams p) {
 #pragma unroll
       for (int j = 0; j < kPer; ++j) f(kResident ? held[j] : load(chunk, j));
   };
-
-  // range and number of the scores above minus infinity
-  uint32_t lo = 0xffffffffu, hi = 0, count = 0;
-  each([&](uint32_t k) {
-    if (k > kLowest) lo = min(lo, k), hi = max(hi, k), ++count;
-  });
+  // over the workgroup: smallest, largest, and two sums
+  auto reduced = [&](uint32_t& lo, uint32_t& hi, uint32_t& x, uint32_t& y) {
 #pragma unroll
-  for (int d = 32; d > 0; d >>= 1) {
-    lo = min(lo, static_cast<uint32_t>(__shfl_xor(static_cast<int>(lo), d)));
-    hi = max(hi, static_cast<uint32_t>(__shfl_xor(static_cast<int>(hi), d)));
-    count += static_cast<uint32_t>(__shfl_xor(static_cast<int>(count), d));
-  }
-  if (lane == 0) parts[0][wave] = lo, parts[1][wave] = hi, parts[2][wave] = count;
-  __syncthreads();
-  lo = 0xffffffffu, hi = 0, count = 0;
+    for (int d = 32; d > 0; d >>= 1) {
+      lo = min(lo, static_cast<uint32_t>(__shfl_xor(static_cast<int>(lo), d)));
+      hi = max(hi, static_cast<uint32_t>(__shfl_xor(static_cast<int>(hi), d)));
+      x += static_cast<uint32_t>(__shfl_xor(static_cast<int>(x), d));
+      y += static_cast<uint32_t>(__shfl_xor(static_cast<int>(y), d));
+    }
+    __syncthreads();
+    if (lane == 0) parts[0][wave] = lo, parts[1][wave] = hi, parts[2][wave] = x, parts[3][wave] = y;
+    __syncthreads();
+    lo = 0xffffffffu, hi = x = y = 0;
 #pragma unroll
-  for (int w = 0; w < kWavesHere; ++w) lo = min(lo, parts[0][w]), hi = max(hi, parts[1][w]), count += parts[2][w];
-
-  // prefix sums over the workgroup of a value per thread, without its own; parts[0] is free between calls
+    for (int w = 0; w < kWavesHere; ++w)
+      lo = min(lo, parts[0][w]), hi = max(hi, parts[1][w]), x += parts[2][w], y += parts[3][w];
+  };
+  // prefix sums over the workgroup of a value per thread, without its own
   auto before_me = [&](uint32_t x) {
     const uint32_t with_me = wave_inclusive_scan(x);
     __syncthreads();
@@ -224,47 +280,103 @@ __global__ __launch_bounds__(kThreads) void best_kernel(SelectParams p) {
     for (int w = 0; w < wave; ++w) before += parts[0][w];
     return before;
   };
+  // histogram of the bins that `bin` gives (or -1); found: the bin that holds the need-th, those before it, and its own
+  auto find_bin = [&](uint32_t need, auto bin) {
+    __syncthreads();
+#pragma unroll
+    for (int b = 0; b < kBins / kThreads; ++b) hist[b * kThreads + tid] = 0;
+    if (tid == 0) few_count = 0;
+    __syncthreads();
+    each([&](uint32_t k) {
+      const int at = bin(k);
+      if (at < 0) return;
+      // (many equal scores would queue up at one address)
+      const int one = __builtin_amdgcn_readfirstlane(at);
+      const uint64_t all = __ballot(true);
+      if (__ballot(at == one) == all) {
+        if (lane == __builtin_ctzll(all)) atomicAdd(&hist[one], static_cast<uint32_t>(__popcll(all)));
+      } else {
+        atomicAdd(&hist[at], 1u);
+      }
+    });
+    __syncthreads();
+    constexpr int kMine = kBins / kThreads;
+    uint32_t bins[kMine], mine = 0;
+#pragma unroll
+    for (int b = 0; b < kMine; ++b) bins[b] = hist[tid * kMine + b], mine += bins[b];
+    uint32_t before = before_me(mine);
+#pragma unroll
+    for (int b = 0; b < kMine; ++b) {
+      if (before < need && need <= before + bins[b]) found[0] = tid * kMine + b, found[1] = before, found[2] = bins[b];
+      before += bins[b];
+    }
+    __syncthreads();
+  };
 
-  uint32_t threshold = kLowest, need = 0;   // taken: all above the threshold, and the first `need` at it
-  if (count <= static_cast<uint32_t>(want)) {
-    need = want - count;
+  uint32_t lo = 0xffffffffu, hi = 0, finite = 0, infinite = 0;
+  each([&](uint32_t k) {
+    const bool is_finite = k > kLowest && k < kHighest;
+    lo = min(lo, is_finite ? k : 0xffffffffu);
+    hi = max(hi, is_finite ? k : 0u);
+    finite += is_finite;
+    infinite += k == kHighest;
+  });
+  reduced(lo, hi, finite, infinite);
+
+  uint32_t threshold, need;   // taken: all above the threshold, and the first `need` at it
+  if (infinite >= want) {
+    threshold = kHighest, need = want;
+  } else if (infinite + finite <= want) {
+    threshold = kLowest, need = want - infinite - finite;
   } else {
-    need = want;
-    for (;;) {
+    need = want - infinite;
+    const float top = unordered(hi), width = top - unordered(lo), by = (kBins - 1) / width;
+    bool narrow = true;   // by bits
+    if (width < 1e37f && by < 1e37f) {
+      auto bin = [&](uint32_t k) {
+        return k >= lo && k <= hi ? min(static_cast<int>((top - unordered(k)) * by), kBins - 1) : -1;
+      };
+      find_bin(need, bin);
+      const int here = found[0];
+      const uint32_t size = found[2];
+      need -= found[1];
+      if (size <= kFew) {
+        // (before_me's barriers lie between the last reads of the histogram and this)
+        each([&](uint32_t k) {
+          if (bin(k) == here) hist[atomicAdd(&few_count, 1u)] = k;
+        });
+        __syncthreads();
+        for (uint32_t i = tid; i < size; i += kThreads) {
+          const uint32_t k = hist[i];
+          uint32_t above = 0, equal = 0;
+          for (uint32_t o = 0; o < size; ++o) {
+            const uint32_t other = hist[o];
+            above += other > k, equal += other == k;
+          }
+          if (above < need && need <= above + equal) found[0] = k, found[1] = above;   // (equal ones write the same)
+        }
+        __syncthreads();
+        threshold = found[0], need -= found[1];
+        narrow = false;
+      } else {
+        uint32_t low = 0xffffffffu, high = 0, none = 0, more = 0;
+        each([&](uint32_t k) {
+          const bool in = bin(k) == here;
+          low = min(low, in ? k : 0xffffffffu);
+          high = max(high, in ? k : 0u);
+        });
+        reduced(low, high, none, more);
+        lo = low, hi = high;
+      }
+    }
+    while (narrow) {
       const uint32_t span = hi - lo;
       const int low_bits = max(0, 32 - 11 - (span ? __builtin_clz(span) : 32));
-      __syncthreads();
-#pragma unroll
-      for (int b = 0; b < kBins / kThreads; ++b) hist[b * kThreads + tid] = 0;
-      __syncthreads();
-      each([&](uint32_t k) {
-        if (k < lo || k > hi) return;
-        const uint32_t bin = (hi - k) >> low_bits;   // the largest scores in the first bins
-        // (many equal scores would queue up at one address)
-        const uint32_t one = __builtin_amdgcn_readfirstlane(bin);
-        const uint64_t all = __ballot(true), same = __ballot(bin == one);
-        if (all == same) {
-          if (lane == __builtin_ctzll(all)) atomicAdd(&hist[one], static_cast<uint32_t>(__popcll(all)));
-        } else {
-          atomicAdd(&hist[bin], 1u);
-        }
-      });
-      __syncthreads();
-      constexpr int kMine = kBins / kThreads;
-      uint32_t bins[kMine], mine = 0;
-#pragma unroll
-      for (int b = 0; b < kMine; ++b) bins[b] = hist[tid * kMine + b], mine += bins[b];
-      uint32_t before = before_me(mine);
-#pragma unroll
-      for (int b = 0; b < kMine; ++b) {
-        if (before < need && need <= before + bins[b]) found[0] = tid * kMine + b, found[1] = before, found[2] = bins[b];
-        before += bins[b];
-      }
-      __syncthreads();
-      const uint32_t top = hi - (found[0] << low_bits), size = (1u << low_bits) - 1;
+      find_bin(need, [&](uint32_t k) { return k >= lo && k <= hi ? static_cast<int>((hi - k) >> low_bits) : -1; });
+      const uint32_t high = hi - (found[0] << low_bits), size = (1u << low_bits) - 1;
       need -= found[1];
-      lo = top - lo > size ? top - size : lo;
-      hi = top;
+      lo = high - lo > size ? high - size : lo;
+      hi = high;
       if (need == found[2]) {   // all that is left of the bin
         threshold = lo - 1, need = 0;
         break;
@@ -277,8 +389,18 @@ __global__ __launch_bounds__(kThreads) void best_kernel(SelectParams p) {
   }
 
   const int64_t token = static_cast<int64_t>(r) * p.n_q + g;
-  int32_t* const index = p.index + token * p.topk;
-  float* const out = p.out_scores ? p.out_scores + token * want : nullptr;
+  int32_t* index;
+  float* out;
+  if constexpr (kFrom == From::kSegment) {
+    // every segment but the last has as many
+    const int64_t at = static_cast<int64_t>(row) * p.candidates + static_cast<int64_t>(blockIdx.x % p.segments) * min(p.segment, static_cast<uint32_t>(wanted));
+    index = p.candidate_blocks + at;
+    out = p.candidate_scores + at;
+  } else {
+    index = p.index + token * p.topk;
+    out = p.out_scores ? p.out_scores + token * wanted : nullptr;
+  }
+  const int32_t* const candidates = kFrom == From::kSegments ? p.candidate_blocks + static_cast<int64_t>(row) * p.candidates : nullptr;
   uint32_t above_base = 0, equal_base = 0;
   for (int chunk = 0; chunk < chunks; ++chunk) {
     if (chunk > 0) __syncthreads();
@@ -305,9 +427,15 @@ __global__ __launch_bounds__(kThreads) void best_kernel(SelectParams p) {
       const uint64_t all = __ballot(taken);
       if (taken) {
         const uint32_t at = above_at + min(equal_at, need) + __popcll(all & lower);
-        const int block = chunk * kChunk + j * kThreads + tid;
-        for (int i = 0; i < 1 << shift; ++i) index[(static_cast<int64_t>(at) << shift) + i] = (block << shift) + i;
-        if (out) out[at] = unordered(k);
+        const int i = chunk * kChunk + j * kThreads + tid;
+        if constexpr (kFrom == From::kSegment) {
+          index[at] = static_cast<int>(first) + i;
+          out[at] = unordered(k);
+        } else {
+          const int block = candidates ? candidates[i] : i;
+          for (int x = 0; x < 1 << shift; ++x) index[(static_cast<int64_t>(at) << shift) + x] = (block << shift) + x;
+          if (out) out[at] = unordered(k);
+        }
       }
     }
   }
@@ -325,15 +453,28 @@ hipError_t run_scores(const SelectParams& p, hipStream_t s) {
   const int64_t runs = (tiles + run_tiles - 1) / run_tiles;
   const int64_t run_groups = (runs * waves_on_tokens + kWaves - 1) / kWaves, token_groups = (groups + waves_on_tokens - 1) / waves_on_tokens;
   const int64_t total = run_groups * token_groups * p.requests;
-  score_kernel<kTiles, kTok><<<dim3(static_cast<unsigned>(total)), kWaves * 64, 0, s>>>(
-      p, static_cast<int>(run_tiles), static_cast<int>(runs), groups, waves_on_tokens);
+  const auto kernel = p.cache.page_shift >= 4 ? &score_kernel<kTiles, kTok, true> : &score_kernel<kTiles, kTok, false>;
+  kernel<<<dim3(static_cast<unsigned>(total)), kWaves * 64, 0, s>>>(p, static_cast<int>(run_tiles), static_cast<int>(runs), groups,
+                                                                    waves_on_tokens);
   return hipGetLastError();
 }
 
-template <int kThreads, int kPer, bool kResident>
+template <int kThreads, int kPer, bool kResident, From kFrom>
 hipError_t run_best(const SelectParams& p, hipStream_t s) {
-  best_kernel<kThreads, kPer, kResident><<<dim3(static_cast<unsigned>(p.requests) * p.tokens), kThreads, 0, s>>>(p);
+  const int64_t groups = static_cast<int64_t>(p.requests) * p.tokens * (kFrom == From::kSegment ? p.segments : 1);
+  best_kernel<kThreads, kPer, kResident, kFrom><<<dim3(static_cast<unsigned>(groups)), kThreads, 0, s>>>(p);
   return hipGetLastError();
+}
+
+// From n scores each.
+template <From kFrom>
+hipError_t best_of(const SelectParams& p, int64_t n, hipStream_t s) {
+  if (n <= 2048) return run_best<256, 8, true, kFrom>(p, s);
+  if (n <= 8192) return run_best<512, 16, true, kFrom>(p, s);
+  if (n <= 16384) return run_best<512, 32, true, kFrom>(p, s);
+  if (n <= 32768) return run_best<1024, 32, true, kFrom>(p, s);
+  if (n <= 65536) return run_best<1024, 64, true, kFrom>(p, s);
+  return run_best<1024, 64, false, kFrom>(p, s);
 }
 
 }  // namespace
@@ -352,11 +493,11 @@ hipError_t launch_scores(const SelectParams& p, hipStream_t s) {
 }
 
 hipError_t launch_best(const SelectParams& p, hipStream_t s) {
-  const int n = p.longest >> p.block_shift;
-  if (n <= 2048) return run_best<256, 8, true>(p, s);
-  if (n <= 16384) return run_best<512, 32, true>(p, s);
-  if (n <= 65536) return run_best<1024, 64, true>(p, s);
-  return run_best<1024, 64, false>(p, s);
+  if (p.segments > 1) {
+    if (const hipError_t e = best_of<From::kSegment>(p, p.segment, s); e != hipSuccess) return e;
+    return best_of<From::kSegments>(p, p.candidates, s);
+  }
+  return best_of<From::kScores>(p, p.longest >> p.block_shift, s);
 }
 
 }  // namespace avsg
