@@ -196,6 +196,130 @@ __global__ __launch_bounds__(kWaves * 64, 2) void score_kernel(SelectParams p, i
   }
 }
 
+// Chunks of a prompt: a workgroup scores kChunkWaves tokens of a request, one per wave, against a run of keys that
+// they share in LDS, 64 keys at a time, while the next ones are on their way.
+constexpr int kChunkWaves = 8;
+constexpr int kStageKeys = 64;
+constexpr int kStagedRow = 144;   // bytes of a row in LDS: its codes, its scale; sixteen rows' sixteen bytes are in banks of their own
+template <int kTiles>
+__global__ __launch_bounds__(kChunkWaves * 64, kTiles > 4 ? 2 : 4) void chunk_kernel(SelectParams p, int run_stages, int runs, int groups) {
+  __shared__ __align__(16) unsigned char staged[2][kStageKeys * kStagedRow];
+  const int lane = threadIdx.x & 63, l16 = lane & 15, quad = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int run = static_cast<int>(blockIdx.x % runs), rest = static_cast<int>(blockIdx.x / runs);
+  const int group = rest % groups, r = p.r0 + rest / groups;
+  int most = 0, seen = 0;
+  for (int w = 0; w < kChunkWaves; ++w) {
+    const int t = group * kChunkWaves + w, n = t < p.tokens ? seen_by(p, r, p.g0 + t) : 0;
+    most = max(most, n);
+    if (w == wave) seen = n;   // none of a token past the last
+  }
+  const int first_key = run * run_stages * kStageKeys;
+  if (first_key >= most) return;
+  const int stages = min(run_stages, (most - first_key + kStageKeys - 1) / kStageKeys);
+  const int in_token = min(group * kChunkWaves + wave, p.tokens - 1);
+
+  i32x4 q[kTiles][2];
+  double weight[kTiles][4];
+  {
+    const int64_t at = static_cast<int64_t>(r) * p.n_q + p.g0 + in_token;
+    const int8_t* from = p.q + at * p.q_token_stride + quad * 32;
+    const float* weights = p.weights + at * p.weight_stride;
+#pragma unroll
+    for (int x = 0; x < kTiles; ++x) {
+      const int8_t* row = from + min(x * 16 + l16, p.heads - 1) * p.q_head_stride;
+      q[x][0] = *reinterpret_cast<const i32x4*>(row);
+      q[x][1] = *reinterpret_cast<const i32x4*>(row + 16);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int h = x * 16 + quad * 4 + i;
+        const float w = weights[min(h, p.heads - 1)];
+        weight[x][i] = h < p.heads ? static_cast<double>(w) : 0.0;
+      }
+    }
+  }
+  // eight threads per row
+  static_assert(kChunkWaves * 64 == kStageKeys * 8);
+  const int my_row = threadIdx.x / 8, my_part = threadIdx.x % 8 * 16;
+  i32x4 part;
+  float part_scale;
+  bool part_there;
+  auto load = [&](int stage) {
+    const int key = min(first_key + stage * kStageKeys + my_row, most - 1);
+    const int64_t at = static_cast<int64_t>(r) * p.cache.pages_per_request + (key >> p.cache.page_shift);
+    const int page = p.cache.table ? p.cache.table[at] : static_cast<int>(at);
+    part_there = page >= 0 && page < p.cache.pages;
+    const uint64_t row = p.cache.base + (part_there ? page * p.cache.page_stride + (key & p.cache.page_mask) * p.cache.row_stride : 0);
+    part = load_global<i32x4_at_4>(row + my_part);
+    part_scale = load_global<float>(row + kKeyScaleAt);
+  };
+  auto leave = [&](int buffer) {
+    unsigned char* const to = staged[buffer] + my_row * kStagedRow;
+    *reinterpret_cast<i32x4*>(to + my_part) = part;
+    if (my_part == 0) *reinterpret_cast<float*>(to + kKeyScaleAt) = part_there ? part_scale : __uint_as_float(0x7fc00000u);
+  };
+  auto meet_all = [&] {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+  };
+  const int shift = p.block_shift;
+  float* const out = p.scores + (static_cast<int64_t>(r - p.r0) * p.tokens + in_token) * p.score_stride;
+  float best = -__builtin_inff();   // of a block of 128 positions
+  load(0);
+  leave(0);
+  meet_all();
+  for (int stage = 0; stage < stages; ++stage) {
+    const int stage_key = first_key + stage * kStageKeys;
+    load(stage + 1);
+    if (stage_key < seen) {
+      const unsigned char* const from = staged[stage & 1];
+      double sum[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        i32x4 keys[2], dot[kTiles];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          keys[h] = *reinterpret_cast<const i32x4*>(from + (u * kTileKeys + l16) * kStagedRow + quad * 32 + h * 16);
+#pragma unroll
+        for (int x = 0; x < kTiles; ++x) dot[x] = __builtin_amdgcn_mfma_i32_16x16x64_i8(q[x][0], keys[0], i32x4{}, 0, 0, 0);
+#pragma unroll
+        for (int x = 0; x < kTiles; ++x) dot[x] = __builtin_amdgcn_mfma_i32_16x16x64_i8(q[x][1], keys[1], dot[x], 0, 0, 0);
+        sum[u] = 0.0;
+#pragma unroll
+        for (int x = 0; x < kTiles; ++x)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) sum[u] = __builtin_fma(weight[x][i], static_cast<double>(max(dot[x][i], 0)), sum[u]);
+      }
+      // row i of sixteen lanes gets the sums of tile i: lane l has key l of the stage
+      const float scale = *reinterpret_cast<const float*>(from + lane * kStagedRow + kKeyScaleAt);
+      float score = static_cast<float>(row_sums<4>(sum) * static_cast<double>(scale)) + 0.0f;
+      const int key = stage_key + lane;
+      if (!(score == score)) score = -__builtin_inff();
+      if (key < p.first || key >= seen - p.recent) score = __builtin_inff();
+      if (key >= seen) score = -__builtin_inff();
+      if (shift == 0) {
+        if (key < seen) out[key] = score;
+      } else {
+        score = group_max(score, shift);
+        if (shift > 4) score = fmaxf(score, __shfl_xor(score, 16));
+        if (shift > 5) score = fmaxf(score, __shfl_xor(score, 32));
+        if (shift <= 6) {
+          if ((lane & ((1 << shift) - 1)) == 0 && key < seen) out[key >> shift] = score;
+        } else {
+          best = fmaxf(best, score);
+          if ((stage & 1) != 0 || stage_key + kStageKeys >= seen || stage + 1 == stages) {
+            if (lane == 0) out[key >> shift] = best;
+            best = -__builtin_inff();
+          }
+        }
+      }
+    }
+    leave((stage + 1) & 1);
+    meet_all();
+  }
+}
+
 // Bits that order as the floats do (none of which is NaN), and back.
 __device__ __forceinline__ uint32_t ordered(float x) {
   const uint32_t u = __float_as_uint(x);
@@ -459,6 +583,19 @@ hipError_t run_scores(const SelectParams& p, hipStream_t s) {
   return hipGetLastError();
 }
 
+template <int kTiles>
+hipError_t run_chunk(const SelectParams& p, hipStream_t s) {
+  const int groups = (p.tokens + kChunkWaves - 1) / kChunkWaves;
+  const int64_t stages = (static_cast<int64_t>(p.longest) + kStageKeys - 1) / kStageKeys;
+  // runs of up to 16 stages, in pairs of them (the largest block)
+  const int64_t per_group = std::max<int64_t>(1, 1024 / (static_cast<int64_t>(p.requests) * groups));
+  const int64_t run_stages = std::min<int64_t>(16, ((stages + per_group - 1) / per_group + 1) / 2 * 2);
+  const int64_t runs = (stages + run_stages - 1) / run_stages;
+  chunk_kernel<kTiles><<<dim3(static_cast<unsigned>(runs * groups * p.requests)), kChunkWaves * 64, 0, s>>>(
+      p, static_cast<int>(run_stages), static_cast<int>(runs), groups);
+  return hipGetLastError();
+}
+
 template <int kThreads, int kPer, bool kResident, From kFrom>
 hipError_t run_best(const SelectParams& p, hipStream_t s) {
   const int64_t groups = static_cast<int64_t>(p.requests) * p.tokens * (kFrom == From::kSegment ? p.segments : 1);
@@ -481,6 +618,12 @@ hipError_t best_of(const SelectParams& p, int64_t n, hipStream_t s) {
 
 hipError_t launch_scores(const SelectParams& p, hipStream_t s) {
   const int tiles = (p.heads + 15) / 16;
+  if (p.tokens >= 6) {
+    if (tiles == 1) return run_chunk<1>(p, s);
+    if (tiles == 2) return run_chunk<2>(p, s);
+    if (tiles <= 4) return run_chunk<4>(p, s);
+    return run_chunk<8>(p, s);
+  }
   if (tiles > 4) return run_scores<8, 1>(p, s);
   if (p.tokens == 1) {
     if (tiles == 1) return run_scores<1, 1>(p, s);
