@@ -1,6 +1,7 @@
 // Scores of the key cache's positions for a step's query tokens, and the best
 // of them.
 #include <algorithm>
+#include <cfloat>
 
 #include "select_internal.h"
 
@@ -329,54 +330,52 @@ __device__ __forceinline__ float unordered(uint32_t u) { return __uint_as_float(
 constexpr uint32_t kLowest = 0x007fffffu, kHighest = 0xff800000u;   // ordered(-inf), ordered(inf)
 
 constexpr int kBins = 2048;
-constexpr int kFew = 512;   // scores of a bin that are compared with each other
+constexpr int kFew = 512;             // scores of a bin that are compared with each other
+constexpr int kCandidates = 4096;     // scores that are kept from the one pass over all of them
+constexpr int kSample = 4096;
 
-// What a workgroup picks from: the scores of a token's blocks; those of a segment of them; or what the
-// segments' workgroups left, in the blocks' order.
-enum class From { kScores, kSegment, kSegments };
-
-// The best blocks of a token, one workgroup per token (or segment).  The threshold lies in one of 2048 bins of
-// equal width between the smallest and the largest finite score, the scores of that bin are compared
-// with each other, and the blocks above the threshold, and the lowest of those at it, are written in
-// their order.  Where the bin holds many, or the scores are too far apart for such bins, histograms of
-// their bits narrow the range down until a bin holds one value or all that is wanted.
-// kResident: the scores stay in registers, else every pass reads them again.
-template <int kThreads, int kPer, bool kResident, From kFrom>
+// The best blocks of a token, one workgroup per token.  A sample of the scores gives a bound that a few more than those
+// wanted reach; one pass over all scores keeps these; the threshold lies in one of 2048 bins of equal width of
+// theirs, and the scores of that bin are compared with each other.  The blocks above the threshold, and those at it, are
+// marked in bit maps, from whose prefix sums each finds its place in the result.
+// Where that does not do (no bound that leaves few enough, as with many equal scores; more wanted than are
+// kept) histograms of all scores' bits narrow the threshold's range down until a bin holds one value or all that is
+// wanted, reading the scores again for each.
+// kMarks: blocks that are marked, and placed, at a time.
+template <int kThreads, int kMarks>
 __global__ __launch_bounds__(kThreads) void best_kernel(SelectParams p) {
-  constexpr int kWavesHere = kThreads / 64, kChunk = kThreads * kPer, kCounts = kPer * kWavesHere;
-  static_assert(kCounts <= kThreads && kBins % kThreads == 0 && kFew <= kBins);
-  __shared__ uint32_t hist[kBins];
-  __shared__ uint32_t above_counts[kCounts], equal_counts[kCounts];
+  constexpr int kWavesHere = kThreads / 64;
+  constexpr int kWords = kMarks / 32;
+  static_assert(kBins % kThreads == 0 && kWords % kThreads == 0 && kSample % kThreads == 0);
+  __shared__ uint32_t shared[kBins > 3 * kWords ? kBins : 3 * kWords];
+  uint32_t *const hist = shared, *const above_marks = shared, *const equal_marks = shared + kWords, *const before_words = shared + 2 * kWords;
+  __shared__ uint32_t kept[kCandidates], kept_block[kCandidates];
   __shared__ uint32_t parts[4][kWavesHere];
   __shared__ uint32_t found[3];
-  __shared__ uint32_t few_count;
+  __shared__ uint32_t count;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int row = kFrom == From::kSegment ? static_cast<int>(blockIdx.x) / p.segments : static_cast<int>(blockIdx.x);
-  const int r = p.r0 + row / p.tokens, g = p.g0 + row % p.tokens;
-  const int shift = p.block_shift, wanted = p.topk >> shift;   // of the token
-  const uint32_t blocks = p.longest >> shift;
-  const uint32_t first = kFrom == From::kSegment ? blockIdx.x % p.segments * p.segment : 0;
-  const uint32_t n = kFrom == From::kSegments ? static_cast<uint32_t>(p.candidates) : kFrom == From::kSegment ? min(blocks - first, p.segment) : blocks;
-  const uint32_t want = kFrom == From::kSegment ? min(n, static_cast<uint32_t>(wanted)) : wanted;
-  const uint32_t in_reach = (static_cast<uint32_t>(seen_by(p, r, g)) + (1u << shift) - 1) >> shift;
-  const uint32_t seen = kFrom == From::kSegments ? n : in_reach > first ? min(in_reach - first, n) : 0;
-  const float* const scores = kFrom == From::kSegments ? p.candidate_scores + static_cast<int64_t>(row) * p.candidates
-                                                       : p.scores + row * p.score_stride + first;
-  const int chunks = kResident ? 1 : static_cast<int>((n + kChunk - 1) / kChunk);
-  auto load = [&](int chunk, int j) {
-    const uint32_t i = static_cast<uint32_t>(chunk) * kChunk + j * kThreads + tid;
-    return i < seen ? ordered(scores[i]) : i < n ? kLowest : 0u;
+  const uint64_t lower = (uint64_t{1} << lane) - 1;
+  const int r = p.r0 + static_cast<int>(blockIdx.x) / p.tokens, g = p.g0 + static_cast<int>(blockIdx.x) % p.tokens;
+  const int shift = p.block_shift;
+  const uint32_t n = p.longest >> shift, want = p.topk >> shift;
+  const uint32_t seen = (static_cast<uint32_t>(seen_by(p, r, g)) + (1u << shift) - 1) >> shift;
+  const float* const scores = p.scores + static_cast<int64_t>(blockIdx.x) * p.score_stride;
+  const int64_t token = static_cast<int64_t>(r) * p.n_q + g;
+  int32_t* const index = p.index + token * p.topk;
+  float* const out = p.out_scores ? p.out_scores + token * want : nullptr;
+  auto put = [&](uint32_t at, uint32_t block, float score) {
+    for (int x = 0; x < 1 << shift; ++x) index[(static_cast<int64_t>(at) << shift) + x] = static_cast<int>(block << shift) + x;
+    if (out) out[at] = score;
   };
-  uint32_t held[kPer];
-  if constexpr (kResident) {
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) held[j] = load(0, j);
+
+  if (seen <= want) {
+    // all that is seen, and the lowest others
+    for (uint32_t i = tid; i < want << shift; i += kThreads) index[i] = static_cast<int>(i);
+    if (out)
+      for (uint32_t i = tid; i < want; i += kThreads) out[i] = i < seen ? scores[i] : -__builtin_inff();
+    return;
   }
-  auto each = [&](auto f) {
-    for (int chunk = 0; chunk < chunks; ++chunk)
-#pragma unroll
-      for (int j = 0; j < kPer; ++j) f(kResident ? held[j] : load(chunk, j));
-  };
+
   // over the workgroup: smallest, largest, and two sums
   auto reduced = [&](uint32_t& lo, uint32_t& hi, uint32_t& x, uint32_t& y) {
 #pragma unroll
@@ -404,24 +403,14 @@ __global__ __launch_bounds__(kThreads) void best_kernel(SelectParams p) {
     for (int w = 0; w < wave; ++w) before += parts[0][w];
     return before;
   };
-  // histogram of the bins that `bin` gives (or -1); found: the bin that holds the need-th, those before it, and its own
-  auto find_bin = [&](uint32_t need, auto bin) {
+  // a histogram of what `fill` adds; found: the bin that holds the need-th, those before it, and its own
+  auto find_bin = [&](uint32_t need, auto fill) {
     __syncthreads();
 #pragma unroll
     for (int b = 0; b < kBins / kThreads; ++b) hist[b * kThreads + tid] = 0;
-    if (tid == 0) few_count = 0;
     __syncthreads();
-    each([&](uint32_t k) {
-      const int at = bin(k);
-      if (at < 0) return;
-      // (many equal scores would queue up at one address)
-      const int one = __builtin_amdgcn_readfirstlane(at);
-      const uint64_t all = __ballot(true);
-      if (__ballot(at == one) == all) {
-        if (lane == __builtin_ctzll(all)) atomicAdd(&hist[one], static_cast<uint32_t>(__popcll(all)));
-      } else {
-        atomicAdd(&hist[at], 1u);
-      }
+    fill([&](int at) {
+      if (at >= 0) atomicAdd(&hist[at], 1u);
     });
     __syncthreads();
     constexpr int kMine = kBins / kThreads;
@@ -436,67 +425,195 @@ __global__ __launch_bounds__(kThreads) void best_kernel(SelectParams p) {
     }
     __syncthreads();
   };
+  auto is_finite = [](uint32_t k) { return k > kLowest && k < kHighest; };
+  // bins of equal width from the largest down, of finite scores from lo to hi
+  struct Bins {
+    uint32_t lo, hi;
+    float top, by;
+    __device__ bool fine() const { return top - unordered(lo) < 1e37f && by < 1e37f; }
+    __device__ int operator()(uint32_t k) const {
+      return k >= lo && k <= hi ? min(static_cast<int>((top - unordered(k)) * by), kBins - 1) : -1;
+    }
+  };
+  auto bins_of = [&](uint32_t lo, uint32_t hi) {
+    const float top = unordered(hi);
+    return Bins{lo, hi, top, (kBins - 1) / (top - unordered(lo))};
+  };
 
-  uint32_t lo = 0xffffffffu, hi = 0, finite = 0, infinite = 0;
-  each([&](uint32_t k) {
-    const bool is_finite = k > kLowest && k < kHighest;
-    lo = min(lo, is_finite ? k : 0xffffffffu);
-    hi = max(hi, is_finite ? k : 0u);
-    finite += is_finite;
-    infinite += k == kHighest;
-  });
-  reduced(lo, hi, finite, infinite);
-
-  uint32_t threshold, need;   // taken: all above the threshold, and the first `need` at it
-  if (infinite >= want) {
-    threshold = kHighest, need = want;
-  } else if (infinite + finite <= want) {
-    threshold = kLowest, need = want - infinite - finite;
-  } else {
-    need = want - infinite;
-    const float top = unordered(hi), width = top - unordered(lo), by = (kBins - 1) / width;
-    bool narrow = true;   // by bits
-    if (width < 1e37f && by < 1e37f) {
-      auto bin = [&](uint32_t k) {
-        return k >= lo && k <= hi ? min(static_cast<int>((top - unordered(k)) * by), kBins - 1) : -1;
-      };
-      find_bin(need, bin);
-      const int here = found[0];
-      const uint32_t size = found[2];
-      need -= found[1];
-      if (size <= kFew) {
-        // (before_me's barriers lie between the last reads of the histogram and this)
-        each([&](uint32_t k) {
-          if (bin(k) == here) hist[atomicAdd(&few_count, 1u)] = k;
+  uint32_t threshold = 0, need = 0;   // taken: all above the threshold, and the first `need` at it
+  bool done = false;
+  uint32_t candidates = 0;
+  if (want <= kCandidates) {
+    float bound = -FLT_MAX;
+    if (seen > kCandidates) {
+      // of the sample as many as are wanted of all, three standard deviations and three more
+      uint32_t k[kSample / kThreads], lo = 0xffffffffu, hi = 0, number = 0, none = 0;
+#pragma unroll
+      for (int j = 0; j < kSample / kThreads; ++j) {
+        k[j] = ordered(scores[static_cast<uint64_t>(j * kThreads + tid) * seen / kSample]);
+        const bool in = is_finite(k[j]);
+        lo = min(lo, in ? k[j] : 0xffffffffu);
+        hi = max(hi, in ? k[j] : 0u);
+        number += in;
+      }
+      reduced(lo, hi, number, none);
+      const float share = static_cast<float>(want) / static_cast<float>(seen) * kSample;
+      const uint32_t rank = static_cast<uint32_t>(share + 3.0f * sqrtf(share) + 3.0f);
+      const Bins bin = bins_of(lo, hi);
+      if (rank <= number && bin.fine()) {
+        find_bin(rank, [&](auto add) {
+#pragma unroll
+          for (int j = 0; j < kSample / kThreads; ++j) add(bin(k[j]));
         });
-        __syncthreads();
-        for (uint32_t i = tid; i < size; i += kThreads) {
-          const uint32_t k = hist[i];
-          uint32_t above = 0, equal = 0;
-          for (uint32_t o = 0; o < size; ++o) {
-            const uint32_t other = hist[o];
-            above += other > k, equal += other == k;
-          }
-          if (above < need && need <= above + equal) found[0] = k, found[1] = above;   // (equal ones write the same)
-        }
-        __syncthreads();
-        threshold = found[0], need -= found[1];
-        narrow = false;
-      } else {
-        uint32_t low = 0xffffffffu, high = 0, none = 0, more = 0;
-        each([&](uint32_t k) {
-          const bool in = bin(k) == here;
-          low = min(low, in ? k : 0xffffffffu);
-          high = max(high, in ? k : 0u);
-        });
-        reduced(low, high, none, more);
-        lo = low, hi = high;
+        bound = bin.top - static_cast<float>(found[0] + 1) / bin.by;
       }
     }
-    while (narrow) {
+    // where it is reached, in no order: 32 scores of a thread at a time, as bits
+    if (tid == 0) count = 0;
+    __syncthreads();
+    for (uint32_t at = 0; at < seen; at += kThreads * 32) {
+      f32x4 x[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if (at + j * kThreads * 4 >= seen) break;
+        x[j] = *reinterpret_cast<const f32x4*>(scores + min(at + (j * kThreads + tid) * 4, (seen - 1) & ~3u));
+      }
+      uint32_t hits = 0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if (at + j * kThreads * 4 >= seen) break;
+        const uint32_t i = at + (j * kThreads + tid) * 4, left = i < seen ? seen - i : 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) hits |= x[j][e] >= bound ? 1u << (4 * j + e) : 0;
+        if (left < 4) hits &= ~(15u << (4 * j)) | ((1u << left) - 1) << (4 * j);
+      }
+      const uint32_t mine = __popc(hits), with_me = wave_inclusive_scan(mine);
+      uint32_t to = 0;
+      if (lane == 63 && with_me) to = atomicAdd(&count, with_me);
+      to = __builtin_amdgcn_readlane(to, 63) + with_me - mine;
+      while (hits) {
+        const int b = __ffs(static_cast<int>(hits)) - 1;
+        hits &= hits - 1;
+        if (to < kCandidates) kept_block[to] = at + (b / 4 * kThreads + tid) * 4 + b % 4;
+        ++to;
+      }
+    }
+    __syncthreads();
+    candidates = count;
+    if (candidates >= want && candidates <= kCandidates) {
+      uint32_t lo = 0xffffffffu, hi = 0, infinite = 0, none = 0;
+      for (uint32_t i = tid; i < candidates; i += kThreads) {
+        const uint32_t k = ordered(scores[kept_block[i]]);
+        kept[i] = k;
+        lo = min(lo, is_finite(k) ? k : 0xffffffffu);
+        hi = max(hi, is_finite(k) ? k : 0u);
+        infinite += k == kHighest;
+      }
+      reduced(lo, hi, infinite, none);
+      if (infinite >= want) {
+        threshold = kHighest, need = want, done = true;
+      } else if (const Bins bin = bins_of(lo, hi); bin.fine()) {
+        need = want - infinite;
+        find_bin(need, [&](auto add) {
+          for (uint32_t i = tid; i < candidates; i += kThreads) add(bin(kept[i]));
+        });
+        const int here = found[0];
+        const uint32_t before = found[1], size = found[2];
+        if (size <= kFew) {
+          need -= before;
+          if (tid == 0) count = 0;
+          __syncthreads();
+          // (the histogram has been read)
+          for (uint32_t i = tid; i < candidates; i += kThreads)
+            if (bin(kept[i]) == here) hist[atomicAdd(&count, 1u)] = kept[i];
+          __syncthreads();
+          for (uint32_t i = tid; i < size; i += kThreads) {
+            const uint32_t k = hist[i];
+            uint32_t above = 0, equal = 0;
+            for (uint32_t o = 0; o < size; ++o) {
+              const uint32_t other = hist[o];
+              above += other > k, equal += other == k;
+            }
+            if (above < need && need <= above + equal) found[0] = k, found[1] = above;   // (equal ones write the same)
+          }
+          __syncthreads();
+          threshold = found[0], need -= found[1], done = true;
+        }
+      }
+    }
+  }
+
+  if (done) {
+    uint32_t above_base = 0, equal_base = 0;
+    for (uint32_t first = 0; first < seen; first += kMarks) {
+      constexpr int kMine = kWords / kThreads;   // words per thread
+      __syncthreads();
+#pragma unroll
+      for (int w = 0; w < kMine; ++w) above_marks[w * kThreads + tid] = 0, equal_marks[w * kThreads + tid] = 0;
+      __syncthreads();
+      for (uint32_t i = tid; i < candidates; i += kThreads) {
+        const uint32_t k = kept[i], block = kept_block[i] - first;
+        if (k >= threshold && block < kMarks) atomicOr(&(k == threshold ? equal_marks : above_marks)[block / 32], 1u << (block & 31));
+      }
+      __syncthreads();
+      // above and equal in one word: at most kCandidates each
+      uint32_t words[kMine], both = 0;
+#pragma unroll
+      for (int w = 0; w < kMine; ++w) {
+        words[w] = __popc(above_marks[tid * kMine + w]) + (__popc(equal_marks[tid * kMine + w]) << 16);
+        both += words[w];
+      }
+      uint32_t before = before_me(both);
+      if (tid == kThreads - 1) found[2] = before + both;
+#pragma unroll
+      for (int w = 0; w < kMine; ++w) {
+        before_words[tid * kMine + w] = before;
+        before += words[w];
+      }
+      __syncthreads();
+      for (uint32_t i = tid; i < candidates; i += kThreads) {
+        const uint32_t k = kept[i], block = kept_block[i] - first;
+        if (k < threshold || block >= kMarks) continue;
+        const uint32_t word = block / 32, below = (1u << (block & 31)) - 1, prior = before_words[word];
+        const uint32_t above_at = above_base + (prior & 0xffff) + __popc(above_marks[word] & below);
+        const uint32_t equal_at = equal_base + (prior >> 16) + __popc(equal_marks[word] & below);
+        if (k > threshold || equal_at < need) put(above_at + min(equal_at, need), first + block, unordered(k));
+      }
+      above_base += found[2] & 0xffff, equal_base += found[2] >> 16;
+    }
+    return;
+  }
+
+  // all scores, again and again
+  auto load = [&](uint32_t i) { return i < seen ? ordered(scores[i]) : i < n ? kLowest : 0u; };
+  uint32_t lo = 0xffffffffu, hi = 0, number = 0, none = 0;
+  for (uint32_t i = tid; i < seen; i += kThreads) {
+    const uint32_t k = load(i);
+    if (k > kLowest) lo = min(lo, k), hi = max(hi, k), ++number;
+  }
+  reduced(lo, hi, number, none);
+  threshold = kLowest, need = want;
+  if (number <= want) {
+    need = want - number;
+  } else {
+    for (;;) {
       const uint32_t span = hi - lo;
       const int low_bits = max(0, 32 - 11 - (span ? __builtin_clz(span) : 32));
-      find_bin(need, [&](uint32_t k) { return k >= lo && k <= hi ? static_cast<int>((hi - k) >> low_bits) : -1; });
+      find_bin(need, [&](auto) {
+        for (uint32_t i = tid; i < seen; i += kThreads) {
+          const uint32_t k = load(i);
+          if (k < lo || k > hi) continue;
+          const int at = (hi - k) >> low_bits;   // the largest scores in the first bins
+          // (many equal scores would queue up at one address)
+          const int one = __builtin_amdgcn_readfirstlane(at);
+          const uint64_t all = __ballot(true);
+          if (__ballot(at == one) == all) {
+            if (lane == __builtin_ctzll(all)) atomicAdd(&hist[one], static_cast<uint32_t>(__popcll(all)));
+          } else {
+            atomicAdd(&hist[at], 1u);
+          }
+        }
+      });
       const uint32_t high = hi - (found[0] << low_bits), size = (1u << low_bits) - 1;
       need -= found[1];
       lo = high - lo > size ? high - size : lo;
@@ -511,57 +628,21 @@ __global__ __launch_bounds__(kThreads) void best_kernel(SelectParams p) {
       }
     }
   }
-
-  const int64_t token = static_cast<int64_t>(r) * p.n_q + g;
-  int32_t* index;
-  float* out;
-  if constexpr (kFrom == From::kSegment) {
-    // every segment but the last has as many
-    const int64_t at = static_cast<int64_t>(row) * p.candidates + static_cast<int64_t>(blockIdx.x % p.segments) * min(p.segment, static_cast<uint32_t>(wanted));
-    index = p.candidate_blocks + at;
-    out = p.candidate_scores + at;
-  } else {
-    index = p.index + token * p.topk;
-    out = p.out_scores ? p.out_scores + token * wanted : nullptr;
-  }
-  const int32_t* const candidates = kFrom == From::kSegments ? p.candidate_blocks + static_cast<int64_t>(row) * p.candidates : nullptr;
   uint32_t above_base = 0, equal_base = 0;
-  for (int chunk = 0; chunk < chunks; ++chunk) {
-    if (chunk > 0) __syncthreads();
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-      const uint32_t k = kResident ? held[j] : load(chunk, j);
-      const uint64_t above = __ballot(k > threshold), equal = __ballot(k == threshold);
-      if (lane == 0) above_counts[j * kWavesHere + wave] = __popcll(above), equal_counts[j * kWavesHere + wave] = __popcll(equal);
-    }
+  for (uint32_t first = 0; first < n; first += kThreads) {
+    const uint32_t k = load(first + tid);
+    const uint64_t above = __ballot(k > threshold), equal = __ballot(k == threshold);
     __syncthreads();
-    const uint32_t above_here = tid < kCounts ? above_counts[tid] : 0, equal_here = tid < kCounts ? equal_counts[tid] : 0;
-    const uint32_t above_before = before_me(above_here), equal_before = before_me(equal_here);
-    if (tid < kCounts) above_counts[tid] = above_base + above_before, equal_counts[tid] = equal_base + equal_before;
-    if (tid == kThreads - 1) found[0] = above_base + above_before + above_here, found[1] = equal_base + equal_before + equal_here;
+    if (lane == 0) parts[0][wave] = __popcll(above), parts[1][wave] = __popcll(equal);
     __syncthreads();
-    above_base = found[0], equal_base = found[1];
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-      const uint32_t k = kResident ? held[j] : load(chunk, j);
-      const uint32_t above_at = above_counts[j * kWavesHere + wave], equal_at = equal_counts[j * kWavesHere + wave];
-      const uint64_t lower = (uint64_t{1} << lane) - 1;
-      const uint64_t equal = __ballot(k == threshold);
-      const bool taken = k > threshold || (k == threshold && equal_at + __popcll(equal & lower) < need);
-      const uint64_t all = __ballot(taken);
-      if (taken) {
-        const uint32_t at = above_at + min(equal_at, need) + __popcll(all & lower);
-        const int i = chunk * kChunk + j * kThreads + tid;
-        if constexpr (kFrom == From::kSegment) {
-          index[at] = static_cast<int>(first) + i;
-          out[at] = unordered(k);
-        } else {
-          const int block = candidates ? candidates[i] : i;
-          for (int x = 0; x < 1 << shift; ++x) index[(static_cast<int64_t>(at) << shift) + x] = (block << shift) + x;
-          if (out) out[at] = unordered(k);
-        }
-      }
+    uint32_t above_at = above_base, equal_at = equal_base;
+    for (int w = 0; w < kWavesHere; ++w) {
+      if (w < wave) above_at += parts[0][w], equal_at += parts[1][w];
+      above_base += parts[0][w], equal_base += parts[1][w];
     }
+    const bool taken = k > threshold || (k == threshold && equal_at + __popcll(equal & lower) < need);
+    const uint64_t all = __ballot(taken);
+    if (taken) put(above_at + min(equal_at, need) + __popcll(all & lower), first + tid, unordered(k));
   }
 }
 
@@ -596,22 +677,10 @@ hipError_t run_chunk(const SelectParams& p, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <int kThreads, int kPer, bool kResident, From kFrom>
+template <int kThreads, int kMarks>
 hipError_t run_best(const SelectParams& p, hipStream_t s) {
-  const int64_t groups = static_cast<int64_t>(p.requests) * p.tokens * (kFrom == From::kSegment ? p.segments : 1);
-  best_kernel<kThreads, kPer, kResident, kFrom><<<dim3(static_cast<unsigned>(groups)), kThreads, 0, s>>>(p);
+  best_kernel<kThreads, kMarks><<<dim3(static_cast<unsigned>(p.requests) * p.tokens), kThreads, 0, s>>>(p);
   return hipGetLastError();
-}
-
-// From n scores each.
-template <From kFrom>
-hipError_t best_of(const SelectParams& p, int64_t n, hipStream_t s) {
-  if (n <= 2048) return run_best<256, 8, true, kFrom>(p, s);
-  if (n <= 8192) return run_best<512, 16, true, kFrom>(p, s);
-  if (n <= 16384) return run_best<512, 32, true, kFrom>(p, s);
-  if (n <= 32768) return run_best<1024, 32, true, kFrom>(p, s);
-  if (n <= 65536) return run_best<1024, 64, true, kFrom>(p, s);
-  return run_best<1024, 64, false, kFrom>(p, s);
 }
 
 }  // namespace
@@ -636,11 +705,10 @@ hipError_t launch_scores(const SelectParams& p, hipStream_t s) {
 }
 
 hipError_t launch_best(const SelectParams& p, hipStream_t s) {
-  if (p.segments > 1) {
-    if (const hipError_t e = best_of<From::kSegment>(p, p.segment, s); e != hipSuccess) return e;
-    return best_of<From::kSegments>(p, p.candidates, s);
-  }
-  return best_of<From::kScores>(p, p.longest >> p.block_shift, s);
+  const int n = p.longest >> p.block_shift;
+  if (n <= 4096) return run_best<256, 8192>(p, s);
+  if (n <= 16384) return run_best<512, 16384>(p, s);
+  return run_best<1024, 131072>(p, s);
 }
 
 }  // namespace avsg

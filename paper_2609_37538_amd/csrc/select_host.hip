@@ -21,23 +21,6 @@ bool codes16(const void* p, int64_t token_stride, int64_t head_stride) {
   return p && aligned(p, 16) && (token_stride & 15) == 0 && (head_stride & 15) == 0;
 }
 
-// Blocks that a workgroup picks from where a token's are split, and how many blocks are split.
-constexpr int64_t kSegment = 8192, kSplitFrom = 32768;
-// Tokens of a turn whose blocks are split: with more the CUs are busy without.
-constexpr int64_t kSplitTokens = 64;
-
-// How a turn's tokens are picked from: sets the segments if they leave at most half of the blocks.
-void split(SelectParams& p, int64_t blocks, int64_t wanted) {
-  p.segments = 1;
-  if (blocks <= kSplitFrom) return;
-  const int64_t segments = (blocks + kSegment - 1) / kSegment, last = blocks - (segments - 1) * kSegment;
-  const int64_t candidates = (segments - 1) * std::min(wanted, kSegment) + std::min(wanted, last);
-  if (candidates * 2 > blocks) return;
-  p.segments = static_cast<int32_t>(segments);
-  p.segment = static_cast<uint32_t>(kSegment);
-  p.candidates = static_cast<int32_t>(candidates);
-}
-
 // floats of a token's block scores
 int64_t score_floats(int32_t longest, int32_t block) { return (static_cast<int64_t>(longest) / block + 3) & ~int64_t{3}; }
 
@@ -127,9 +110,8 @@ size_t avsg_select_workspace_least(int32_t longest, int32_t block) {
 size_t avsg_select_workspace_bytes(int32_t batch, int32_t n_q, int32_t longest, int32_t block) {
   const int64_t token = static_cast<int64_t>(avsg_select_workspace_least(longest, block));
   if (batch < 1 || n_q < 1 || token == 0) return 0;
-  const int64_t tokens = static_cast<int64_t>(batch) * n_q, turn = std::min(tokens, std::max<int64_t>(1, kTurnBytes / token));
-  // what segments leave is at most half of the scores and as many block numbers
-  return static_cast<size_t>((turn + (longest / block > kSplitFrom && turn <= kSplitTokens ? turn : 0)) * token);
+  const int64_t tokens = static_cast<int64_t>(batch) * n_q;
+  return static_cast<size_t>(std::min(tokens, std::max<int64_t>(1, kTurnBytes / token)) * token);
 }
 
 avsg_status avsg_select(const avsg_key_cache* cache, const avsg_selection* a, void* d_workspace, size_t workspace_bytes,
@@ -179,13 +161,6 @@ avsg_status avsg_select(const avsg_key_cache* cache, const avsg_selection* a, vo
   p.tokens = static_cast<int32_t>(std::min<int64_t>(a->n_q, most));
   p.requests = p.tokens < a->n_q ? 1 : static_cast<int32_t>(std::min<int64_t>(cache->batch, most / a->n_q));
   const int32_t by_r = p.requests, by_g = p.tokens;
-  const int64_t turn = static_cast<int64_t>(by_r) * by_g;
-  p.segments = 1;
-  if (turn <= kSplitTokens && 2 * turn <= room) {
-    split(p, a->longest / a->block, a->topk / a->block);
-    p.candidate_scores = p.scores + turn * floats;
-    p.candidate_blocks = reinterpret_cast<int32_t*>(p.candidate_scores + turn * p.candidates);
-  }
   for (p.r0 = 0; p.r0 < cache->batch; p.r0 += by_r) {
     p.requests = std::min(by_r, cache->batch - p.r0);
     for (p.g0 = 0; p.g0 < a->n_q; p.g0 += by_g) {

@@ -46,12 +46,6 @@ struct SelectParams {
   float* out_scores;        // or nullptr
   float* scores;            // workspace: [tokens of a turn][score_stride]
   int64_t score_stride;     // blocks of a token's positions, rounded up to 16 bytes
-  // with few tokens of many blocks, workgroups pick from segments of them first
-  int32_t segments;         // 1: they do not
-  uint32_t segment;         // blocks of a segment (the last has the rest)
-  int32_t candidates;       // what the segments of a token leave together
-  float* candidate_scores;  // workspace: [tokens of a turn][candidates]
-  int32_t* candidate_blocks;
   int32_t r0, g0, requests, tokens;   // a turn: tokens [g0, g0 + tokens) of requests [r0, r0 + requests)
 };
 
