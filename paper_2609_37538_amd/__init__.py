@@ -7,6 +7,8 @@ The operator lives in the HIP library ``libavsg.so`` (C ABI in
 rows that a step placed, and the 4-bit microscaled form; and
 :mod:`paper_2609_37538_amd.selection` what makes a step's selection
 (``include/avsg_select.h``): the cache of index keys and the scores over it.
+:mod:`paper_2609_37538_amd.fp8` (``include/avsg_fp8.h``) has matrices in 8-bit
+floating point and their product.
 """
 from .avsg import (  # noqa: F401
     AVSG_GATHER_BALANCED, AVSG_GATHER_NONE, AVSG_GATHER_PIPELINED, AVSG_GATHER_POSITION,
@@ -22,6 +24,7 @@ from .latent import (  # noqa: F401
     AVSG_BF16, AVSG_F32, AVSG_ROPE_HALVES, AVSG_ROPE_PAIRS, AVSG_ROWS_BF16, AVSG_ROWS_MX4, LatentCache, Mx4,
     mx4_dequantize, mx4_matmul, mx4_quantize,
 )
+from .fp8 import Fp8, fp8_dequantize, fp8_matmul, fp8_quantize  # noqa: F401
 from .selection import KeyCache  # noqa: F401
 
 

@@ -14,7 +14,7 @@ LIB_PATH = os.path.join(PKG, "libavsg.so")
 
 SOURCES = ["avsg_host.hip", "match_hash.hip", "match_dualptr.hip", "gather.hip", "step_pipelined.hip",
            "step_early.hip", "latent_host.hip", "latent_cache.hip", "latent_attend.hip", "mx4.hip", "mx4_matmul.hip",
-           "select_host.hip", "keys.hip", "select.hip"]
+           "select_host.hip", "keys.hip", "select.hip", "fp8_host.hip", "fp8.hip", "fp8_matmul.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
