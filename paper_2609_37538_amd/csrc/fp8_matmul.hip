@@ -6,6 +6,8 @@
 // scales.  The operands change places, so that a lane holds four neighbouring columns of one row of
 // out, and with them one scale of a; b's is the same for 128 columns of out.
 #include <algorithm>
+#include <type_traits>
+#include <utility>
 
 #include "fp8_internal.h"
 
@@ -121,15 +123,198 @@ __global__ __launch_bounds__(kWaves * 64) void thin_kernel(Fp8Product p) {
   }
 }
 
+// What columns past the end read in place of codes.
+__device__ __align__(16) const unsigned char zero_block[16] = {};
+
+// Bits of a row by which its staged blocks of 16 bytes are exchanged: the eight pairs of the sixteen rows that are
+// read together differ in them.
+__device__ __forceinline__ int exchange(int row) { return row >> 1 & 7; }
+
+// f(0), f(1), ..., each with its number as a constant.
+template <class F, int... kI>
+__device__ __forceinline__ void each(std::integer_sequence<int, kI...>, F f) {
+  (f(std::integral_constant<int, kI>{}), ...);
+}
+template <int kCount, class F>
+__device__ __forceinline__ void each(F f) {
+  each(std::make_integer_sequence<int, kCount>{}, f);
+}
+
+// Larger products: tiles of kTile x kTile outputs, kWavesM x kWavesN waves.  Steps of 128 columns, a block, go from
+// global memory to LDS without passing registers, the next step's while this one's products run.  In LDS a row
+// has its 128 bytes of the step, its eight blocks of 16 exchanged by three bits of the row, so that the sixteen lanes that
+// read one block of sixteen rows meet every bank; eight neighbouring lanes fetch a row's whole line.
+// The rows' scales of the step follow, a's, then b's for each 128 rows.
+// kGroups groups of such waves share the columns, a run of steps each, and add up in LDS.
+template <int kTile, int kWavesM, int kWavesN, int kGroups, bool kF32>
+__global__ __launch_bounds__(kGroups * kWavesM * kWavesN * 64, kGroups * kWavesM * kWavesN / 4) void staged_kernel(Fp8Product p, int tiles_m, int tiles_n) {
+  constexpr int kWaves = kWavesM * kWavesN, kThreads = kWaves * 64;
+  constexpr int kM = kTile / kWavesM / 16, kN = kTile / kWavesN / 16;
+  constexpr int kRows = 2 * kTile;                // rows of a, then rows of b
+  constexpr int kLoads = kRows / 8 / kWaves;      // eight rows each
+  constexpr int kScaleLoads = kTile / 64 + 1;     // 64 scales each: a's, and b's
+  static_assert(kRows % (8 * kWaves) == 0 && kScaleLoads <= kWaves + 1);
+  constexpr int kStage = kRows * 128 + kScaleLoads * 256;
+  extern __shared__ __align__(16) unsigned char all_lds[];   // [kGroups][2][kStage], then the groups' sums
+  const int lane = threadIdx.x & 63, l16 = lane & 15, quad = lane >> 4;
+  const int group = kGroups > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / kThreads) : 0;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) - group * kWaves;
+  unsigned char* const lds = all_lds + group * 2 * kStage;
+  // tiles of eight rows of tiles follow each other down the columns, on one XCD, so that its L2 holds the operands
+  // they share
+  const unsigned total = gridDim.x, per = total / kXcds, more = total % kXcds, xcd = blockIdx.x % kXcds;
+  const unsigned id = xcd * per + min(xcd, more) + blockIdx.x / kXcds;
+  constexpr int kBand = 8;
+  const int in_band = kBand * tiles_n, band = id / in_band, rows_here = min(kBand, tiles_m - band * kBand);
+  const int tm = band * kBand + (id - band * in_band) % rows_here, tn = (id - band * in_band) / rows_here;
+  const int64_t i = blockIdx.y;
+  const int steps = (p.k + kFp8Block - 1) / kFp8Block;
+
+  // Row `r` of the tile's rows of a and b, as an offset from the first of them; rows past the end are not stored, and read
+  // as the last.
+  const uint8_t* const codes_a = p.a.codes + i * p.a.code_batch_stride + static_cast<int64_t>(tm) * kTile * p.a.code_stride;
+  const uint8_t* const codes_b = p.b.codes + i * p.b.code_batch_stride + static_cast<int64_t>(tn) * kTile * p.b.code_stride;
+  const int last_a = p.m - 1 - tm * kTile, last_b = p.n - 1 - tn * kTile;
+  auto from_a = [&](int j) { return (j * kWaves + wave) * 8 < kTile; };   // eight rows are of one matrix
+  uint32_t row_at[kLoads];
+  static_assert(kWaves % 2 == 0, "all loads exchange blocks alike");
+#pragma unroll
+  for (int j = 0; j < kLoads; ++j) {
+    const int r = (j * kWaves + wave) * 8 + lane / 8;
+    row_at[j] = from_a(j) ? min(r, last_a) * static_cast<uint32_t>(p.a.code_stride)
+                          : min(r - kTile, last_b) * static_cast<uint32_t>(p.b.code_stride);
+  }
+  const int my_block = (lane & 7) ^ exchange(wave * 8 + lane / 8);
+  // a's scales by the first waves, b's by the one after them (or the first)
+  constexpr int kWaveOfB = (kScaleLoads - 1) % kWaves;
+  const float* const scales_a = p.a.scales + i * p.a.scale_batch_stride + (tm * kTile + min(wave * 64 + lane, last_a)) * p.a.scale_stride;
+  const float* const scales_b =
+      p.b.scales + i * p.b.scale_batch_stride + min(tn * kTile / kFp8Block + (lane & 1), (p.n - 1) / kFp8Block) * p.b.scale_stride;
+  auto fetch = [&](int j, int step, int buffer) {
+    // (the compiler would keep advancing 64-bit addresses)
+    uint32_t row = row_at[j];
+    asm volatile("" : "+v"(row));
+    const int at = step * kFp8Block + my_block * 16;
+    const uint8_t* from = (from_a(j) ? codes_a : codes_b) + row + static_cast<uint32_t>(at);
+    if (at >= p.k) from = zero_block;
+    __builtin_amdgcn_global_load_lds(
+        reinterpret_cast<const __attribute__((address_space(1))) void*>(reinterpret_cast<uint64_t>(from)),
+        (__attribute__((address_space(3))) void*)(lds + buffer * kStage + (j * kWaves + wave) * 1024), 16, 0, 0);
+  };
+  auto fetch_scales = [&](int step, int buffer) {
+    const int block = min(step, steps - 1);   // (past the end the codes are zeros)
+    const int at = buffer * kStage + kRows * 128;
+    if (wave < kTile / 64)
+      __builtin_amdgcn_global_load_lds(
+          reinterpret_cast<const __attribute__((address_space(1))) void*>(reinterpret_cast<uint64_t>(scales_a + block)),
+          (__attribute__((address_space(3))) void*)(lds + at + wave * 256), 4, 0, 0);
+    if (wave == kWaveOfB)
+      __builtin_amdgcn_global_load_lds(
+          reinterpret_cast<const __attribute__((address_space(1))) void*>(reinterpret_cast<uint64_t>(scales_b + block)),
+          (__attribute__((address_space(3))) void*)(lds + at + kTile * 4), 4, 0, 0);
+  };
+
+  f32x4 sum[kM][kN] = {};
+  const int wave_a = wave / kWavesN * (kM * 16), wave_b = wave % kWavesN * (kN * 16);
+  const unsigned at_a = (wave_a + l16) * 128 + ((2 * quad) ^ exchange(l16)) * 16;
+  const unsigned at_b = (kTile + wave_b + l16) * 128 + ((2 * quad) ^ exchange(l16)) * 16;
+  // a wave's columns are of one block of b's rows
+  static_assert(kFp8Block % (kN * 16) == 0);
+  const unsigned at_scale_a = kRows * 128 + (wave_a + l16) * 4, at_scale_b = kRows * 128 + kTile * 4 + wave_b / kFp8Block * 4;
+  // a group's steps follow each other; what it takes past the last step are zeros
+  const int steps_here = (steps + kGroups - 1) / kGroups, first_step = group * steps_here;
+#pragma unroll
+  for (int j = 0; j < kLoads; ++j) fetch(j, first_step, 0);
+  fetch_scales(first_step, 0);
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  for (int step = 0; step < steps_here; ++step) {
+    const int buffer = step & 1, next = first_step + step + 1;
+    const unsigned char* const from = lds + buffer * kStage;
+    u32x4 a[kM][2], b[kN][2];
+    float scale[kM];
+    const float scale_b = *reinterpret_cast<const float*>(from + at_scale_b);
+    each<kN>([&](auto y) {
+      each<2>([&](auto h) { b[y][h] = *reinterpret_cast<const u32x4*>(from + y * 2048 + (at_b ^ (h * 16))); });
+    });
+    each<kM>([&](auto x) {
+      each<2>([&](auto h) { a[x][h] = *reinterpret_cast<const u32x4*>(from + x * 2048 + (at_a ^ (h * 16))); });
+      scale[x] = *reinterpret_cast<const float*>(from + at_scale_a + x * 64);
+    });
+    fetch_scales(next, buffer ^ 1);
+    each<kM>([&](auto x) {
+      each<kLoads / kM + (kLoads % kM != 0)>([&](auto j) {
+        if constexpr (x * (kLoads / kM + (kLoads % kM != 0)) + j < kLoads) fetch(x * (kLoads / kM + (kLoads % kM != 0)) + j, next, buffer ^ 1);
+      });
+      const float s = scale[x] * scale_b;
+      each<kN>([&](auto y) {
+        const f32x4 part = multiply(b[y][0], b[y][1], a[x][0], a[x][1]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sum[x][y][j] = __builtin_fmaf(part[j], s, sum[x][y][j]);
+      });
+    });
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+  }
+  if constexpr (kGroups > 1) {
+    f32x4* const sums = reinterpret_cast<f32x4*>(all_lds);
+    each<kM>([&](auto x) {
+      each<kN>([&](auto y) {
+        if (group > 0) sums[((group - 1) * kM * kN + x * kN + y) * kThreads + wave * 64 + lane] = sum[x][y];
+      });
+    });
+    __syncthreads();
+    if (group > 0) return;
+    each<kM>([&](auto x) {
+      each<kN>([&](auto y) {
+        each<kGroups - 1>([&](auto g) { sum[x][y] += sums[(g * kM * kN + x * kN + y) * kThreads + wave * 64 + lane]; });
+      });
+    });
+  }
+  each<kM>([&](auto x) {
+    each<kN>([&](auto y) { store4<kF32>(p, i, tm * kTile + wave_a + x * 16 + l16, tn * kTile + wave_b + y * 16 + quad * 4, sum[x][y]); });
+  });
+}
+
+template <int kTile, int kWavesM, int kWavesN, int kGroups, bool kF32>
+hipError_t launch_staged(const Fp8Product& p, int64_t tiles_m, int64_t tiles_n, hipStream_t s) {
+  constexpr int kLds = kGroups * 2 * (2 * kTile * 128 + (kTile / 64 + 1) * 256);
+  static_assert(kLds <= 160 * 1024, "LDS of a workgroup");
+  static_assert((kGroups - 1) * kTile * kTile * 4 <= kLds, "the groups' sums");
+  constexpr auto kernel = &staged_kernel<kTile, kWavesM, kWavesN, kGroups, kF32>;
+  if (const hipError_t e = allow_lds<kernel>(kLds); e != hipSuccess) return e;
+  kernel<<<dim3(static_cast<unsigned>(tiles_m * tiles_n), p.batch), kGroups * kWavesM * kWavesN * 64, kLds, s>>>(
+      p, static_cast<int>(tiles_m), static_cast<int>(tiles_n));
+  return hipGetLastError();
+}
+
 template <bool kF32>
 hipError_t launch(const Fp8Product& p, hipStream_t s) {
-  auto tiles = [](int64_t rows, int64_t by) { return static_cast<unsigned>((rows + by - 1) / by); };
+  auto tiles = [](int64_t rows, int64_t by) { return (rows + by - 1) / by; };
+  // offsets within a tile's rows are held in 32 bits
+  const int64_t longest = std::max(p.a.code_stride, p.b.code_stride);
+  const bool staged = p.k > 0 && p.a.code_stride >= 0 && p.b.code_stride >= 0 && longest * 256 + p.k < (int64_t{1} << 31);
   const int rows = p.m <= 16 ? 16 : p.m <= 32 ? 32 : 64;
-  const dim3 grid(tiles(p.n, 16), tiles(p.m, rows), p.batch);
-  if (rows == 16) thin_kernel<1, 8, kF32><<<grid, 512, 0, s>>>(p);
-  else if (rows == 32) thin_kernel<2, 4, kF32><<<grid, 256, 0, s>>>(p);
-  else thin_kernel<4, 4, kF32><<<grid, 256, 0, s>>>(p);
-  return hipGetLastError();
+  const int64_t pieces = tiles(p.n, 16) * tiles(p.m, rows) * (rows / 16) * p.batch;
+#ifdef VAR
+  const int which = VAR;
+#else
+  const int which = 0;
+#endif
+  if (!staged || which == 1 || (which == 0 && p.m <= 32 && pieces <= 512)) {
+    const dim3 grid(static_cast<unsigned>(tiles(p.n, 16)), static_cast<unsigned>(tiles(p.m, rows)), p.batch);
+    if (rows == 16) thin_kernel<1, 8, kF32><<<grid, 512, 0, s>>>(p);
+    else if (rows == 32) thin_kernel<2, 4, kF32><<<grid, 256, 0, s>>>(p);
+    else thin_kernel<4, 4, kF32><<<grid, 256, 0, s>>>(p);
+    return hipGetLastError();
+  }
+  const int64_t small = tiles(p.m, 64) * tiles(p.n, 64) * p.batch, middle = tiles(p.m, 128) * tiles(p.n, 128) * p.batch;
+  const int64_t wide = tiles(p.m, 256) * tiles(p.n, 256) * p.batch;
+  if (which == 2 || (which == 0 && small <= 512)) return launch_staged<64, 2, 2, 2, kF32>(p, tiles(p.m, 64), tiles(p.n, 64), s);
+  if (which == 3 || (which == 0 && middle <= 256)) return launch_staged<128, 2, 2, 2, kF32>(p, tiles(p.m, 128), tiles(p.n, 128), s);
+  if (which == 5 || (which == 0 && middle > 512 && wide * 4 <= middle + middle / 4))
+    return launch_staged<256, 2, 4, 1, kF32>(p, tiles(p.m, 256), tiles(p.n, 256), s);
+  return launch_staged<128, 2, 2, 1, kF32>(p, tiles(p.m, 128), tiles(p.n, 128), s);
 }
 
 }  // namespace
