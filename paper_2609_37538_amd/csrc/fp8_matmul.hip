@@ -190,7 +190,7 @@ __global__ __launch_bounds__(kGroups * kWavesM * kWavesN * 64, kGroups * kWavesM
   const float* const scales_a = p.a.scales + i * p.a.scale_batch_stride + (tm * kTile + min(wave * 64 + lane, last_a)) * p.a.scale_stride;
   const float* const scales_b =
       p.b.scales + i * p.b.scale_batch_stride + min(tn * kTile / kFp8Block + (lane & 1), (p.n - 1) / kFp8Block) * p.b.scale_stride;
-  auto fetch = [&](int j, int step, int buffer) {
+  auto fetch = [&](int j, int step, unsigned char* to) {
     // (the compiler would keep advancing 64-bit addresses)
     uint32_t row = row_at[j];
     asm volatile("" : "+v"(row));
@@ -199,19 +199,19 @@ __global__ __launch_bounds__(kGroups * kWavesM * kWavesN * 64, kGroups * kWavesM
     if (at >= p.k) from = zero_block;
     __builtin_amdgcn_global_load_lds(
         reinterpret_cast<const __attribute__((address_space(1))) void*>(reinterpret_cast<uint64_t>(from)),
-        (__attribute__((address_space(3))) void*)(lds + buffer * kStage + (j * kWaves + wave) * 1024), 16, 0, 0);
+        (__attribute__((address_space(3))) void*)(to + (j * kWaves + wave) * 1024), 16, 0, 0);
   };
-  auto fetch_scales = [&](int step, int buffer) {
+  auto fetch_scales = [&](int step, unsigned char* to) {
     const int block = min(step, steps - 1);   // (past the end the codes are zeros)
-    const int at = buffer * kStage + kRows * 128;
+    to += kRows * 128;
     if (wave < kTile / 64)
       __builtin_amdgcn_global_load_lds(
           reinterpret_cast<const __attribute__((address_space(1))) void*>(reinterpret_cast<uint64_t>(scales_a + block)),
-          (__attribute__((address_space(3))) void*)(lds + at + wave * 256), 4, 0, 0);
+          (__attribute__((address_space(3))) void*)(to + wave * 256), 4, 0, 0);
     if (wave == kWaveOfB)
       __builtin_amdgcn_global_load_lds(
           reinterpret_cast<const __attribute__((address_space(1))) void*>(reinterpret_cast<uint64_t>(scales_b + block)),
-          (__attribute__((address_space(3))) void*)(lds + at + kTile * 4), 4, 0, 0);
+          (__attribute__((address_space(3))) void*)(to + kTile * 4), 4, 0, 0);
   };
 
   f32x4 sum[kM][kN] = {};
@@ -223,36 +223,44 @@ __global__ __launch_bounds__(kGroups * kWavesM * kWavesN * 64, kGroups * kWavesM
   const unsigned at_scale_a = kRows * 128 + (wave_a + l16) * 4, at_scale_b = kRows * 128 + kTile * 4 + wave_b / kFp8Block * 4;
   // a group's steps follow each other; what it takes past the last step are zeros
   const int steps_here = (steps + kGroups - 1) / kGroups, first_step = group * steps_here;
-#pragma unroll
-  for (int j = 0; j < kLoads; ++j) fetch(j, first_step, 0);
-  fetch_scales(first_step, 0);
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  __syncthreads();
-  for (int step = 0; step < steps_here; ++step) {
-    const int buffer = step & 1, next = first_step + step + 1;
-    const unsigned char* const from = lds + buffer * kStage;
-    u32x4 a[kM][2], b[kN][2];
-    float scale[kM];
+  // What a step reads and what it brings are different buffers.  (`__restrict__` says so: else every read of LDS would
+  // wait for the loads into it.)
+  auto run = [&](const unsigned char* __restrict__ from, unsigned char* __restrict__ to, int next) {
+    u32x4 a[2][2], b[kN][2];
+    float scale[2];
+    auto read_a = [&](auto x) {
+      each<2>([&](auto h) { a[x % 2][h] = *reinterpret_cast<const u32x4*>(from + x * 2048 + (at_a ^ (h * 16))); });
+      scale[x % 2] = *reinterpret_cast<const float*>(from + at_scale_a + x * 64);
+    };
     const float scale_b = *reinterpret_cast<const float*>(from + at_scale_b);
     each<kN>([&](auto y) {
       each<2>([&](auto h) { b[y][h] = *reinterpret_cast<const u32x4*>(from + y * 2048 + (at_b ^ (h * 16))); });
     });
+    read_a(std::integral_constant<int, 0>{});
+    fetch_scales(next, to);
+    constexpr int kEach = (kLoads + kM - 1) / kM;
     each<kM>([&](auto x) {
-      each<2>([&](auto h) { a[x][h] = *reinterpret_cast<const u32x4*>(from + x * 2048 + (at_a ^ (h * 16))); });
-      scale[x] = *reinterpret_cast<const float*>(from + at_scale_a + x * 64);
-    });
-    fetch_scales(next, buffer ^ 1);
-    each<kM>([&](auto x) {
-      each<kLoads / kM + (kLoads % kM != 0)>([&](auto j) {
-        if constexpr (x * (kLoads / kM + (kLoads % kM != 0)) + j < kLoads) fetch(x * (kLoads / kM + (kLoads % kM != 0)) + j, next, buffer ^ 1);
+      if constexpr (x + 1 < kM) read_a(std::integral_constant<int, x + 1>{});
+      each<kEach>([&](auto j) {
+        if constexpr (x * kEach + j < kLoads) fetch(x * kEach + j, next, to);
       });
-      const float s = scale[x] * scale_b;
+      const float s = scale[x % 2] * scale_b;
       each<kN>([&](auto y) {
-        const f32x4 part = multiply(b[y][0], b[y][1], a[x][0], a[x][1]);
+        const f32x4 part = multiply(b[y][0], b[y][1], a[x % 2][0], a[x % 2][1]);
 #pragma unroll
         for (int j = 0; j < 4; ++j) sum[x][y][j] = __builtin_fmaf(part[j], s, sum[x][y][j]);
       });
+      __builtin_amdgcn_sched_barrier(0);
     });
+  };
+#pragma unroll
+  for (int j = 0; j < kLoads; ++j) fetch(j, first_step, lds);
+  fetch_scales(first_step, lds);
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  for (int step = 0; step < steps_here; ++step) {
+    const int buffer = step & 1;
+    run(lds + buffer * kStage, lds + (buffer ^ 1) * kStage, first_step + step + 1);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
   }
