@@ -216,39 +216,49 @@ __global__ __launch_bounds__(kGroups * kWavesM * kWavesN * 64, kGroups * kWavesM
 
   f32x4 sum[kM][kN] = {};
   const int wave_a = wave / kWavesN * (kM * 16), wave_b = wave % kWavesN * (kN * 16);
-  const unsigned at_a = (wave_a + l16) * 128 + ((2 * quad) ^ exchange(l16)) * 16;
-  const unsigned at_b = (kTile + wave_b + l16) * 128 + ((2 * quad) ^ exchange(l16)) * 16;
+    const unsigned at_a = (wave_a + l16) * 128 + (quad ^ exchange(l16)) * 16;
+  const unsigned at_b = (kTile + wave_b + l16) * 128 + (quad ^ exchange(l16)) * 16;
   // a wave's columns are of one block of b's rows
   static_assert(kFp8Block % (kN * 16) == 0);
   const unsigned at_scale_a = kRows * 128 + (wave_a + l16) * 4, at_scale_b = kRows * 128 + kTile * 4 + wave_b / kFp8Block * 4;
   // a group's steps follow each other; what it takes past the last step are zeros
   const int steps_here = (steps + kGroups - 1) / kGroups, first_step = group * steps_here;
+  // The last tile's products of a step are added up in the next one.
+  static_assert(kM % 2 == 0);
+  f32x4 part[2][kN] = {};
+  float prior_scale = 0.0f;
   // What a step reads and what it brings are different buffers.  (`__restrict__` says so: else every read of LDS would
   // wait for the loads into it.)
   auto run = [&](const unsigned char* __restrict__ from, unsigned char* __restrict__ to, int next) {
     u32x4 a[2][2], b[kN][2];
     float scale[2];
     auto read_a = [&](auto x) {
-      each<2>([&](auto h) { a[x % 2][h] = *reinterpret_cast<const u32x4*>(from + x * 2048 + (at_a ^ (h * 16))); });
+      each<2>([&](auto h) { a[x % 2][h] = *reinterpret_cast<const u32x4*>(from + x * 2048 + (at_a ^ (h * 64))); });
       scale[x % 2] = *reinterpret_cast<const float*>(from + at_scale_a + x * 64);
     };
     const float scale_b = *reinterpret_cast<const float*>(from + at_scale_b);
     each<kN>([&](auto y) {
-      each<2>([&](auto h) { b[y][h] = *reinterpret_cast<const u32x4*>(from + y * 2048 + (at_b ^ (h * 16))); });
+      each<2>([&](auto h) { b[y][h] = *reinterpret_cast<const u32x4*>(from + y * 2048 + (at_b ^ (h * 64))); });
     });
     read_a(std::integral_constant<int, 0>{});
     fetch_scales(next, to);
-    constexpr int kEach = (kLoads + kM - 1) / kM;
+    constexpr int kEach = (kLoads + kM - 1) / kM * 2;   // in the first half: spread over all of it took 5% longer
     each<kM>([&](auto x) {
       if constexpr (x + 1 < kM) read_a(std::integral_constant<int, x + 1>{});
       each<kEach>([&](auto j) {
         if constexpr (x * kEach + j < kLoads) fetch(x * kEach + j, next, to);
       });
-      const float s = scale[x % 2] * scale_b;
+      // the products of a tile of a, each followed by the sums of the tile before, whose products are done by then
+      constexpr int kPrior = (x + kM - 1) % kM;
       each<kN>([&](auto y) {
-        const f32x4 part = multiply(b[y][0], b[y][1], a[x % 2][0], a[x % 2][1]);
+        part[x % 2][y] = multiply(b[y][0], b[y][1], a[x % 2][0], a[x % 2][1]);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) sum[x][y][j] = __builtin_fmaf(part[j], s, sum[x][y][j]);
+        for (int j = 0; j < 4; ++j) sum[kPrior][y][j] = __builtin_fmaf(part[(x + 1) % 2][y][j], prior_scale, sum[kPrior][y][j]);
+      });
+      prior_scale = scale[x % 2] * scale_b;
+      each<kN>([&](auto) {
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x2, 4, 0);
       });
       __builtin_amdgcn_sched_barrier(0);
     });
@@ -264,6 +274,10 @@ __global__ __launch_bounds__(kGroups * kWavesM * kWavesN * 64, kGroups * kWavesM
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
   }
+  each<kN>([&](auto y) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sum[kM - 1][y][j] = __builtin_fmaf(part[1][y][j], prior_scale, sum[kM - 1][y][j]);
+  });
   if constexpr (kGroups > 1) {
     f32x4* const sums = reinterpret_cast<f32x4*>(all_lds);
     each<kM>([&](auto x) {
