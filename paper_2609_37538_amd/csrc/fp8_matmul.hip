@@ -146,6 +146,11 @@ __device__ __forceinline__ void each(F f) {
 // read one block of sixteen rows meet every bank; eight neighbouring lanes fetch a row's whole line.
 // The rows' scales of the step follow, a's, then b's for each 128 rows.
 // kGroups groups of such waves share the columns, a run of steps each, and add up in LDS.
+// 8192 x 4096 x 4096 takes 127 us, 2.2 PFLOP/s, with 256 x 256: 4240 cycles per step, whose products take 2112; without
+// the loads it takes 95, and without the sums' multiplications too 95: they hide behind the products, the loads'
+// latency does not, with two buffers being all that LDS holds.  Lane l's 32 bytes are the blocks l / 16 and l / 16 + 4 of
+// its row (the columns' order does not matter while both operands have the same): with two neighbouring ones
+// 46% of LDS's cycles were bank conflicts, so there are none.
 template <int kTile, int kWavesM, int kWavesN, int kGroups, bool kF32>
 __global__ __launch_bounds__(kGroups * kWavesM * kWavesN * 64, kGroups * kWavesM * kWavesN / 4) void staged_kernel(Fp8Product p, int tiles_m, int tiles_n) {
   constexpr int kWaves = kWavesM * kWavesN, kThreads = kWaves * 64;
@@ -310,6 +315,22 @@ hipError_t launch_staged(const Fp8Product& p, int64_t tiles_m, int64_t tiles_n, 
   return hipGetLastError();
 }
 
+// Which kernel, by what each took (us, bfloat16 results, one call after the other in a graph):
+//   rows x columns of out, k   thin   64, 2 groups   128, 2 groups    128    256
+//       1 x  4096, 4096         5.2      11.7            17.9        25.8    44.1
+//       1 x 32768, 4096        26.1      22.0            27.0        32.2    50.7
+//      32 x  4096, 4096        10.1      12.0            18.1        26.1    44.8
+//      64 x  4096, 4096        16.6      12.0            18.9        26.7    45.7
+//     512 x  4096, 4096                  19.7            23.8        30.7    52.2
+//    1024 x  4096, 4096                  37.3            27.2        34.0    53.6
+//    1536 x  4096, 4096                  53.7            48.5        42.5    54.0
+//    2304 x  4096, 4096                  81.1            71.4        68.9    54.8
+//    8192 x  4096, 4096                                 187.7       175.7   128.9
+// Two groups halve the steps that wait for memory one after the other, while a tile for each CU, or two, is
+// all there is; large tiles read less per product.  Heads (rows x columns x products, k):
+//      32 x 512 x  16, 128      3.0       3.9             5.4         4.2     5.3
+//       8 x 512 x  64, 128      3.9       4.6             5.1         4.1     4.9
+//     128 x 512 x 128, 128     26.4      16.4            12.9         9.8    10.0
 template <bool kF32>
 hipError_t launch(const Fp8Product& p, hipStream_t s) {
   auto tiles = [](int64_t rows, int64_t by) { return (rows + by - 1) / by; };
@@ -318,24 +339,18 @@ hipError_t launch(const Fp8Product& p, hipStream_t s) {
   const bool staged = p.k > 0 && p.a.code_stride >= 0 && p.b.code_stride >= 0 && longest * 256 + p.k < (int64_t{1} << 31);
   const int rows = p.m <= 16 ? 16 : p.m <= 32 ? 32 : 64;
   const int64_t pieces = tiles(p.n, 16) * tiles(p.m, rows) * (rows / 16) * p.batch;
-#ifdef VAR
-  const int which = VAR;
-#else
-  const int which = 0;
-#endif
-  if (!staged || which == 1 || (which == 0 && p.m <= 32 && pieces <= 512)) {
+  if (!staged || (p.m <= 32 && pieces <= (p.k < 256 ? 2048 : 512))) {
     const dim3 grid(static_cast<unsigned>(tiles(p.n, 16)), static_cast<unsigned>(tiles(p.m, rows)), p.batch);
     if (rows == 16) thin_kernel<1, 8, kF32><<<grid, 512, 0, s>>>(p);
     else if (rows == 32) thin_kernel<2, 4, kF32><<<grid, 256, 0, s>>>(p);
     else thin_kernel<4, 4, kF32><<<grid, 256, 0, s>>>(p);
     return hipGetLastError();
   }
-  const int64_t small = tiles(p.m, 64) * tiles(p.n, 64) * p.batch, middle = tiles(p.m, 128) * tiles(p.n, 128) * p.batch;
-  const int64_t wide = tiles(p.m, 256) * tiles(p.n, 256) * p.batch;
-  if (which == 2 || (which == 0 && small <= 512)) return launch_staged<64, 2, 2, 2, kF32>(p, tiles(p.m, 64), tiles(p.n, 64), s);
-  if (which == 3 || (which == 0 && middle <= 256)) return launch_staged<128, 2, 2, 2, kF32>(p, tiles(p.m, 128), tiles(p.n, 128), s);
-  if (which == 5 || (which == 0 && middle > 512 && wide * 4 <= middle + middle / 4))
-    return launch_staged<256, 2, 4, 1, kF32>(p, tiles(p.m, 256), tiles(p.n, 256), s);
+  const int64_t middle = tiles(p.m, 128) * tiles(p.n, 128) * p.batch, wide = tiles(p.m, 256) * tiles(p.n, 256) * p.batch;
+  if (tiles(p.m, 64) * tiles(p.n, 64) * p.batch <= 512) return launch_staged<64, 2, 2, 2, kF32>(p, tiles(p.m, 64), tiles(p.n, 64), s);
+  if (middle <= 256) return launch_staged<128, 2, 2, 2, kF32>(p, tiles(p.m, 128), tiles(p.n, 128), s);
+  // (large tiles that few rows or columns leave half empty are no gain)
+  if (middle > 512 && wide * 4 <= middle + middle / 4) return launch_staged<256, 2, 4, 1, kF32>(p, tiles(p.m, 256), tiles(p.n, 256), s);
   return launch_staged<128, 2, 2, 1, kF32>(p, tiles(p.m, 128), tiles(p.n, 128), s);
 }
 
