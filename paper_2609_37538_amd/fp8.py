@@ -74,8 +74,10 @@ def _torch():
 
 
 def _strides(x):
-    """Strides of a tensor, 0 for dimensions of one entry, which do not matter."""
-    return [0 if n <= 1 else s for s, n in zip(x.stride(), x.shape)]
+    """Strides of a tensor, 0 for dimensions of one entry, which do not matter, and of tensors without entries."""
+    if 0 in x.shape:
+        return (0,) * x.dim()
+    return tuple(0 if n == 1 else s for s, n in zip(x.stride(), x.shape))
 
 
 class Fp8:
@@ -83,7 +85,9 @@ class Fp8:
     scales, [..., R, K/128] (rows=1, of activations) or [..., R/128, K/128] (rows=128, of weights), counts
     of blocks rounded up; K a multiple of 16."""
 
-    __slots__ = ("codes", "scales", "rows", "_view")
+    # Small calls cost more time on the host than on the GPU, so what fp8_quantize makes is one allocation
+    # (codes, then scales), and its tensors are made where they are asked for.
+    __slots__ = ("device", "rows", "_shape", "_codes", "_scales", "_base", "_code_strides", "_scale_strides", "_view")
 
     def __init__(self, codes, scales, rows: int = 1):
         torch = _torch()
@@ -93,75 +97,109 @@ class Fp8:
         for x in (codes, scales):
             if x.requires_grad:
                 _L._no_gradient("codes and scales")
-        shape = codes.shape
+        shape = tuple(codes.shape)
         _need(len(shape) in (2, 3) and shape[-1] % 16 == 0, "codes must be [..., R, K] with K a multiple of 16")
         _need(scales.shape == (*shape[:-2], -(-shape[-2] // rows), -(-shape[-1] // AVSG_FP8_BLOCK)),
               "codes and scales must belong together: a scale for each block")
-        self.codes, self.scales, self.rows, self._view = codes, scales, rows, None
+        self.device, self.rows, self._shape = codes.device, rows, shape
+        self._codes, self._scales, self._base, self._view = codes, scales, None, None
 
     @property
     def shape(self):
         """Of the matrix it stands for."""
-        return tuple(self.codes.shape)
+        return self._shape
 
     @property
-    def device(self):
-        return self.codes.device
+    def codes(self):
+        if self._codes is None:
+            flat = self._base[:self._code_bytes()].view(_L._t.float8_e4m3fn)
+            self._codes = flat.as_strided(self._shape, (*self._code_strides, 1))
+        return self._codes
+
+    @property
+    def scales(self):
+        if self._scales is None:
+            shape = (*self._shape[:-2], -(-self._shape[-2] // self.rows), -(-self._shape[-1] // AVSG_FP8_BLOCK))
+            flat = self._base[self._code_bytes():].view(_L._t.float32)
+            self._scales = flat.as_strided(shape, (*self._scale_strides, 1))
+        return self._scales
+
+    def _code_bytes(self) -> int:
+        n = 1
+        for size in self._shape:
+            n *= size
+        return n
 
     def transpose(self, i: int, j: int) -> "Fp8":
         """With two leading dimensions exchanged (the columns stay in place; blocks of 128 rows too)."""
-        n = self.codes.dim()
+        n = len(self._shape)
         _need(i % n != n - 1 and j % n != n - 1, "columns cannot be exchanged: blocks lie along them")
         if i % n == j % n:
             return self
         _need(self.rows == 1, "rows in blocks of 128 cannot be exchanged")
-        return _fp8(self.codes.transpose(i, j), self.scales.transpose(i, j), 1)
+        if self._base is None:
+            return Fp8(self._codes.transpose(i, j), self._scales.transpose(i, j))
+        s, c, b = self._shape, self._code_strides, self._scale_strides
+        return _fp8(self.device, self._base, 1, (s[1], s[0], s[2]), (c[1], c[0]), (b[1], b[0]))
 
     def _c(self) -> AvsgFp8:
         """The matrix as the library takes it; made once, for codes and scales do not move."""
         view = self._view
-        if view is None:
-            codes, scales = self.codes, self.scales
-            at, c, s = codes.data_ptr(), _strides(codes), _strides(scales)
-            if 0 in codes.shape:
-                c = s = [0] * len(c)
-            else:
+        if view is not None:
+            return view
+        if self._base is not None:
+            at, c, s = self._base.data_ptr(), self._code_strides, self._scale_strides
+            scales_at = at + self._code_bytes()
+            view = (AvsgFp8(at, scales_at, c[0], 0, s[0], 0, self.rows) if len(c) == 1
+                    else AvsgFp8(at, scales_at, c[1], c[0], s[1], s[0], self.rows))
+        else:
+            at, c, s = self._codes.data_ptr(), _strides(self._codes), _strides(self._scales)
+            if self._codes.numel():
                 _need(c[-1] == 1 and s[-1] in (0, 1) and not at & 15 and not any(st & 15 for st in c[:-1]),
                       "rows of codes must be contiguous and 16-byte aligned, and a row's scales contiguous")
-            view = AvsgFp8(at, scales.data_ptr(), c[-2], c[0] if len(c) == 3 else 0, s[-2], s[0] if len(s) == 3 else 0, self.rows)
-            self._view = view
+            view = AvsgFp8(at, self._scales.data_ptr(), c[-2], c[0] if len(c) == 3 else 0, s[-2], s[0] if len(s) == 3 else 0, self.rows)
+        self._view = view
         return view
 
 
-def _fp8(codes, scales, rows) -> Fp8:
-    """An Fp8 of tensors that need no checks."""
+def _fp8(device, base, rows, shape, code_strides, scale_strides) -> Fp8:
+    """An Fp8 in one allocation: the codes, then the scales."""
     m = Fp8.__new__(Fp8)
-    m.codes, m.scales, m.rows, m._view = codes, scales, rows, None
+    m.device, m.rows, m._base, m._shape, m._code_strides, m._scale_strides = device, rows, base, shape, code_strides, scale_strides
+    m._codes = m._scales = m._view = None
     return m
 
 
 def _plain(x, dtype, what):
     """(address, row stride, batch stride) of a plain [..., R, K] whose rows are 16-byte aligned."""
-    st, unit = _strides(x), 8 if dtype == _L.AVSG_BF16 else 4
-    if 0 in x.shape:
-        return x.data_ptr(), 0, 0
-    _need(st[-1] == 1 and not x.data_ptr() & 15 and not any(s % unit for s in st[:-1]), f"{what}: rows must be contiguous and 16-byte aligned")
-    return x.data_ptr(), st[-2], st[0] if len(st) == 3 else 0
+    at, shape = x.data_ptr(), x.shape
+    if x.is_contiguous() and not at & 15:
+        # (rows are of multiples of 16 entries)
+        return at, shape[-1], shape[-2] * shape[-1]
+    st, mask = _strides(x), 7 if dtype == _L.AVSG_BF16 else 3
+    if 0 in shape:
+        return at, 0, 0
+    _need(st[-1] == 1 and not at & 15 and not any(s & mask for s in st[:-1]), f"{what}: rows must be contiguous and 16-byte aligned")
+    return at, st[-2], st[0] if len(st) == 3 else 0
 
 
 def fp8_quantize(x, rows: int = 1) -> Fp8:
     """8-bit form of x, [R][K] or [A][R][K] with K a multiple of 16, in bfloat16 or float32: a scale for each
     128 columns of a row (rows=1) or for each block of 128 x 128 (rows=128)."""
-    torch = _torch()
-    dtype, shape, dev = _plain_type(x, "x"), x.shape, x.device
+    torch = _torch() if _lib is None else _L._t
+    dtype, shape, dev = _plain_type(x, "x"), tuple(x.shape), x.device
     _need(len(shape) in (2, 3) and shape[-1] % 16 == 0, "x must be [..., R, K] with K a multiple of 16")
-    _need(rows in (1, AVSG_FP8_BLOCK), f"rows must be 1 or {AVSG_FP8_BLOCK}")
     at, stride, batch_stride = _plain(x, dtype, "x")
-    codes = torch.empty(shape, dtype=torch.float8_e4m3fn, device=dev)
-    scales = torch.empty((*shape[:-2], -(-shape[-2] // rows), -(-shape[-1] // AVSG_FP8_BLOCK)), dtype=torch.float32, device=dev)
-    m = _fp8(codes, scales, rows)
-    batch = shape[0] if len(shape) == 3 else 1
-    _L._run(_lib.avsg_fp8_quantize, "avsg_fp8_quantize", dev.index, at, dtype, batch, shape[-2], shape[-1], stride, batch_stride, m._c())
+    batch, r, k = shape if len(shape) == 3 else (1, *shape)
+    if rows == 1:
+        down = r
+    else:
+        _need(rows == AVSG_FP8_BLOCK, f"rows must be 1 or {AVSG_FP8_BLOCK}")
+        down = -(-r // AVSG_FP8_BLOCK)
+    across = -(-k // AVSG_FP8_BLOCK)
+    base = torch.empty(batch * (r * k + 4 * down * across), dtype=torch.uint8, device=dev)
+    m = _fp8(dev, base, rows, shape, (k,) if len(shape) == 2 else (r * k, k), (across,) if len(shape) == 2 else (down * across, across))
+    _L._run(_lib.avsg_fp8_quantize, "avsg_fp8_quantize", dev.index, at, dtype, batch, r, k, stride, batch_stride, m._c())
     return m
 
 
@@ -179,9 +217,9 @@ def fp8_dequantize(m: Fp8, dtype=None):
 def fp8_matmul(a: Fp8, b: Fp8, out=None, dtype=None):
     """a b^T for a [M][K] with scales per row and b [N][K] with scales per 128 x 128, or for batches of both;
     `out` ([M][N] or [batch][M][N], bfloat16 or float32, rows contiguous) or a new tensor of `dtype` (bfloat16)."""
-    sa, sb, dev = a.codes.shape, b.codes.shape, a.codes.device
+    sa, sb, dev = a._shape, b._shape, a.device
     three = len(sa) == 3
-    if len(sa) != len(sb) or sa[-1] != sb[-1] or dev != b.codes.device or (three and sa[0] != sb[0]):
+    if len(sa) != len(sb) or sa[-1] != sb[-1] or dev != b.device or (three and sa[0] != sb[0]):
         raise ValueError("a and b must have the same dimensions, batch, columns and GPU")
     if a.rows != 1 or b.rows != AVSG_FP8_BLOCK:
         raise ValueError("a must have a scale per 128 columns of a row (rows=1), b per 128 x 128 (rows=128)")

@@ -100,26 +100,14 @@ def _torch():
 
 
 def _codes(x, shape, device, what):
-    """(address, token stride, head stride) of int8 [...][128] codes, whose vectors are read 16 bytes at a time."""
+    """(address, token stride, head stride) of int8 [...][H][128] codes, whose vectors are read 16 bytes at a time."""
     if x.dtype is not _L._t.int8 or x.shape != shape or x.device != device:
         raise ValueError(f"{what} must be an int8 tensor of shape {tuple(shape)} on {device}")
-    return _strided(x, 15, what)
-
-
-def _strided(x, mask, what):
-    """(address, stride of the tokens, ...) of a tensor whose last dimension is contiguous; its leading dimensions but the
-    last one, [B][n_q] or [T], are tokens at equal distances.  `mask`: of strides and, in bytes, of the address."""
-    at, shape = x.data_ptr(), x.shape
-    st = [0 if n <= 1 else s for s, n in zip(x.stride(), shape)]     # strides of dimensions of one entry do not matter
-    if 0 in shape:
-        return at, 0, 0
-    if len(shape) == 4:
-        if shape[1] == 1:
-            st[1] = st[0]
-        elif shape[0] > 1 and st[0] != shape[1] * st[1]:
-            raise ValueError(f"{what}: tokens must lie at equal distances")
-        st = st[1:]
-    if (shape[-1] > 1 and st[-1] != 1) or any(s & mask for s in st[:-1]) or at & 15:
+    at = x.data_ptr()
+    if x.is_contiguous() and not at & 15:
+        return at, shape[-2] * AVSG_KEY_DIM, AVSG_KEY_DIM
+    st = _token_strides(x, what)
+    if x.numel() and (at & 15 or st[-1] != 1 or st[0] & 15 or st[1] & 15):
         raise ValueError(f"{what}: vectors must be contiguous and 16-byte aligned")
     return at, st[0], st[1]
 
@@ -130,18 +118,25 @@ def _weights(x, shape, device, what):
         _L._no_gradient(what)
     if x.dtype is not _L._t.float32 or x.shape != shape or x.device != device:
         raise ValueError(f"{what} must be a float32 tensor of shape {tuple(shape)} on {device}")
+    if x.is_contiguous():
+        return x.data_ptr(), shape[-1]
+    st = _token_strides(x, what, 2)
+    if x.numel() and shape[-1] > 1 and st[-1] != 1:
+        raise ValueError(f"{what}: a token's weights must be contiguous")
+    return x.data_ptr(), st[0]
+
+
+def _token_strides(x, what, inner: int = 3):
+    """Strides of x, 0 for dimensions of one entry, which do not matter; leading dimensions [B][n_q] before the `inner`
+    last ones (of which the first are tokens) are tokens at equal distances."""
+    shape = x.shape
     st = [0 if n <= 1 else s for s, n in zip(x.stride(), shape)]
-    if 0 in shape:
-        return x.data_ptr(), 0
-    if len(shape) == 3:
+    if 0 not in shape and len(shape) > inner:
         if shape[1] == 1:
             st[1] = st[0]
         elif shape[0] > 1 and st[0] != shape[1] * st[1]:
             raise ValueError(f"{what}: tokens must lie at equal distances")
-        st = st[1:]
-    if shape[-1] > 1 and st[-1] != 1:
-        raise ValueError(f"{what}: a token's weights must be contiguous")
-    return x.data_ptr(), st[0]
+    return st[len(shape) - inner:]
 
 
 class KeyCache:
