@@ -14,6 +14,27 @@ typedef int i32x4_at_4 __attribute__((ext_vector_type(4), aligned(4)));
 constexpr int kWaves = 4;      // of a workgroup of scores
 constexpr int kTileKeys = 16;  // keys that a matrix instruction takes
 
+// Whole numbers become doubles without a conversion: as the low words of numbers whose high word is zero, which are
+// the numbers times 2^-1074.  Weights are held times 2^890, so that sums are normal numbers, 2^-184 of what they stand for.
+constexpr double kWeightUnit = 0x1p890, kSumUnit = 0x1p184;
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+// Pairs of words with high words of zero, which the compiler does not know and so keeps.
+template <int kCount>
+struct LowWords {
+  i32x2 pair[kCount];
+  __device__ __forceinline__ LowWords() {
+#pragma unroll
+    for (int j = 0; j < kCount; ++j) {
+      pair[j] = i32x2{0, 0};
+      asm volatile("" : "+v"(pair[j]));
+    }
+  }
+  __device__ __forceinline__ double operator()(int j, int x) {
+    pair[j][0] = x;
+    return __builtin_bit_cast(double, pair[j]);
+  }
+};
+
 struct F64Pair {
   double a, b;
 };
@@ -103,7 +124,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void score_kernel(SelectParams p, i
       for (int i = 0; i < 4; ++i) {
         const int h = x * 16 + quad * 4 + i;
         const float w = weights[min(h, p.heads - 1)];
-        weight[t][x][i] = h < p.heads ? static_cast<double>(w) : 0.0;
+        weight[t][x][i] = h < p.heads ? static_cast<double>(w) * kWeightUnit : 0.0;
       }
     }
   }
@@ -144,6 +165,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void score_kernel(SelectParams p, i
   const bool stores = quad < 2 * kTok && in_token < p.tokens;
   float* const out = p.scores + (static_cast<int64_t>(r - p.r0) * p.tokens + min(in_token, p.tokens - 1)) * p.score_stride;
   float best = -__builtin_inff();   // of a block of more than sixteen positions
+  LowWords<4> low;
   auto meet = [&](const Keys (&pair)[2], int tile) {
     double sum[2 * kTok];
 #pragma unroll
@@ -160,12 +182,12 @@ __global__ __launch_bounds__(kWaves * 64, 2) void score_kernel(SelectParams p, i
 #pragma unroll
         for (int x = 0; x < kTiles; ++x)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) s = __builtin_fma(weight[t][x][i], static_cast<double>(max(dot[x][i], 0)), s);
+          for (int i = 0; i < 4; ++i) s = __builtin_fma(weight[t][x][i], low(i, max(dot[x][i], 0)), s);
       }
     const float scale = my_tile ? pair[1].scale : pair[0].scale;
     const bool there = my_tile ? pair[1].there : pair[0].there;
     // (zeros of either sign are one)
-    float score = static_cast<float>(row_sums<2 * kTok>(sum) * static_cast<double>(scale)) + 0.0f;
+    float score = static_cast<float>(row_sums<2 * kTok>(sum) * kSumUnit * static_cast<double>(scale)) + 0.0f;
     const int key = first_key + (tile + my_tile) * kTileKeys + l16;
     if (!there || !(score == score)) score = -__builtin_inff();
     if (key < p.first || key >= my_seen - p.recent) score = __builtin_inff();
@@ -235,7 +257,7 @@ __global__ __launch_bounds__(kChunkWaves * 64, kTiles > 4 ? 2 : 4) void chunk_ke
       for (int i = 0; i < 4; ++i) {
         const int h = x * 16 + quad * 4 + i;
         const float w = weights[min(h, p.heads - 1)];
-        weight[x][i] = h < p.heads ? static_cast<double>(w) : 0.0;
+        weight[x][i] = h < p.heads ? static_cast<double>(w) * kWeightUnit : 0.0;
       }
     }
   }
@@ -245,14 +267,20 @@ __global__ __launch_bounds__(kChunkWaves * 64, kTiles > 4 ? 2 : 4) void chunk_ke
   i32x4 part;
   float part_scale;
   bool part_there;
+  // (a row's page is looked up a stage before the row is loaded)
+  int page;
+  auto key_of = [&](int stage) { return min(first_key + stage * kStageKeys + my_row, most - 1); };
+  auto page_of = [&](int stage) {
+    const int64_t at = static_cast<int64_t>(r) * p.cache.pages_per_request + (key_of(stage) >> p.cache.page_shift);
+    page = p.cache.table ? p.cache.table[at] : static_cast<int>(at);
+  };
   auto load = [&](int stage) {
-    const int key = min(first_key + stage * kStageKeys + my_row, most - 1);
-    const int64_t at = static_cast<int64_t>(r) * p.cache.pages_per_request + (key >> p.cache.page_shift);
-    const int page = p.cache.table ? p.cache.table[at] : static_cast<int>(at);
+    const int key = key_of(stage);
     part_there = page >= 0 && page < p.cache.pages;
     const uint64_t row = p.cache.base + (part_there ? page * p.cache.page_stride + (key & p.cache.page_mask) * p.cache.row_stride : 0);
     part = load_global<i32x4_at_4>(row + my_part);
     part_scale = load_global<float>(row + kKeyScaleAt);
+    page_of(stage + 1);
   };
   auto leave = [&](int buffer) {
     unsigned char* const to = staged[buffer] + my_row * kStagedRow;
@@ -267,6 +295,8 @@ __global__ __launch_bounds__(kChunkWaves * 64, kTiles > 4 ? 2 : 4) void chunk_ke
   const int shift = p.block_shift;
   float* const out = p.scores + (static_cast<int64_t>(r - p.r0) * p.tokens + in_token) * p.score_stride;
   float best = -__builtin_inff();   // of a block of 128 positions
+  LowWords<4> low;
+  page_of(0);
   load(0);
   leave(0);
   meet_all();
@@ -290,11 +320,11 @@ __global__ __launch_bounds__(kChunkWaves * 64, kTiles > 4 ? 2 : 4) void chunk_ke
 #pragma unroll
         for (int x = 0; x < kTiles; ++x)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) sum[u] = __builtin_fma(weight[x][i], static_cast<double>(max(dot[x][i], 0)), sum[u]);
+          for (int i = 0; i < 4; ++i) sum[u] = __builtin_fma(weight[x][i], low(i, max(dot[x][i], 0)), sum[u]);
       }
       // row i of sixteen lanes gets the sums of tile i: lane l has key l of the stage
       const float scale = *reinterpret_cast<const float*>(from + lane * kStagedRow + kKeyScaleAt);
-      float score = static_cast<float>(row_sums<4>(sum) * static_cast<double>(scale)) + 0.0f;
+      float score = static_cast<float>(row_sums<4>(sum) * kSumUnit * static_cast<double>(scale)) + 0.0f;
       const int key = stage_key + lane;
       if (!(score == score)) score = -__builtin_inff();
       if (key < p.first || key >= seen - p.recent) score = __builtin_inff();
