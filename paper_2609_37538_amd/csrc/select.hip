@@ -364,8 +364,7 @@ constexpr uint32_t kLowest = 0x007fffffu, kHighest = 0xff800000u;   // ordered(-
 
 constexpr int kBins = 2048;
 constexpr int kFew = 512;             // scores of a bin that are compared with each other
-constexpr int kCandidates = 4096;     // scores that are kept from the one pass over all of them
-constexpr int kSample = 4096;
+constexpr uint32_t kSample = 4096, kSampleMost = 16384;   // (by 1024 threads)
 
 // The best blocks of a token, one workgroup per token.  A sample of the scores gives a bound that a few more than those
 // wanted reach; one pass over all scores keeps these; the threshold lies in one of 2048 bins of equal width of
@@ -374,12 +373,12 @@ constexpr int kSample = 4096;
 // Where that does not do (no bound that leaves few enough, as with many equal scores; more wanted than are
 // kept) histograms of all scores' bits narrow the threshold's range down until a bin holds one value or all that is
 // wanted, reading the scores again for each.
-// kMarks: blocks that are marked, and placed, at a time.
-template <int kThreads, int kMarks>
+// kMarks: blocks that are marked, and placed, at a time; kCandidates: scores that are kept from the one pass over all.
+template <int kThreads, int kMarks, uint32_t kCandidates>
 __global__ __launch_bounds__(kThreads) void best_kernel(SelectParams p) {
   constexpr int kWavesHere = kThreads / 64;
   constexpr int kWords = kMarks / 32;
-  static_assert(kBins % kThreads == 0 && kWords % kThreads == 0 && kSample % kThreads == 0);
+  static_assert(kBins % kThreads == 0 && kWords % kThreads == 0);
   __shared__ uint32_t shared[kBins > 3 * kWords ? kBins : 3 * kWords];
   uint32_t *const hist = shared, *const above_marks = shared, *const equal_marks = shared + kWords, *const before_words = shared + 2 * kWords;
   __shared__ uint32_t kept[kCandidates], kept_block[kCandidates];
@@ -479,24 +478,32 @@ __global__ __launch_bounds__(kThreads) void best_kernel(SelectParams p) {
   if (want <= kCandidates) {
     float bound = -FLT_MAX;
     if (seen > kCandidates) {
-      // of the sample as many as are wanted of all, three standard deviations and three more
-      uint32_t k[kSample / kThreads], lo = 0xffffffffu, hi = 0, number = 0, none = 0;
+      // Of the sample as many as are wanted of all, four and a half standard deviations and three more: too few in one
+      // of 300000 tokens.  It is larger where it would not hold 128 of those wanted.
+      constexpr int kMine = kSampleMost / 1024;
+      uint32_t sample = kSample;
+      while (sample < kMine * kThreads && static_cast<uint64_t>(want) * sample < uint64_t{128} * seen) sample *= 2;
+      uint32_t k[kMine], lo = 0xffffffffu, hi = 0, number = 0, none = 0;
 #pragma unroll
-      for (int j = 0; j < kSample / kThreads; ++j) {
-        k[j] = ordered(scores[static_cast<uint64_t>(j * kThreads + tid) * seen / kSample]);
+      for (int j = 0; j < kMine; ++j) {
+        if (j * kThreads >= sample) break;
+        k[j] = ordered(scores[static_cast<uint64_t>(j * kThreads + tid) * seen / sample]);
         const bool in = is_finite(k[j]);
         lo = min(lo, in ? k[j] : 0xffffffffu);
         hi = max(hi, in ? k[j] : 0u);
         number += in;
       }
       reduced(lo, hi, number, none);
-      const float share = static_cast<float>(want) / static_cast<float>(seen) * kSample;
-      const uint32_t rank = static_cast<uint32_t>(share + 3.0f * sqrtf(share) + 3.0f);
+      const float share = static_cast<float>(want) / static_cast<float>(seen) * static_cast<float>(sample);
+      const uint32_t rank = static_cast<uint32_t>(share + 4.5f * sqrtf(share) + 3.0f);
       const Bins bin = bins_of(lo, hi);
       if (rank <= number && bin.fine()) {
         find_bin(rank, [&](auto add) {
 #pragma unroll
-          for (int j = 0; j < kSample / kThreads; ++j) add(bin(k[j]));
+          for (int j = 0; j < kMine; ++j) {
+            if (j * kThreads >= sample) break;
+            add(bin(k[j]));
+          }
         });
         bound = bin.top - static_cast<float>(found[0] + 1) / bin.by;
       }
@@ -710,9 +717,9 @@ hipError_t run_chunk(const SelectParams& p, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <int kThreads, int kMarks>
+template <int kThreads, int kMarks, uint32_t kCandidates>
 hipError_t run_best(const SelectParams& p, hipStream_t s) {
-  best_kernel<kThreads, kMarks><<<dim3(static_cast<unsigned>(p.requests) * p.tokens), kThreads, 0, s>>>(p);
+  best_kernel<kThreads, kMarks, kCandidates><<<dim3(static_cast<unsigned>(p.requests) * p.tokens), kThreads, 0, s>>>(p);
   return hipGetLastError();
 }
 
@@ -739,9 +746,11 @@ hipError_t launch_scores(const SelectParams& p, hipStream_t s) {
 
 hipError_t launch_best(const SelectParams& p, hipStream_t s) {
   const int n = p.longest >> p.block_shift;
-  if (n <= 4096) return run_best<256, 8192>(p, s);
-  if (n <= 16384) return run_best<512, 16384>(p, s);
-  return run_best<1024, 131072>(p, s);
+  const int want = p.topk >> p.block_shift;
+  if (n <= 4096) return run_best<256, 8192, 4096>(p, s);
+  if (n <= 16384 && want <= 2560) return run_best<512, 16384, 4096>(p, s);
+  if (n <= 16384) return run_best<512, 16384, 8192>(p, s);
+  return run_best<1024, 131072, 8192>(p, s);
 }
 
 }  // namespace avsg

@@ -421,3 +421,49 @@ def test_refusals():
     for kw in (dict(topk=129), dict(topk=4, longest=200), dict(topk=6, block=3), dict(topk=4, workspace=torch.zeros(256, dtype=torch.uint8, device=dev))):
         with pytest.raises(A.AvsgError):
             cache.select(q, w, **kw)
+
+
+# ---------------------------------------------------------------------------
+# any scores: one head, one column, so that a row's scale is its score
+# ---------------------------------------------------------------------------
+def with_scores(scores):
+    n = len(scores)
+    pool = torch.zeros(1, n, 132, dtype=torch.uint8)
+    pool[..., 0] = 1
+    pool[0, :, 128:] = scores.float().contiguous().view(n, 1).view(torch.uint8).view(n, 4)
+    q = torch.zeros(1, 1, 1, 128, dtype=torch.int8)
+    q[..., 0] = 1
+    return q, torch.ones(1, 1, 1), pool
+
+
+def shapes(kind, n, g):
+    x = torch.randn(n, generator=g)
+    at = torch.arange(n)
+    return {
+        "normal": lambda: x,
+        "ascending": lambda: x.sort().values, "descending": lambda: x.sort(descending=True).values,
+        "periodic": lambda: torch.where(at % 4 == 0, x + 10, x), "rare": lambda: torch.where(at % 4 == 1, x + 10, x),
+        "outliers": lambda: torch.where(at % 997 == 5, x * 1e38, x), "wide": lambda: x.sign() * torch.exp2(x * 40),
+        "tiny": lambda: x * 1e-44, "few": lambda: (x * 2).round(), "one": lambda: torch.zeros(n), "two": lambda: (at % 3 == 0).float(),
+        "neighbours": lambda: (1.0 + 2.0 ** -23 * torch.randint(0, 50, (n,), generator=g).double()).float(),
+        "infinite": lambda: torch.where(x > 1, math.inf, torch.where(x < -1, -math.inf, x)),
+        "nothing": lambda: torch.where(x > 2, x, math.nan), "late": lambda: torch.where(at > n - 50, x, -math.inf),
+        "close": lambda: 1000.0 + x * 1e-3,
+    }[kind]()
+
+
+@gpu
+@pytest.mark.parametrize("n", [300, 4096, 4097, 9000, 16384, 20001, 70000, 140000])
+@pytest.mark.parametrize("kind", ["normal", "ascending", "descending", "periodic", "rare", "outliers", "wide", "tiny", "few", "one", "two",
+                                  "neighbours", "infinite", "nothing", "late", "close"])
+def test_any_scores(kind, n):
+    g = torch.Generator().manual_seed(n)
+    s = shapes(kind, n, g)
+    q, weights, pool = with_scores(s)
+    cache = S.KeyCache(pool.cuda(), 1)
+    for topk in sorted({1, 63, n // 3, min(2048, n - 1), min(2561, n - 1), min(7000, n - 1), n - 1, n}):
+        for lens in (None, torch.tensor([[n - 17]])):
+            got = cache.select(q.cuda(), weights.cuda(), topk=topk, lens=None if lens is None else lens.cuda())
+            want = R.best(s, n if lens is None else n - 17, topk, 1)
+            assert torch.equal(got[0][0, 0].cpu(), want[0]), (topk, lens)
+            assert torch.equal(got[1][0, 0].cpu(), want[1]), (topk, lens)
