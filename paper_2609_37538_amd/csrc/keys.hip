@@ -6,7 +6,8 @@ namespace avsg {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kPerGroup = kThreads / kLanesPerKey;   // vectors of a workgroup
+constexpr int kPerGroup = kThreads / kLanesPerKey;   // rows of sixteen lanes of a workgroup
+constexpr int kHeadsPerRow = 4;
 static_assert(kLanesPerKey == 16, "a row of lanes per vector");
 
 typedef unsigned int u32x2_at_4 __attribute__((ext_vector_type(2), aligned(4)));
@@ -20,43 +21,43 @@ __device__ __forceinline__ uint32_t row_max(uint32_t x) {
   return x;
 }
 
-// Turns the lane's eight columns of a vector: lane s of sixteen has columns 8s..8s+7, the lanes
-// [first, first + 8) the 64 rotated ones.  t: the cosines and sines of the position.  Every product
-// and sum is rounded to float32, so that the same steps elsewhere give the same codes.
+// Cosines and sines for the lane's columns: lane s of sixteen has columns 8s..8s+7, the lanes [first, first + 8) the 64
+// rotated ones.  Pairs are neighbours (four of them, in the first half of t) or columns i and i + 32 (eight).
 template <bool kHalves>
-__device__ __forceinline__ void turn(float (&x)[8], const float* t, int s, int first) {
+__device__ __forceinline__ void load_turns(f32x4 (&t)[4], const float* angles, int p) {
+  const f32x4* at = reinterpret_cast<const f32x4*>(angles + (kHalves ? 16 * (p & 3) : 8 * p));
+#pragma unroll
+  for (int j = 0; j < (kHalves ? 4 : 2); ++j) t[j] = at[j];
+}
+// Turns the lane's eight columns, p being its place among the eight lanes that do (all sixteen take part in the exchange).
+// Every product and sum is rounded to float32, so that the same steps elsewhere give the same codes.
+template <bool kHalves>
+__device__ __forceinline__ void turn(float (&x)[8], const f32x4 (&t)[4], int p) {
 #pragma clang fp contract(off)
-  const int p = s - first;
   const bool mine = p >= 0 && p < 8;
   if constexpr (kHalves) {
     float other[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) other[j] = __shfl_xor(x[j], 4, 16);   // columns i and i + 32 are four lanes apart
     if (!mine) return;
-    const f32x4* at = reinterpret_cast<const f32x4*>(t + 16 * (p & 3));
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const f32x4 two = at[j];
+    for (int j = 0; j < 4; ++j)
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const float c = two[2 * i], d = two[2 * i + 1], mine_by_c = x[2 * j + i] * c, other_by_d = other[2 * j + i] * d;
+        const float c = t[j][2 * i], d = t[j][2 * i + 1], mine_by_c = x[2 * j + i] * c, other_by_d = other[2 * j + i] * d;
         x[2 * j + i] = p < 4 ? mine_by_c - other_by_d : other_by_d + mine_by_c;
       }
-    }
   } else {
     if (!mine) return;
-    const f32x4* at = reinterpret_cast<const f32x4*>(t + 8 * p);
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const f32x4 two = at[j];
+    for (int j = 0; j < 2; ++j)
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const float a = x[4 * j + 2 * i], b = x[4 * j + 2 * i + 1], c = two[2 * i], d = two[2 * i + 1];
+        const float a = x[4 * j + 2 * i], b = x[4 * j + 2 * i + 1], c = t[j][2 * i], d = t[j][2 * i + 1];
         const float ac = a * c, bd = b * d, ad = a * d, bc = b * c;
         x[4 * j + 2 * i] = ac - bd;
         x[4 * j + 2 * i + 1] = ad + bc;
       }
-    }
   }
 }
 
@@ -79,9 +80,10 @@ __device__ __forceinline__ u32x2 encode(const float (&x)[8], float& scale) {
   return codes;
 }
 
-// Sixteen lanes per vector, eight columns each: the keys of all tokens, then their queries.
+// Sixteen lanes per vector, eight columns each: the keys of all tokens, one each, then kHeadsPerRow queries of a token, which
+// share its angles.  5122 tokens of 64 queries take 28 us, 130 MB at 4.6 TB/s (with a query per row 37).
 template <bool kHalves>
-__global__ __launch_bounds__(kThreads) void append_kernel(KeyAppendParams p) {
+__global__ __launch_bounds__(kThreads) void append_kernel(KeyAppendParams p, int groups) {
   const int s = threadIdx.x % kLanesPerKey;
   int64_t item = static_cast<int64_t>(blockIdx.x) * kPerGroup + threadIdx.x / kLanesPerKey;
   const bool is_key = item < p.tokens;
@@ -89,40 +91,48 @@ __global__ __launch_bounds__(kThreads) void append_kernel(KeyAppendParams p) {
   int head = 0;
   if (!is_key) {
     item -= p.tokens;
-    if (p.heads == 0 || item >= p.tokens * p.heads) return;
-    token = item / p.heads;
-    head = static_cast<int>(item - token * p.heads);
+    if (groups == 0 || item >= p.tokens * groups) return;
+    token = item / groups;
+    head = static_cast<int>(item - token * groups) * kHeadsPerRow;
   }
   const int64_t pos = p.position[token];
   const bool known = pos >= 0 && (p.rope_at < 0 || pos < p.positions);
-  const __bf16* from = p.key + token * p.key_stride;
-  uint64_t row = 0;
-  if (is_key) {
-    const int r = p.request[token];
-    if (!known || r < 0 || r >= p.cache.batch) return;
-    row = cache_row(p.cache, r, pos);
-    if (row == 0) return;
-  } else {
-    from = p.q + token * p.q_token_stride + head * p.q_head_stride;
-  }
-  u32x2 codes{};
-  float scale = 0.0f;
-  if (known) {
-    const bf16x8 v = *reinterpret_cast<const bf16x8*>(from + 8 * s);
+  const int place = s - p.rope_at / 8;   // among the lanes that turn
+  f32x4 turns[4] = {};
+  if (known && p.rope_at >= 0 && place >= 0 && place < 8) load_turns<kHalves>(turns, p.angles + pos * kRope, place);
+  auto codes_of = [&](bf16x8 v, float& scale) {
     float x[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) x[j] = static_cast<float>(v[j]);
-    if (p.rope_at >= 0) turn<kHalves>(x, p.angles + pos * kRope, s, p.rope_at / 8);
-    codes = encode(x, scale);
-  }
+    if (p.rope_at >= 0) turn<kHalves>(x, turns, place);
+    return encode(x, scale);
+  };
   if (is_key) {
+    const int r = p.request[token];
+    if (!known || r < 0 || r >= p.cache.batch) return;
+    const uint64_t row = cache_row(p.cache, r, pos);
+    if (row == 0) return;
+    float scale;
+    const u32x2 codes = codes_of(*reinterpret_cast<const bf16x8*>(p.key + token * p.key_stride + 8 * s), scale);
     store_global<u32x2_at_4>(row + 8 * s, codes);
     if (s == 0) store_global<float>(row + kKeyScaleAt, scale);
-  } else {
-    *reinterpret_cast<u32x2*>(p.q_out + token * p.q_out_token_stride + head * p.q_out_head_stride + 8 * s) = codes;
+    return;
+  }
+  const int most = min(kHeadsPerRow, p.heads - head);
+  bf16x8 v[kHeadsPerRow] = {};
+#pragma unroll
+  for (int h = 0; h < kHeadsPerRow; ++h)
+    if (known && h < most) v[h] = *reinterpret_cast<const bf16x8*>(p.q + token * p.q_token_stride + (head + h) * p.q_head_stride + 8 * s);
+#pragma unroll
+  for (int h = 0; h < kHeadsPerRow; ++h) {
+    if (h >= most) break;
+    u32x2 codes{};
+    float scale = 0.0f;
+    if (known) codes = codes_of(v[h], scale);
+    *reinterpret_cast<u32x2*>(p.q_out + token * p.q_out_token_stride + (head + h) * p.q_out_head_stride + 8 * s) = codes;
     if (s == 0)
-      p.weights_out[token * p.weight_out_stride + head] =
-          !known ? 0.0f : p.weights ? p.weights[token * p.weight_stride + head] * scale : scale;
+      p.weights_out[token * p.weight_out_stride + head + h] =
+          !known ? 0.0f : p.weights ? p.weights[token * p.weight_stride + head + h] * scale : scale;
   }
 }
 
@@ -148,9 +158,10 @@ unsigned groups_of(int64_t vectors) { return static_cast<unsigned>((vectors + kP
 }  // namespace
 
 hipError_t launch_key_append(const KeyAppendParams& p, int rope_style, hipStream_t s) {
-  const dim3 grid(groups_of(p.tokens * (1 + p.heads)));
-  if (rope_style == AVSG_ROPE_HALVES) append_kernel<true><<<grid, kThreads, 0, s>>>(p);
-  else append_kernel<false><<<grid, kThreads, 0, s>>>(p);
+  const int groups = (p.heads + kHeadsPerRow - 1) / kHeadsPerRow;
+  const dim3 grid(groups_of(p.tokens * (1 + groups)));
+  if (rope_style == AVSG_ROPE_HALVES) append_kernel<true><<<grid, kThreads, 0, s>>>(p, groups);
+  else append_kernel<false><<<grid, kThreads, 0, s>>>(p, groups);
   return hipGetLastError();
 }
 
