@@ -223,13 +223,10 @@ __global__ __launch_bounds__(kWaves * 64, 2) void score_kernel(SelectParams p, i
 // they share in LDS, 64 keys at a time, while the next ones are on their way.
 constexpr int kChunkWaves = 8;
 constexpr int kStageKeys = 64;
-// In LDS the eight blocks of 16 bytes of a row are exchanged by three bits of the row, so that the sixteen lanes that read one
-// block of sixteen rows meet every bank.  (With rows of 144 bytes 9% of the time went to bank conflicts.)
-__device__ __forceinline__ int exchange(int row) { return row >> 1 & 7; }
+constexpr int kStagedRow = 144;   // bytes of a row in LDS: its codes, its scale; sixteen rows' sixteen bytes are in banks of their own
 template <int kTiles>
 __global__ __launch_bounds__(kChunkWaves * 64, kTiles > 4 ? 2 : 4) void chunk_kernel(SelectParams p, int run_stages, int runs, int groups) {
-  __shared__ __align__(16) unsigned char staged[2][kStageKeys * kIndexDim];
-  __shared__ float staged_scales[2][kStageKeys];
+  __shared__ __align__(16) unsigned char staged[2][kStageKeys * kStagedRow];
   const int lane = threadIdx.x & 63, l16 = lane & 15, quad = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int run = static_cast<int>(blockIdx.x % runs), rest = static_cast<int>(blockIdx.x / runs);
@@ -249,13 +246,13 @@ __global__ __launch_bounds__(kChunkWaves * 64, kTiles > 4 ? 2 : 4) void chunk_ke
   double weight[kTiles][4];
   {
     const int64_t at = static_cast<int64_t>(r) * p.n_q + p.g0 + in_token;
-    const int8_t* from = p.q + at * p.q_token_stride + quad * 16;
+    const int8_t* from = p.q + at * p.q_token_stride + quad * 32;
     const float* weights = p.weights + at * p.weight_stride;
 #pragma unroll
     for (int x = 0; x < kTiles; ++x) {
       const int8_t* row = from + min(x * 16 + l16, p.heads - 1) * p.q_head_stride;
       q[x][0] = *reinterpret_cast<const i32x4*>(row);
-      q[x][1] = *reinterpret_cast<const i32x4*>(row + 64);
+      q[x][1] = *reinterpret_cast<const i32x4*>(row + 16);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int h = x * 16 + quad * 4 + i;
@@ -286,8 +283,9 @@ __global__ __launch_bounds__(kChunkWaves * 64, kTiles > 4 ? 2 : 4) void chunk_ke
     page_of(stage + 1);
   };
   auto leave = [&](int buffer) {
-    *reinterpret_cast<i32x4*>(staged[buffer] + my_row * kIndexDim + (my_part ^ exchange(my_row) * 16)) = part;
-    if (my_part == 0) staged_scales[buffer][my_row] = part_there ? part_scale : __uint_as_float(0x7fc00000u);
+    unsigned char* const to = staged[buffer] + my_row * kStagedRow;
+    *reinterpret_cast<i32x4*>(to + my_part) = part;
+    if (my_part == 0) *reinterpret_cast<float*>(to + kKeyScaleAt) = part_there ? part_scale : __uint_as_float(0x7fc00000u);
   };
   auto meet_all = [&] {
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
@@ -307,14 +305,13 @@ __global__ __launch_bounds__(kChunkWaves * 64, kTiles > 4 ? 2 : 4) void chunk_ke
     load(stage + 1);
     if (stage_key < seen) {
       const unsigned char* const from = staged[stage & 1];
-      const int mine = l16 * kIndexDim + (quad ^ exchange(l16)) * 16;
       double sum[4];
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         i32x4 keys[2], dot[kTiles];
 #pragma unroll
         for (int h = 0; h < 2; ++h)
-          keys[h] = *reinterpret_cast<const i32x4*>(from + u * kTileKeys * kIndexDim + (mine ^ (h * 64)));
+          keys[h] = *reinterpret_cast<const i32x4*>(from + (u * kTileKeys + l16) * kStagedRow + quad * 32 + h * 16);
 #pragma unroll
         for (int x = 0; x < kTiles; ++x) dot[x] = __builtin_amdgcn_mfma_i32_16x16x64_i8(q[x][0], keys[0], i32x4{}, 0, 0, 0);
 #pragma unroll
@@ -326,7 +323,7 @@ __global__ __launch_bounds__(kChunkWaves * 64, kTiles > 4 ? 2 : 4) void chunk_ke
           for (int i = 0; i < 4; ++i) sum[u] = __builtin_fma(weight[x][i], low(i, max(dot[x][i], 0)), sum[u]);
       }
       // row i of sixteen lanes gets the sums of tile i: lane l has key l of the stage
-      const float scale = staged_scales[stage & 1][lane];
+      const float scale = *reinterpret_cast<const float*>(from + lane * kStagedRow + kKeyScaleAt);
       float score = static_cast<float>(row_sums<4>(sum) * kSumUnit * static_cast<double>(scale)) + 0.0f;
       const int key = stage_key + lane;
       if (!(score == score)) score = -__builtin_inff();
