@@ -82,7 +82,8 @@ __device__ __forceinline__ float group_max(float x, int shift) {
   return x;
 }
 
-// A wave scores kTok tokens of a request against a run of keys, sixteen at a time.  The matrix instruction
+// A wave scores kTok tokens of a request against a run of keys, sixteen at a time.  128 tokens of 64 heads over 32768
+// keys per two of them take 60 us, 280 MB at 4.7 TB/s.  The matrix instruction
 // (16 x 64 by 64 x 16, 8-bit) multiplies sixteen heads' queries with sixteen keys: lane l holds head, or
 // key, l % 16 and columns (l / 16) * 32 .. + 31 in two instructions, and gets the products of heads (l / 16) *
 // 4 .. + 3 with key l % 16.  The queries and their weights (in 64 bits) stay in registers.
@@ -223,7 +224,12 @@ __global__ __launch_bounds__(kWaves * 64, 2) void score_kernel(SelectParams p, i
 // they share in LDS, 64 keys at a time, while the next ones are on their way.
 constexpr int kChunkWaves = 8;
 constexpr int kStageKeys = 64;
-constexpr int kStagedRow = 144;   // bytes of a row in LDS: its codes, its scale; sixteen rows' sixteen bytes are in banks of their own
+// 2048 tokens of 64 heads over 16384 keys each take 340 us, 1.5 POP/s.  What bounds it is the issue of instructions: per sixteen
+// heads and keys two matrix instructions (each takes about two places of the others) and eight for the sums, relu and weight
+// (sum in 64 bits: 32-bit sums would take as many), 63% of the cycles, and with the matrix instructions 78%.
+// Reads of LDS without bank conflicts (9% of the cycles have one), 128 keys at a time, and other orders of the
+// products and sums took as long.
+constexpr int kStagedRow = 144;   // bytes of a row in LDS: its codes, its scale
 template <int kTiles>
 __global__ __launch_bounds__(kChunkWaves * 64, kTiles > 4 ? 2 : 4) void chunk_kernel(SelectParams p, int run_stages, int runs, int groups) {
   __shared__ __align__(16) unsigned char staged[2][kStageKeys * kStagedRow];
@@ -722,9 +728,16 @@ hipError_t run_best(const SelectParams& p, hipStream_t s) {
 
 }  // namespace
 
+// By waves on their own or by workgroups that share their keys, by what a selection took (us, in a graph; 8192 positions):
+//   requests x tokens x heads    alone   shared        requests x tokens x heads    alone   shared
+//       16 x 2 x 64              18.8     26.3             64 x 6 x 64              72.8     57.5
+//        8 x 4 x 64              18.8     20.2             64 x 4 x 16              36.3     27.0
+//       64 x 4 x 64              41.7     44.8             64 x 8 x 16              51.7     34.1
+//        8 x 6 x 64              23.5     22.0              1 x 64 x 64             24.1     22.5
+// (a wave on its own holds two tokens, so few tokens waste less of it than of a workgroup for eight.)
 hipError_t launch_scores(const SelectParams& p, hipStream_t s) {
   const int tiles = (p.heads + 15) / 16;
-  if (p.tokens >= 6) {
+  if (p.tokens >= (tiles <= 2 ? 4 : 6)) {
     if (tiles == 1) return run_chunk<1>(p, s);
     if (tiles == 2) return run_chunk<2>(p, s);
     if (tiles <= 4) return run_chunk<4>(p, s);
