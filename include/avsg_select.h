@@ -40,7 +40,7 @@ extern "C" {
  * request r lies in page p = d_page_table[r * pages_per_request + x / page_rows]
  * (without a table p = r * pages_per_request + x / page_rows) at byte
  * p * page_stride + (x % page_rows) * row_stride of `base`.  Rows and pages
- * out of range are never touched. */
+ * out of range are never written, and never read from. */
 typedef struct avsg_key_cache {
     void *base;               /* device or pinned mapped host memory, 4-byte aligned */
     int64_t pages;            /* pages of the pool */
@@ -106,7 +106,7 @@ typedef struct avsg_selection {
     int64_t q_token_stride, q_head_stride;   /* bytes, multiples of 16 */
     const float *d_weights;   /* [B][n_q][heads] */
     int64_t weight_stride;    /* elements from one token to the next */
-    const int64_t *d_lens;    /* device [B][n_q]: positions a query token may see, or NULL: all of longest */
+    const int64_t *d_lens;    /* device [B][n_q]: positions a query token may see (no more than longest), or NULL: all of longest */
     int32_t *d_index;         /* device [B][n_q][K]: the positions selected, ascending (avsg_step's d_topk) */
     float *d_scores;          /* float32 [B][n_q][K / block]: the selected blocks' scores, or NULL */
 } avsg_selection;
@@ -127,8 +127,9 @@ size_t avsg_select_workspace_least(int32_t longest, int32_t block);
  * positions to see, the selection goes on with the lowest others, and the K entries are
  * distinct positions below `longest` in any case: what avsg_step takes, and what
  * avsg_attend masks by their position.
- * Rows that no token of a request sees are not read.
- * batch * n_q is at most 2^19, or AVSG_E_RANGE. */
+ * Rows that no token of a request sees are not read; in place of a row that does not exist
+ * the pool's first one is read, and counts for nothing.
+ * batch * n_q is at most 2^19 and longest at most 2^30, or AVSG_E_RANGE. */
 avsg_status avsg_select(const avsg_key_cache *cache, const avsg_selection *s, void *d_workspace,
                         size_t workspace_bytes, void *stream);
 

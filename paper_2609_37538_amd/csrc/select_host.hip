@@ -24,8 +24,10 @@ bool codes16(const void* p, int64_t token_stride, int64_t head_stride) {
 // floats of a token's block scores
 int64_t score_floats(int32_t longest, int32_t block) { return (static_cast<int64_t>(longest) / block + 3) & ~int64_t{3}; }
 
+constexpr int32_t kMostPositions = 1 << 30;
+
 bool takes(int32_t longest, int32_t block) {
-  return longest >= 1 && block >= 1 && block <= 128 && (block & (block - 1)) == 0 && longest % block == 0;
+  return longest >= 1 && longest <= kMostPositions && block >= 1 && block <= 128 && (block & (block - 1)) == 0 && longest % block == 0;
 }
 
 // Scores of more tokens than these are worked through in turns, so that they stay in the last cache
@@ -126,6 +128,8 @@ avsg_status avsg_select(const avsg_key_cache* cache, const avsg_selection* a, vo
     return fail(AVSG_E_NOTPOW2, "block must be a power of two, 1 to 128");
   if (a->longest % a->block != 0 || a->topk % a->block != 0)
     return fail(AVSG_E_RANGE, "longest and topk must be multiples of block");
+  // (keys past a run's end are counted in 32 bits)
+  if (a->longest > kMostPositions) return fail(AVSG_E_RANGE, "longest must be at most 2^30");
   if (a->topk > a->longest) return fail(AVSG_E_RANGE, "topk must be at most longest");
   if (a->longest > p.cache.capacity) return fail(AVSG_E_CAPACITY, "longest is more than the rows of a request");
   const int64_t tokens = static_cast<int64_t>(cache->batch) * a->n_q;

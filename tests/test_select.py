@@ -185,6 +185,31 @@ def test_part_of_the_rows(longest):
 
 
 @gpu
+@pytest.mark.parametrize("page", [1, 2, 4, 8, 16])
+@pytest.mark.parametrize("n_q,heads,block", [(1, 16, 1), (2, 40, 1), (3, 100, 32), (9, 8, 1), (6, 64, 128)])
+def test_small_pages(page, n_q, heads, block):
+    """Pages that end inside a tile of keys, some of which do not exist."""
+    g = torch.Generator().manual_seed(page + n_q)
+    pages = 2 * 640 // page
+    q, weights, pool, table = made(g, 2, n_q, heads, pages, page)
+    table[:, ::7] = torch.tensor([[-1], [pages]], dtype=torch.int32)
+    lens = torch.randint(1, 641, (2, n_q), generator=g)
+    kw = dict(topk=256, block=block)
+    check(run(q, weights, pool, table, lens, **kw), R.select(q, weights, pool, table, lens, **kw))
+
+
+@gpu
+@pytest.mark.parametrize("n", [1, 15, 17, 100, 1001])
+def test_one_page_of_any_rows(n):
+    """Rows of one page per request whose number is no multiple of a tile, up to the pool's last byte."""
+    g = torch.Generator().manual_seed(n)
+    q, weights, pool, _ = made(g, 3, 2, 20, 3, n, table=False)
+    check(run(q, weights, pool, None, None, topk=min(n, 50)), R.select(q, weights, pool, None, None, topk=min(n, 50)))
+    q, weights, pool, _ = made(g, 2, 7, 20, 2, n, table=False)
+    check(run(q, weights, pool, None, None, topk=min(n, 50)), R.select(q, weights, pool, None, None, topk=min(n, 50)))
+
+
+@gpu
 def test_rows_that_no_token_sees_are_not_read():
     """What lies past the lengths does not matter: NaN scales there, and pages that do not exist."""
     g = torch.Generator().manual_seed(11)

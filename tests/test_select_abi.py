@@ -97,7 +97,7 @@ def test_caches_refused(bad, want):
     (dict(first=-1), A.AVSG_E_INVAL), (dict(recent=-1), A.AVSG_E_INVAL), (dict(d_q=0), A.AVSG_E_INVAL), (dict(d_q=4104), A.AVSG_E_INVAL),
     (dict(q_head_stride=120), A.AVSG_E_INVAL), (dict(q_token_stride=8), A.AVSG_E_INVAL), (dict(d_weights=0), A.AVSG_E_INVAL),
     (dict(d_weights=4097), A.AVSG_E_INVAL), (dict(d_index=0), A.AVSG_E_INVAL), (dict(d_scores=4098), A.AVSG_E_INVAL),
-    (dict(n_q=2 ** 19), A.AVSG_E_RANGE)])
+    (dict(n_q=2 ** 19), A.AVSG_E_RANGE), (dict(longest=2 ** 30 + 1), A.AVSG_E_RANGE)])
 def test_selections_refused(bad, want):
     assert status(S.avsg_select, cache(), selection(**bad), 4096, 1 << 20) == want
 
@@ -112,7 +112,7 @@ def test_workspaces():
     assert S.avsg_select_workspace_bytes(1, 1, 2 ** 30, 1) == 2 ** 32      # never less than a token's
     for bad in ((0, 1, 256, 1), (1, 0, 256, 1), (1, 1, 0, 1), (1, 1, 256, 3), (1, 1, 250, 4)):
         assert S.avsg_select_workspace_bytes(*bad) == 0
-    assert S.avsg_select_workspace_least(-1, 1) == 0 and S.avsg_select_workspace_least(256, 256) == 0
+    assert S.avsg_select_workspace_least(2 ** 30 + 1, 1) == 0 and S.avsg_select_workspace_least(-1, 1) == 0 and S.avsg_select_workspace_least(256, 256) == 0
 
 
 def test_empty_calls_take_nothing():
