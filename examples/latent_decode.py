@@ -8,11 +8,12 @@ host memory in 4-bit form, on one GPU:
     attend      all heads over the slots, 4-bit rows read as they are
     outputs --quantise--> per-head values, output projection
 
-Weights are random and the selection is a stand-in for an indexer (recent rows
+Weights are random.  The selection is that of an indexer over 8-bit keys on the device, whose
+projections are products of 8-bit matrices (--index-heads), or a stand-in for one (recent rows
 and a slowly changing random set).  With draft tokens (n_q > 1) the verified length
 goes to the step, which drops the drafts' rows when it is done.
 
-    python examples/latent_decode.py [--batch 16] [--heads 64] [--steps 32]
+    python examples/latent_decode.py [--batch 16] [--heads 64] [--steps 32] [--index-heads 64]
 """
 from __future__ import annotations
 
@@ -25,7 +26,9 @@ import torch
 
 sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 from paper_2609_37538_amd import avsg as A  # noqa: E402
+from paper_2609_37538_amd import fp8 as F  # noqa: E402
 from paper_2609_37538_amd import latent as L  # noqa: E402
+from paper_2609_37538_amd import selection as S  # noqa: E402
 
 NOPE, ROPE, LATENT, VALUE = 128, L.AVSG_ROPE_DIM, L.AVSG_LATENT_DIM, 128
 
@@ -33,7 +36,7 @@ NOPE, ROPE, LATENT, VALUE = 128, L.AVSG_ROPE_DIM, L.AVSG_LATENT_DIM, 128
 class Layer:
     """Weights, the host's rows and the slots of one layer."""
 
-    def __init__(self, batch, n_q, heads, hidden, topk, slots, context, seed=0, device="cuda"):
+    def __init__(self, batch, n_q, heads, hidden, topk, slots, context, seed=0, device="cuda", index_heads=0):
         self.batch, self.n_q, self.heads, self.topk, self.context = batch, n_q, heads, topk, context
         self.device = torch.device(device, torch.cuda.current_device())
         self.random = g = torch.Generator(self.device).manual_seed(seed)
@@ -59,13 +62,42 @@ class Layer:
         self.slots = L.LatentCache.of_slots(self.op)
         self.request = torch.arange(batch, dtype=torch.int32, device=self.device).repeat_interleave(n_q)
         self.scale = (NOPE + ROPE) ** -0.5
+        self.index_heads = index_heads
+        if index_heads:
+            def weight8(*shape):
+                w = torch.randn(*shape, generator=g, device=self.device) * shape[-1] ** -0.5
+                return F.fp8_quantize(w.to(torch.bfloat16), rows=F.AVSG_FP8_BLOCK)
+
+            self.w_index_query = weight8(index_heads * S.AVSG_KEY_DIM, hidden)
+            self.w_index_key = weight8(S.AVSG_KEY_DIM, hidden)
+            self.w_index_weight = weight8(index_heads, hidden)
+            self.keys = S.KeyCache(torch.zeros(batch, context, S.AVSG_KEY_ROW_BYTES, dtype=torch.uint8, device=self.device), batch)
+
+    def index(self, hidden_states, verified):
+        """Keys of hidden_states [batch][n_q][hidden] into the key cache, and the topk positions that each token selects."""
+        batch, n_q, hidden = hidden_states.shape
+        tokens, heads = batch * n_q, self.index_heads
+        position = (verified[:, None] - 1 + torch.arange(n_q, device=self.device)).reshape(-1)
+        x = F.fp8_quantize(hidden_states.reshape(tokens, hidden))
+        query = F.fp8_matmul(x, self.w_index_query).view(tokens, heads, S.AVSG_KEY_DIM)
+        weights = F.fp8_matmul(x, self.w_index_weight, dtype=torch.float32)
+        codes = torch.empty(tokens, heads, S.AVSG_KEY_DIM, dtype=torch.int8, device=self.device)
+        scaled = torch.empty(tokens, heads, device=self.device)
+        self.keys.append(F.fp8_matmul(x, self.w_index_key), self.request, position, self.angles, q=query, weights=weights,
+                         q_out=codes, weights_out=scaled)
+        selected, _ = self.keys.select(codes.view(batch, n_q, heads, -1), scaled.view(batch, n_q, heads), topk=self.topk,
+                                       lens=(position + 1).view(batch, n_q), recent=1)
+        return selected
 
     def prefill(self, request, hidden_states):
         """Rows of one request's hidden_states [length][hidden] into the host's rows from position 0."""
         length = len(hidden_states)
         rows = L.mx4_matmul(L.mx4_quantize(hidden_states), self.w_row)
         requests = torch.full((length,), request, dtype=torch.int32, device=self.device)
-        self.host.append(rows[:, :LATENT], rows[:, LATENT:], requests, torch.arange(length, device=self.device), self.angles)
+        places = torch.arange(length, device=self.device)
+        self.host.append(rows[:, :LATENT], rows[:, LATENT:], requests, places, self.angles)
+        if self.index_heads:
+            self.keys.append(F.fp8_matmul(F.fp8_quantize(hidden_states), self.w_index_key), requests, places, self.angles)
 
     def step(self, hidden_states, verified, selected):
         """Outputs [batch][n_q][hidden] of hidden_states [batch][n_q][hidden], whose tokens stand at
@@ -113,10 +145,10 @@ class Layer:
 def main():
     ap = argparse.ArgumentParser(description=__doc__.split("\n\n")[0])
     for name, value in (("batch", 16), ("n-q", 2), ("heads", 64), ("hidden", 2048), ("topk", 2048), ("slots", 8192),
-                        ("context", 16384), ("prompt", 8192), ("steps", 32)):
+                        ("context", 16384), ("prompt", 8192), ("steps", 32), ("index-heads", 0)):
         ap.add_argument(f"--{name}", type=int, default=value)
     args = ap.parse_args()
-    layer = Layer(args.batch, args.n_q, args.heads, args.hidden, args.topk, args.slots, args.context)
+    layer = Layer(args.batch, args.n_q, args.heads, args.hidden, args.topk, args.slots, args.context, index_heads=args.index_heads)
     g = layer.random
     for request in range(args.batch):
         layer.prefill(request, torch.randn(args.prompt, args.hidden, generator=g, device=layer.device, dtype=torch.bfloat16))
@@ -129,10 +161,10 @@ def main():
         verified = verified + 1 + accepted     # the last step's drafts that were right, and a new token
         fresh = torch.rand(taste.shape, generator=g, device=layer.device)
         taste = torch.where(torch.rand(taste.shape, generator=g, device=layer.device) < 0.9, taste, fresh)
-        selected = layer.select(verified, taste)
+        selected = None if args.index_heads else layer.select(verified, taste)
         torch.cuda.synchronize()
         start = time.perf_counter()
-        layer.step(x, verified, selected)
+        layer.step(x, verified, layer.index(x, verified) if args.index_heads else selected)
         torch.cuda.synchronize()
         times.append((time.perf_counter() - start) * 1e6)
     stats = layer.op.stats()
