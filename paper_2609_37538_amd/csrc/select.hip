@@ -479,8 +479,11 @@ __global__ __launch_bounds__(kThreads) void best_kernel(SelectParams p) {
   bool done = false;
   uint32_t candidates = 0;
   if (want <= kCandidates) {
-    float bound = -FLT_MAX;
-    if (seen > kCandidates) {
+    // few are all kept
+    const bool all = seen <= kCandidates;
+    candidates = seen;
+    if (!all) {
+      float bound = -FLT_MAX;
       // Of the sample as many as are wanted of all, four and a half standard deviations and three more: too few in one
       // of 300000 tokens.  It is larger where it would not hold 128 of those wanted.
       constexpr int kMine = kSampleMost / 1024;
@@ -510,50 +513,54 @@ __global__ __launch_bounds__(kThreads) void best_kernel(SelectParams p) {
         });
         bound = bin.top - static_cast<float>(found[0] + 1) / bin.by;
       }
+      // where it is reached, in no order: 32 scores of a thread at a time, as bits
+      if (tid == 0) count = 0;
+      __syncthreads();
+      for (uint32_t at = 0; at < seen; at += kThreads * 32) {
+        f32x4 x[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          if (at + j * kThreads * 4 >= seen) break;
+          x[j] = *reinterpret_cast<const f32x4*>(scores + min(at + (j * kThreads + tid) * 4, (seen - 1) & ~3u));
+        }
+        uint32_t hits = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          if (at + j * kThreads * 4 >= seen) break;
+          const uint32_t i = at + (j * kThreads + tid) * 4, left = i < seen ? seen - i : 0;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) hits |= x[j][e] >= bound ? 1u << (4 * j + e) : 0;
+          if (left < 4) hits &= ~(15u << (4 * j)) | ((1u << left) - 1) << (4 * j);
+        }
+        const uint32_t mine = __popc(hits), with_me = wave_inclusive_scan(mine);
+        uint32_t to = 0;
+        if (lane == 63 && with_me) to = atomicAdd(&count, with_me);
+        to = __builtin_amdgcn_readlane(to, 63) + with_me - mine;
+        while (hits) {
+          const int b = __ffs(static_cast<int>(hits)) - 1;
+          hits &= hits - 1;
+          if (to < kCandidates) kept_block[to] = at + (b / 4 * kThreads + tid) * 4 + b % 4;
+          ++to;
+        }
+      }
+      __syncthreads();
+      candidates = count;
     }
-    // where it is reached, in no order: 32 scores of a thread at a time, as bits
-    if (tid == 0) count = 0;
-    __syncthreads();
-    for (uint32_t at = 0; at < seen; at += kThreads * 32) {
-      f32x4 x[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        if (at + j * kThreads * 4 >= seen) break;
-        x[j] = *reinterpret_cast<const f32x4*>(scores + min(at + (j * kThreads + tid) * 4, (seen - 1) & ~3u));
-      }
-      uint32_t hits = 0;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        if (at + j * kThreads * 4 >= seen) break;
-        const uint32_t i = at + (j * kThreads + tid) * 4, left = i < seen ? seen - i : 0;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) hits |= x[j][e] >= bound ? 1u << (4 * j + e) : 0;
-        if (left < 4) hits &= ~(15u << (4 * j)) | ((1u << left) - 1) << (4 * j);
-      }
-      const uint32_t mine = __popc(hits), with_me = wave_inclusive_scan(mine);
-      uint32_t to = 0;
-      if (lane == 63 && with_me) to = atomicAdd(&count, with_me);
-      to = __builtin_amdgcn_readlane(to, 63) + with_me - mine;
-      while (hits) {
-        const int b = __ffs(static_cast<int>(hits)) - 1;
-        hits &= hits - 1;
-        if (to < kCandidates) kept_block[to] = at + (b / 4 * kThreads + tid) * 4 + b % 4;
-        ++to;
-      }
-    }
-    __syncthreads();
-    candidates = count;
     if (candidates >= want && candidates <= kCandidates) {
-      uint32_t lo = 0xffffffffu, hi = 0, infinite = 0, none = 0;
+      uint32_t lo = 0xffffffffu, hi = 0, infinite = 0, number = 0;
       for (uint32_t i = tid; i < candidates; i += kThreads) {
-        const uint32_t k = ordered(scores[kept_block[i]]);
+        if (all) kept_block[i] = i;
+        const uint32_t k = ordered(scores[all ? i : kept_block[i]]);
         kept[i] = k;
+        number += k > kLowest;
         lo = min(lo, is_finite(k) ? k : 0xffffffffu);
         hi = max(hi, is_finite(k) ? k : 0u);
         infinite += k == kHighest;
       }
-      reduced(lo, hi, infinite, none);
-      if (infinite >= want) {
+      reduced(lo, hi, infinite, number);
+      if (number < want) {
+        // (then some of those at minus infinity are wanted)
+      } else if (infinite >= want) {
         threshold = kHighest, need = want, done = true;
       } else if (const Bins bin = bins_of(lo, hi); bin.fine()) {
         need = want - infinite;
