@@ -155,7 +155,8 @@ class Fp8:
         else:
             at, c, s = self._codes.data_ptr(), _strides(self._codes), _strides(self._scales)
             if self._codes.numel():
-                _need(c[-1] == 1 and s[-1] in (0, 1) and not at & 15 and not any(st & 15 for st in c[:-1]),
+                # (one scale that stands for several blocks of a row does not lie where the kernels read the others')
+                _need(c[-1] == 1 and (s[-1] == 1 or self._scales.shape[-1] == 1) and not at & 15 and not any(st & 15 for st in c[:-1]),
                       "rows of codes must be contiguous and 16-byte aligned, and a row's scales contiguous")
             view = AvsgFp8(at, self._scales.data_ptr(), c[-2], c[0] if len(c) == 3 else 0, s[-2], s[0] if len(s) == 3 else 0, self.rows)
         self._view = view
