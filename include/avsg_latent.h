@@ -24,8 +24,9 @@
  * asynchronous on the given stream and never throw, abort or allocate, and can
  * be captured into a HIP graph (they enqueue kernels only).  They keep no state,
  * so calls on different streams are independent as long as their outputs and
- * workspaces are.  avsg_latent_last_error() describes the calling thread's last
- * failure.
+ * workspaces are.  Entries of an output must not share memory (strides are not checked
+ * for that): which of their values stays is left to chance.
+ * avsg_latent_last_error() describes the calling thread's last failure.
  */
 #ifndef AVSG_LATENT_H
 #define AVSG_LATENT_H

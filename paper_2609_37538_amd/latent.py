@@ -205,6 +205,32 @@ def _vectors(x, shape, device, what):
     return at, strides
 
 
+def _apart(n0: int, s0: int, n1: int, s1: int, run: int) -> bool:
+    """Whether n0 x n1 vectors of `run` entries, s0 and s1 entries apart, share none."""
+    if n0 <= 1 or n1 <= 1 or run <= 0:
+        n, s = (n0, s0) if n1 == 1 else (n1, s1) if n0 == 1 else (0, 0)
+        return n <= 1 or s >= run
+    if s0 < s1:
+        n0, s0, n1, s1 = n1, s1, n0, s0
+    if s1 < run:
+        return False
+    last = (n1 - 1) * s1
+    if s0 < last + run:
+        # vectors of one dimension lie between those of the other
+        for j in range(1, min(n0, (last + run - 1) // s0 + 1)):
+            i = min(j * s0 // s1, n1 - 1)
+            if j * s0 - i * s1 < run or (i + 1 < n1 and (i + 1) * s1 - j * s0 < run):
+                return False
+    return True
+
+
+def _outputs(x, what: str, n0: int, s0: int, n1: int, s1: int, run: int) -> None:
+    """Refuses a tensor to write to of which several entries are one place in memory: which of their values stays is
+    left to chance."""
+    if not x.is_contiguous() and not _apart(n0, s0, n1, s1, run):
+        raise ValueError(f"{what}: entries must not share memory")
+
+
 def _tokens(x, shape, device, what):
     """(address, token stride, head stride) of a [B][n_q][H][...] tensor whose tokens lie at equal distances."""
     at, (sb, st, sh, _) = _vectors(x, shape, device, what)
@@ -286,6 +312,7 @@ class LatentCache:
             shape = (t, q_rope.shape[1], AVSG_ROPE_DIM)
             qa, qs = _vectors(q_rope, shape, dev, "q_rope")
             oa, os_ = _vectors(q_out, shape, dev, "q_out")
+            _outputs(q_out, "q_out", t, os_[0], shape[1], os_[1], AVSG_ROPE_DIM)
             a = AvsgAppend(t, la, ls[0], ra, rs[0], req, pos, ang, turns, style, shape[1], qa, qs[0], qs[1], oa, os_[0], os_[1])
         _run(_lib.avsg_kv_append, "avsg_kv_append", dev.index, self.c, a)
 
@@ -297,6 +324,7 @@ class LatentCache:
         if out is None:
             out = _t.empty((n, KEY_DIM), dtype=_t.bfloat16, device=dev)
         at, st = _vectors(out, (n, KEY_DIM), dev, "out")
+        _outputs(out, "out", n, st[0], 1, 0, KEY_DIM)
         _run(_lib.avsg_kv_read, "avsg_kv_read", dev.index, self.c, n, req, pos, at, st[0])
         return out
 
@@ -331,6 +359,7 @@ class LatentCache:
             oa, ot, oh = out.data_ptr(), heads * AVSG_LATENT_DIM, AVSG_LATENT_DIM
         else:
             oa, ot, oh = _tokens(out, (b, n_q, heads, AVSG_LATENT_DIM), dev, "out")
+            _outputs(out, "out", b * n_q, ot, heads, oh, AVSG_LATENT_DIM)
         if lse is None:
             lse = _t.empty((b, n_q, heads), dtype=_t.float32, device=dev)
             lse_at = lse.data_ptr()
@@ -500,6 +529,7 @@ def mx4_matmul(a: Mx4, b: Mx4, out=None, dtype=None):
     if out.shape != shape or out.device != dev or (shape[-1] > 1 and st[-1] != 1):
         raise ValueError(f"out must be {shape} on {dev} with contiguous rows")
     kind = _plain_type(out, "out")
+    _outputs(out, "out", sa[0] if three else 1, st[0], shape[-2], st[-2], shape[-1])
     _run(_lib.avsg_mx4_matmul, "avsg_mx4_matmul", dev.index, a._c(), b._c(), sa[0] if three else 1, shape[-2], shape[-1],
          sa[-1], out.data_ptr(), kind, st[-2], st[0] if three else 0)
     return out
