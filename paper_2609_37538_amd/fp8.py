@@ -187,7 +187,7 @@ def _plain(x, dtype, what):
 def fp8_quantize(x, rows: int = 1) -> Fp8:
     """8-bit form of x, [R][K] or [A][R][K] with K a multiple of 16, in bfloat16 or float32: a scale for each
     128 columns of a row (rows=1) or for each block of 128 x 128 (rows=128)."""
-    torch = _torch() if _lib is None else _L._t
+    torch = _torch() if _lib is None or _L._t is None else _L._t
     dtype, shape, dev = _plain_type(x, "x"), tuple(x.shape), x.device
     _need(len(shape) in (2, 3) and shape[-1] % 16 == 0, "x must be [..., R, K] with K a multiple of 16")
     at, stride, batch_stride = _plain(x, dtype, "x")
