@@ -90,4 +90,11 @@ avsg_status avsg_fp8_matmul(const avsg_fp8* a, const avsg_fp8* b, int32_t batch,
   return launched(launch_fp8_matmul(p, static_cast<hipStream_t>(stream)), "avsg_fp8_matmul");
 }
 
+int32_t avsg_internal_fp8_plan(int32_t batch, int32_t m, int32_t n, int32_t k, int64_t a_stride, int64_t b_stride) {
+  Fp8Product p{};
+  p.batch = batch, p.m = m, p.n = n, p.k = k;
+  p.a.code_stride = a_stride, p.b.code_stride = b_stride;
+  return static_cast<int32_t>(fp8_plan(p));
+}
+
 }  // extern "C"

@@ -45,8 +45,24 @@ constexpr int64_t fp8_groups(int64_t rows, int64_t cols, int32_t block_rows) {
                          : (rows + kFp8Block - 1) / kFp8Block * across;
 }
 
+// How a product is carried out.
+enum class Fp8Kernel {
+  k16Rows,          // up to 16 rows of a per workgroup, b streamed past them
+  k32Rows,          // up to 32
+  k64Rows,          // up to 64: what rows too far apart for 32-bit offsets take
+  k64TwoGroups,     // tiles of 64 x 64 staged through LDS, two groups of waves that share the columns
+  k128TwoGroups,    // tiles of 128 x 128, likewise
+  k128,             // tiles of 128 x 128
+  k256,             // tiles of 256 x 256
+};
+
 hipError_t launch_fp8_quantize(const Fp8Convert& c, bool f32, hipStream_t s);
 hipError_t launch_fp8_dequantize(const Fp8Convert& c, bool f32, hipStream_t s);
+// the kernel of a product, by its sizes and its operands' strides
+Fp8Kernel fp8_plan(const Fp8Product& p);
 hipError_t launch_fp8_matmul(const Fp8Product& p, hipStream_t s);
 
 }  // namespace avsg
+
+// fp8_plan for tests, which assert what their cases run.  Not part of the ABI.
+extern "C" int32_t avsg_internal_fp8_plan(int32_t batch, int32_t m, int32_t n, int32_t k, int64_t a_stride, int64_t b_stride);

@@ -221,7 +221,7 @@ __global__ __launch_bounds__(kGroups * kWavesM * kWavesN * 64, kGroups * kWavesM
 
   f32x4 sum[kM][kN] = {};
   const int wave_a = wave / kWavesN * (kM * 16), wave_b = wave % kWavesN * (kN * 16);
-    const unsigned at_a = (wave_a + l16) * 128 + (quad ^ exchange(l16)) * 16;
+  const unsigned at_a = (wave_a + l16) * 128 + (quad ^ exchange(l16)) * 16;
   const unsigned at_b = (kTile + wave_b + l16) * 128 + (quad ^ exchange(l16)) * 16;
   // a wave's columns are of one block of b's rows
   static_assert(kFp8Block % (kN * 16) == 0);
@@ -303,17 +303,43 @@ __global__ __launch_bounds__(kGroups * kWavesM * kWavesN * 64, kGroups * kWavesM
   });
 }
 
+int64_t tiles_of(int64_t rows, int64_t by) { return (rows + by - 1) / by; }
+
+template <int kRowTiles, int kWaves, bool kF32>
+hipError_t launch_thin(const Fp8Product& p, hipStream_t s) {
+  const dim3 grid(static_cast<unsigned>(tiles_of(p.n, 16)), static_cast<unsigned>(tiles_of(p.m, kRowTiles * 16)), p.batch);
+  thin_kernel<kRowTiles, kWaves, kF32><<<grid, kWaves * 64, 0, s>>>(p);
+  return hipGetLastError();
+}
+
 template <int kTile, int kWavesM, int kWavesN, int kGroups, bool kF32>
-hipError_t launch_staged(const Fp8Product& p, int64_t tiles_m, int64_t tiles_n, hipStream_t s) {
+hipError_t launch_staged(const Fp8Product& p, hipStream_t s) {
   constexpr int kLds = kGroups * 2 * (2 * kTile * 128 + (kTile / 64 + 1) * 256);
   static_assert(kLds <= 160 * 1024, "LDS of a workgroup");
   static_assert((kGroups - 1) * kTile * kTile * 4 <= kLds, "the groups' sums");
   constexpr auto kernel = &staged_kernel<kTile, kWavesM, kWavesN, kGroups, kF32>;
   if (const hipError_t e = allow_lds<kernel>(kLds); e != hipSuccess) return e;
+  const int64_t tiles_m = tiles_of(p.m, kTile), tiles_n = tiles_of(p.n, kTile);
   kernel<<<dim3(static_cast<unsigned>(tiles_m * tiles_n), p.batch), kGroups * kWavesM * kWavesN * 64, kLds, s>>>(
       p, static_cast<int>(tiles_m), static_cast<int>(tiles_n));
   return hipGetLastError();
 }
+
+template <bool kF32>
+hipError_t launch(const Fp8Product& p, hipStream_t s) {
+  switch (fp8_plan(p)) {
+    case Fp8Kernel::k16Rows: return launch_thin<1, 8, kF32>(p, s);
+    case Fp8Kernel::k32Rows: return launch_thin<2, 4, kF32>(p, s);
+    case Fp8Kernel::k64Rows: return launch_thin<4, 4, kF32>(p, s);
+    case Fp8Kernel::k64TwoGroups: return launch_staged<64, 2, 2, 2, kF32>(p, s);
+    case Fp8Kernel::k128TwoGroups: return launch_staged<128, 2, 2, 2, kF32>(p, s);
+    case Fp8Kernel::k128: return launch_staged<128, 2, 2, 1, kF32>(p, s);
+    case Fp8Kernel::k256: return launch_staged<256, 2, 4, 1, kF32>(p, s);
+  }
+  return hipErrorInvalidValue;
+}
+
+}  // namespace
 
 // Which kernel, by what each took (us, bfloat16 results, one call after the other in a graph):
 //   rows x columns of out, k   thin   64, 2 groups   128, 2 groups    128    256
@@ -331,30 +357,20 @@ hipError_t launch_staged(const Fp8Product& p, int64_t tiles_m, int64_t tiles_n, 
 //      32 x 512 x  16, 128      3.0       3.9             5.4         4.2     5.3
 //       8 x 512 x  64, 128      3.9       4.6             5.1         4.1     4.9
 //     128 x 512 x 128, 128     26.4      16.4            12.9         9.8    10.0
-template <bool kF32>
-hipError_t launch(const Fp8Product& p, hipStream_t s) {
-  auto tiles = [](int64_t rows, int64_t by) { return (rows + by - 1) / by; };
+Fp8Kernel fp8_plan(const Fp8Product& p) {
   // offsets within a tile's rows are held in 32 bits
   const int64_t longest = std::max(p.a.code_stride, p.b.code_stride);
-  const bool staged = p.k > 0 && p.a.code_stride >= 0 && p.b.code_stride >= 0 && longest * 256 + p.k < (int64_t{1} << 31);
+  const bool staged = p.k > 0 && p.a.code_stride >= 0 && p.b.code_stride >= 0 && longest <= (INT32_MAX - p.k) / 256;
   const int rows = p.m <= 16 ? 16 : p.m <= 32 ? 32 : 64;
-  const int64_t pieces = tiles(p.n, 16) * tiles(p.m, rows) * (rows / 16) * p.batch;
-  if (!staged || (p.m <= 32 && pieces <= (p.k < 256 ? 2048 : 512))) {
-    const dim3 grid(static_cast<unsigned>(tiles(p.n, 16)), static_cast<unsigned>(tiles(p.m, rows)), p.batch);
-    if (rows == 16) thin_kernel<1, 8, kF32><<<grid, 512, 0, s>>>(p);
-    else if (rows == 32) thin_kernel<2, 4, kF32><<<grid, 256, 0, s>>>(p);
-    else thin_kernel<4, 4, kF32><<<grid, 256, 0, s>>>(p);
-    return hipGetLastError();
-  }
-  const int64_t middle = tiles(p.m, 128) * tiles(p.n, 128) * p.batch, wide = tiles(p.m, 256) * tiles(p.n, 256) * p.batch;
-  if (tiles(p.m, 64) * tiles(p.n, 64) * p.batch <= 512) return launch_staged<64, 2, 2, 2, kF32>(p, tiles(p.m, 64), tiles(p.n, 64), s);
-  if (middle <= 256) return launch_staged<128, 2, 2, 2, kF32>(p, tiles(p.m, 128), tiles(p.n, 128), s);
+  const int64_t pieces = tiles_of(p.n, 16) * tiles_of(p.m, rows) * (rows / 16) * p.batch;
+  if (!staged || (p.m <= 32 && pieces <= (p.k < 256 ? 2048 : 512)))
+    return rows == 16 ? Fp8Kernel::k16Rows : rows == 32 ? Fp8Kernel::k32Rows : Fp8Kernel::k64Rows;
+  const int64_t middle = tiles_of(p.m, 128) * tiles_of(p.n, 128) * p.batch, wide = tiles_of(p.m, 256) * tiles_of(p.n, 256) * p.batch;
+  if (tiles_of(p.m, 64) * tiles_of(p.n, 64) * p.batch <= 512) return Fp8Kernel::k64TwoGroups;
+  if (middle <= 256) return Fp8Kernel::k128TwoGroups;
   // (large tiles that few rows or columns leave half empty are no gain)
-  if (middle > 512 && wide * 4 <= middle + middle / 4) return launch_staged<256, 2, 4, 1, kF32>(p, tiles(p.m, 256), tiles(p.n, 256), s);
-  return launch_staged<128, 2, 2, 1, kF32>(p, tiles(p.m, 128), tiles(p.n, 128), s);
+  return middle > 512 && wide * 4 <= middle + middle / 4 ? Fp8Kernel::k256 : Fp8Kernel::k128;
 }
-
-}  // namespace
 
 hipError_t launch_fp8_matmul(const Fp8Product& p, hipStream_t s) { return p.f32 ? launch<true>(p, s) : launch<false>(p, s); }
 
