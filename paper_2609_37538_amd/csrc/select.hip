@@ -142,15 +142,15 @@ __global__ __launch_bounds__(kWaves * 64, 2) void score_kernel(SelectParams p, i
     const int page = p.cache.table ? p.cache.table[at] : static_cast<int>(at);
     return page < p.cache.pages ? page : -1;
   };
-  const int pages = kWhole ? page_of(min(first_key + lane * kTileKeys, most - 1)) : 0;
+  const int pages = kWhole ? page_of(seen_key(first_key + lane * kTileKeys, most)) : 0;
   const int64_t in_row = quad * 32, to_scale = kKeyScaleAt - quad * 32;
   // (No branch: a wave that may skip a load has to wait for all of them;
   // and nothing is done with a loaded value here, which would wait for it.  Keys past the last one that is seen read as
   // it; in place of rows that do not exist the pool's first one is read.)
   auto fetch = [&](int tile) {
     Keys k;
-    const int key = min(first_key + tile * kTileKeys + l16, most - 1);
-    const int page = kWhole ? __builtin_amdgcn_readlane(pages, min(tile, tiles - 1)) : page_of(key);
+    const int key = seen_key(first_key + tile * kTileKeys + l16, most);
+    const int page = kWhole ? __builtin_amdgcn_readlane(pages, paged_tile(tile, tiles)) : page_of(key);
     const bool there = page >= 0;
     uint64_t row = p.cache.base + (there ? page * p.cache.page_stride : 0);
     row += (there ? key & p.cache.page_mask : 0) * p.cache.row_stride + in_row;
@@ -275,7 +275,7 @@ __global__ __launch_bounds__(kChunkWaves * 64, kTiles > 4 ? 2 : 4) void chunk_ke
   bool part_there;
   // (a row's page is looked up a stage before the row is loaded)
   int page;
-  auto key_of = [&](int stage) { return min(first_key + stage * kStageKeys + my_row, most - 1); };
+  auto key_of = [&](int stage) { return seen_key(first_key + stage * kStageKeys + my_row, most); };
   auto page_of = [&](int stage) {
     const int64_t at = static_cast<int64_t>(r) * p.cache.pages_per_request + (key_of(stage) >> p.cache.page_shift);
     page = p.cache.table ? p.cache.table[at] : static_cast<int>(at);
@@ -697,33 +697,20 @@ __global__ __launch_bounds__(kThreads) void best_kernel(SelectParams p) {
 }
 
 template <int kTiles, int kTok>
-hipError_t run_scores(const SelectParams& p, hipStream_t s) {
-  const int groups = (p.tokens + kTok - 1) / kTok;
-  const int waves_on_tokens = groups >= kWaves ? kWaves : 1;
-  const int64_t tiles = (static_cast<int64_t>(p.longest) + kTileKeys - 1) / kTileKeys;
-  // runs in eights of tiles, the largest block
-  const int64_t waves = 2048, per_group = std::max<int64_t>(1, waves / (static_cast<int64_t>(p.requests) * groups));
-  int64_t run_tiles = std::max<int64_t>(8, (tiles + per_group - 1) / per_group);
-  run_tiles = std::min<int64_t>(64, (run_tiles + 7) / 8 * 8);
-  const int64_t runs = (tiles + run_tiles - 1) / run_tiles;
-  const int64_t run_groups = (runs * waves_on_tokens + kWaves - 1) / kWaves, token_groups = (groups + waves_on_tokens - 1) / waves_on_tokens;
+hipError_t run_scores(const SelectParams& p, const ScorePlan& plan, hipStream_t s) {
+  const int waves_on_keys = kWaves / plan.waves_on_tokens;
+  const int64_t run_groups = (plan.runs + waves_on_keys - 1) / waves_on_keys;
+  const int64_t token_groups = (plan.groups + plan.waves_on_tokens - 1) / plan.waves_on_tokens;
   const int64_t total = run_groups * token_groups * p.requests;
   const auto kernel = p.cache.page_shift >= 4 ? &score_kernel<kTiles, kTok, true> : &score_kernel<kTiles, kTok, false>;
-  kernel<<<dim3(static_cast<unsigned>(total)), kWaves * 64, 0, s>>>(p, static_cast<int>(run_tiles), static_cast<int>(runs), groups,
-                                                                    waves_on_tokens);
+  kernel<<<dim3(static_cast<unsigned>(total)), kWaves * 64, 0, s>>>(p, plan.run, plan.runs, plan.groups, plan.waves_on_tokens);
   return hipGetLastError();
 }
 
 template <int kTiles>
-hipError_t run_chunk(const SelectParams& p, hipStream_t s) {
-  const int groups = (p.tokens + kChunkWaves - 1) / kChunkWaves;
-  const int64_t stages = (static_cast<int64_t>(p.longest) + kStageKeys - 1) / kStageKeys;
-  // runs of up to 16 stages, in pairs of them (the largest block)
-  const int64_t per_group = std::max<int64_t>(1, 1024 / (static_cast<int64_t>(p.requests) * groups));
-  const int64_t run_stages = std::min<int64_t>(16, ((stages + per_group - 1) / per_group + 1) / 2 * 2);
-  const int64_t runs = (stages + run_stages - 1) / run_stages;
-  chunk_kernel<kTiles><<<dim3(static_cast<unsigned>(runs * groups * p.requests)), kChunkWaves * 64, 0, s>>>(
-      p, static_cast<int>(run_stages), static_cast<int>(runs), groups);
+hipError_t run_chunk(const SelectParams& p, const ScorePlan& plan, hipStream_t s) {
+  const int64_t total = static_cast<int64_t>(plan.runs) * plan.groups * p.requests;
+  chunk_kernel<kTiles><<<dim3(static_cast<unsigned>(total)), kChunkWaves * 64, 0, s>>>(p, plan.run, plan.runs, plan.groups);
   return hipGetLastError();
 }
 
@@ -742,23 +729,40 @@ hipError_t run_best(const SelectParams& p, hipStream_t s) {
 //       64 x 4 x 64              41.7     44.8             64 x 8 x 16              51.7     34.1
 //        8 x 6 x 64              23.5     22.0              1 x 64 x 64             24.1     22.5
 // (a wave on its own holds two tokens, so few tokens waste less of it than of a workgroup for eight.)
+ScorePlan score_plan(int requests, int tokens, int heads, int longest) {
+  ScorePlan plan{};
+  const int tiles = (heads + 15) / 16;
+  plan.head_tiles = tiles == 1 ? 1 : tiles == 2 ? 2 : tiles <= 4 ? 4 : 8;
+  plan.shared = tokens >= (tiles <= 2 ? 4 : 6);
+  plan.tokens = plan.shared ? kChunkWaves : tiles > 4 || tokens == 1 ? 1 : 2;
+  plan.groups = (tokens + plan.tokens - 1) / plan.tokens;
+  plan.waves_on_tokens = plan.shared ? kChunkWaves : plan.groups >= kWaves ? kWaves : 1;
+  const int64_t all = static_cast<int64_t>(requests) * plan.groups, unit = plan.shared ? kStageKeys : kTileKeys;
+  const int64_t units = (longest + unit - 1) / unit, per_group = std::max<int64_t>(1, (plan.shared ? 1024 : 2048) / all);
+  const int64_t run = (units + per_group - 1) / per_group;
+  // runs of up to 16 stages in pairs of them, or of up to 64 tiles in eights: the largest block
+  plan.run = static_cast<int>(plan.shared ? std::min<int64_t>(16, (run + 1) / 2 * 2) : std::min<int64_t>(64, std::max<int64_t>(8, (run + 7) / 8 * 8)));
+  plan.runs = static_cast<int>((units + plan.run - 1) / plan.run);
+  return plan;
+}
+
 hipError_t launch_scores(const SelectParams& p, hipStream_t s) {
-  const int tiles = (p.heads + 15) / 16;
-  if (p.tokens >= (tiles <= 2 ? 4 : 6)) {
-    if (tiles == 1) return run_chunk<1>(p, s);
-    if (tiles == 2) return run_chunk<2>(p, s);
-    if (tiles <= 4) return run_chunk<4>(p, s);
-    return run_chunk<8>(p, s);
+  const ScorePlan plan = score_plan(p.requests, p.tokens, p.heads, p.longest);
+  if (plan.shared) {
+    if (plan.head_tiles == 1) return run_chunk<1>(p, plan, s);
+    if (plan.head_tiles == 2) return run_chunk<2>(p, plan, s);
+    if (plan.head_tiles == 4) return run_chunk<4>(p, plan, s);
+    return run_chunk<8>(p, plan, s);
   }
-  if (tiles > 4) return run_scores<8, 1>(p, s);
-  if (p.tokens == 1) {
-    if (tiles == 1) return run_scores<1, 1>(p, s);
-    if (tiles == 2) return run_scores<2, 1>(p, s);
-    return run_scores<4, 1>(p, s);
+  if (plan.head_tiles == 8) return run_scores<8, 1>(p, plan, s);
+  if (plan.tokens == 1) {
+    if (plan.head_tiles == 1) return run_scores<1, 1>(p, plan, s);
+    if (plan.head_tiles == 2) return run_scores<2, 1>(p, plan, s);
+    return run_scores<4, 1>(p, plan, s);
   }
-  if (tiles == 1) return run_scores<1, 2>(p, s);
-  if (tiles == 2) return run_scores<2, 2>(p, s);
-  return run_scores<4, 2>(p, s);
+  if (plan.head_tiles == 1) return run_scores<1, 2>(p, plan, s);
+  if (plan.head_tiles == 2) return run_scores<2, 2>(p, plan, s);
+  return run_scores<4, 2>(p, plan, s);
 }
 
 hipError_t launch_best(const SelectParams& p, hipStream_t s) {
@@ -771,3 +775,10 @@ hipError_t launch_best(const SelectParams& p, hipStream_t s) {
 }
 
 }  // namespace avsg
+
+int32_t avsg_internal_score_row(int32_t first_key, int32_t tiles, int32_t tile, int32_t lane, int32_t most, int32_t page_shift) {
+  const int key = avsg::seen_key(first_key + tile * avsg::kTileKeys + lane, most);
+  if (page_shift < 4 || page_shift > 30) return key;
+  const int paged = avsg::seen_key(first_key + avsg::paged_tile(tile, tiles) * avsg::kTileKeys, most);
+  return (paged >> page_shift << page_shift) + (key & ((1 << page_shift) - 1));
+}

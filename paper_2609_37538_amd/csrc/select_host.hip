@@ -176,4 +176,10 @@ avsg_status avsg_select(const avsg_key_cache* cache, const avsg_selection* a, vo
   return AVSG_OK;
 }
 
+int64_t avsg_internal_score_plan(int32_t requests, int32_t tokens, int32_t heads, int32_t longest) {
+  const ScorePlan p = score_plan(requests, tokens, heads, longest);
+  const int how = 100 * p.head_tiles + (p.shared ? 0 : 10 * p.waves_on_tokens + p.tokens);
+  return static_cast<int64_t>(how) | static_cast<int64_t>(p.run) << 32;
+}
+
 }  // extern "C"

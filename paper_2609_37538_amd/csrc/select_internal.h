@@ -56,9 +56,34 @@ __device__ __forceinline__ int seen_by(const SelectParams& p, int r, int g) {
   return n < 0 ? 0 : n < p.longest ? static_cast<int>(n) : p.longest;
 }
 
+// How the scores of a turn are computed: by waves on their own (with `run` tiles of sixteen keys each), or by workgroups
+// that share their keys (`run` stages of 64).
+struct ScorePlan {
+  bool shared;
+  int32_t head_tiles;        // sixteen heads each: 1, 2, 4 or 8
+  int32_t tokens;            // of a wave on its own, or of a workgroup
+  int32_t groups;            // of so many tokens
+  int32_t waves_on_tokens;   // waves of a workgroup that take different ones
+  int32_t run, runs;         // what a wave or workgroup goes through, and how many of these the positions make
+};
+
+// The key that is read in place of `key` (a tile's or a stage's, of which some may lie past the last one that a token
+// sees), and the tile of a run in whose page a tile's keys are read where none lies in two (tiles past the last are
+// loaded, but not used).
+__host__ __device__ inline int seen_key(int key, int most) { return key < most ? key : most - 1; }
+__host__ __device__ inline int paged_tile(int tile, int tiles) { return tile < tiles ? tile : tiles - 1; }
+
 hipError_t launch_key_append(const KeyAppendParams& p, int rope_style, hipStream_t s);
 hipError_t launch_key_read(const ReadParams& p, hipStream_t s);
+ScorePlan score_plan(int requests, int tokens, int heads, int longest);
 hipError_t launch_scores(const SelectParams& p, hipStream_t s);
 hipError_t launch_best(const SelectParams& p, hipStream_t s);
 
 }  // namespace avsg
+
+// score_plan for tests, which assert what their cases run: 100 * head_tiles + 10 * waves_on_tokens + tokens of a wave on
+// its own, or 100 * head_tiles where they share their keys, in the low half, the run's length in the high one.  Not part of
+// the ABI.
+extern "C" int64_t avsg_internal_score_plan(int32_t requests, int32_t tokens, int32_t heads, int32_t longest);
+// The position whose row lane `lane` of sixteen reads for tile `tile` of a run of `tiles` from first_key.  Likewise.
+extern "C" int32_t avsg_internal_score_row(int32_t first_key, int32_t tiles, int32_t tile, int32_t lane, int32_t most, int32_t page_shift);
