@@ -120,10 +120,10 @@ size_t avsg_select_workspace_least(int32_t longest, int32_t block);
 
 /* Selects, for each query token, the K / block blocks of `block` positions with the
  * best scores, ties going to the lowest, and writes their positions in ascending
- * order.  A block's score is the largest of its positions'.  What ranks lowest,
- * as minus infinity: positions at or past the token's length (a negative length is 0),
- * rows that do not exist, scores that are NaN.  What ranks highest, as infinity: the
- * positions of [0, first) and [len - recent, len) that the token sees.  So with fewer than K
+ * order.  A block's score is the largest of its positions'.  A position's is, by the first of
+ * these that holds: minus infinity at or past the token's length (a negative length is 0);
+ * infinity in [0, first) and [len - recent, len), whatever its row is; minus infinity where the
+ * row does not exist or the score is NaN; the score.  So with fewer than K
  * positions to see, the selection goes on with the lowest others, and the K entries are
  * distinct positions below `longest` in any case: what avsg_step takes, and what
  * avsg_attend masks by their position.

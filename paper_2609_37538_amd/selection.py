@@ -235,7 +235,7 @@ class KeyCache:
         q: int8 [B][n_q][H][128] codes, weights: float32 [B][n_q][H] (append's q_out and weights_out).
         lens: int64 [B][n_q] positions a query token may see, or None: all.
         longest: positions [0, longest) are ranked, None: all rows of a request.
-        first, recent: positions [0, first) and [len - recent, len) that are always taken.
+        first, recent: positions [0, first) and [len - recent, len) that are always taken, whatever their rows are.
         workspace: uint8 tensor to use in place of a new one (at least avsg_select_workspace_least)."""
         dev, torch = self.device, _L._t
         _need(q.dim() == 4, "q must be [batch][n_q][heads][128]")

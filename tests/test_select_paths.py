@@ -1,6 +1,7 @@
 """Every kernel of a selection's scores, through runs of keys as long as large calls have them, on cases that the
-choice gives it now; and which rows they read."""
+choice gives it now; which rows they read; and what the positions that are always taken have precedence over."""
 import ctypes
+import math
 
 import pytest
 import torch
@@ -92,3 +93,25 @@ def test_rows_that_no_token_sees_are_not_addressed(page):
                         if tile < tiles:
                             assert row == min(key, most - 1)
                         assert f(first, tiles, tile, lane, most, 2) == f(first, tiles, tile, lane, most, 31) == min(key, most - 1)
+
+
+@gpu
+@pytest.mark.parametrize("n_q", [1, 2, 7])
+@pytest.mark.parametrize("block", [1, 16])
+def test_always_taken_whatever_the_row_is(n_q, block):
+    """Positions of `first` and `recent` that a token sees are taken, also where the row does not exist or its score is
+    NaN; those that it does not see are not ranked by them."""
+    g = torch.Generator().manual_seed(n_q)
+    q, weights, pool, table = made(g, 1, n_q, 8, 8, 64)
+    table[0, 0], table[0, 4] = -1, 8
+    pool[table[0, 3].long(), 40, 128:] = 255          # a scale of NaN at position 232
+    lens = torch.full((1, n_q), 300)
+    kw = dict(topk=128, block=block, first=5, recent=70)
+    cache = S.KeyCache(pool.cuda(), 1, page_table=table.cuda())
+    got = cache.select(q.cuda(), weights.cuda(), lens=lens.cuda(), **kw)
+    check(got, R.select(q, weights, pool, table, lens, **kw))
+    for t in range(n_q):
+        picked = set(got[0][0, t].tolist())
+        assert set(range(5)) <= picked and set(range(230, 300)) <= picked
+        best = got[1][0, t]
+        assert int((best == math.inf).sum()) == (75 if block == 1 else 6)
