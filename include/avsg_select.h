@@ -3,9 +3,12 @@
  *
  * A row of the key cache is one token position's index key, AVSG_KEY_ROW_BYTES
  * bytes: AVSG_KEY_DIM codes of 8 bits (two's complement, -127 to 127), then one
- * float32 scale; value = code * scale.  It is the second kind of row that
- * avsg_step moves (row_bytes 132).  Queries are codes alike; what their scale
- * multiplies stands in their weights.
+ * float32 scale; value = code * scale.  Rows of this size are the second kind that
+ * avsg_step moves (row_bytes 132), which does not look into them.  The codes here are whole
+ * numbers: rows with codes in 8-bit floating point have the same size, are not told
+ * apart, and would be scored as whole numbers; only rows of avsg_key_append_rows, or of its
+ * form, belong into a cache.  Queries are codes alike; what their scale multiplies
+ * stands in their weights.
  *
  * A query token t has several index queries (heads) q[t][h] with weights w[t][h];
  * all meet the same keys.  The score of position p is
@@ -13,8 +16,10 @@
  *   s[t][p] = float32( scale[p] * sum over h of w[t][h] * max(0, q[t][h] . key[p]) ),
  *
  * where the products of codes add up exactly in whole numbers and the sum over
- * the heads in 64 bits.  So a score does not depend on how the work is split, and a
- * selection is the same for one token as for a chunk of them.
+ * the heads in 64 bits, always in the same order.  So a score does not depend on how the work is
+ * split, and a selection is the same for one token as for a chunk of them.  A score is off the
+ * exact one by its rounding to float32 and by at most 2^-47 of the sum of its terms'
+ * magnitudes (35 roundings to 64 bits); positions that are closer than that may rank either way.
  *
  * Conventions are those of avsg_latent.h: the caller owns all memory, the calls are
  * asynchronous on the given stream, allocate nothing, never throw or abort, can

@@ -224,7 +224,8 @@ __global__ __launch_bounds__(kWaves * 64, 2) void score_kernel(SelectParams p, i
 // they share in LDS, 64 keys at a time, while the next ones are on their way.
 constexpr int kChunkWaves = 8;
 constexpr int kStageKeys = 64;
-// 2048 tokens of 64 heads over 16384 keys each take 340 us, 1.5 POP/s.  What bounds it is the issue of instructions: per sixteen
+// 2048 tokens of 64 heads that see 14337 to 16384 keys each take 340 us, 1.5 POP/s; with 128 heads the selection takes
+// 672 us in place of 378, with 80 heads 653 (they are taken in 1, 2, 4 or 8 sixteens).  What bounds it is the issue of instructions: per sixteen
 // heads and keys two matrix instructions (each takes about two places of the others) and eight for the sums, relu and weight
 // (sum in 64 bits: 32-bit sums would take as many), 63% of the cycles, and with the matrix instructions 78%.
 // Reads of LDS without bank conflicts (9% of the cycles have one), 128 keys at a time, and other orders of the
@@ -373,9 +374,13 @@ constexpr uint32_t kSample = 4096, kSampleMost = 16384;   // (by 1024 threads)
 // wanted reach; one pass over all scores keeps these; the threshold lies in one of 2048 bins of equal width of
 // theirs, and the scores of that bin are compared with each other.  The blocks above the threshold, and those at it, are
 // marked in bit maps, from whose prefix sums each finds its place in the result.
+// 2048 of 131072 scores take 23 us by the clock of the workgroup: sample 5.7, its bins 2.0, the pass 7.6, what it kept
+// 2.6, their bins 1.7, comparisons 1.2, marks 2.5; of 32768 (128 workgroups) 16: 3.7, 1.7, 2.9, 2.4, 1.7, 1.0, 3.0.
 // Where that does not do (no bound that leaves few enough, as with many equal scores; more wanted than are
-// kept) histograms of all scores' bits narrow the threshold's range down until a bin holds one value or all that is
-// wanted, reading the scores again for each.
+// kept, 7000 of 32768 already) histograms of all scores' bits narrow the threshold's range down until a bin holds one
+// value or all that is wanted, reading the scores again for each.  That takes longer: selections of 128 tokens of 64 heads
+// over 32768 positions 128 us in place of 79 (7000 wanted), 112 (all scores equal), 4 tokens over 131072 positions 244 in
+// place of 41 (16384 wanted), 188 (all equal), 276 (one head, whose scores are zero for half of the keys).
 // kMarks: blocks that are marked, and placed, at a time; kCandidates: scores that are kept from the one pass over all.
 template <int kThreads, int kMarks, uint32_t kCandidates>
 __global__ __launch_bounds__(kThreads) void best_kernel(SelectParams p) {
@@ -485,7 +490,8 @@ __global__ __launch_bounds__(kThreads) void best_kernel(SelectParams p) {
     if (!all) {
       float bound = -FLT_MAX;
       // Of the sample as many as are wanted of all, four and a half standard deviations and three more: too few in one
-      // of 300000 tokens.  It is larger where it would not hold 128 of those wanted.
+      // of 300000 tokens where a score does not depend on its position.  (Where it does, too few or too many may reach the
+      // bound more often; then all scores are read again, below.)  It is larger where it would not hold 128 of those wanted.
       constexpr int kMine = kSampleMost / 1024;
       uint32_t sample = kSample;
       while (sample < kMine * kThreads && static_cast<uint64_t>(want) * sample < uint64_t{128} * seen) sample *= 2;

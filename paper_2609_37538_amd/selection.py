@@ -3,7 +3,8 @@ same entry points, argument marshalling only, and :class:`KeyCache`, which takes
 torch tensors.
 
 A :class:`KeyCache` describes rows of 8-bit index keys (a paged pool, the second
-buffers of an :class:`~paper_2609_37538_amd.avsg.Operator`, or host rows); it
+buffers of an :class:`~paper_2609_37538_amd.avsg.Operator`, or host rows), whose codes are
+whole numbers (not 8-bit floating point); it
 appends to them, reads them back, and selects the positions that an operator's
 step and :meth:`~paper_2609_37538_amd.latent.LatentCache.attend` take.  The methods
 run on the current stream of their tensors' GPU and raise ValueError for tensors
