@@ -231,7 +231,8 @@ def fp8_matmul(a: Fp8, b: Fp8, out=None, dtype=None):
     if out.shape != shape or out.device != dev or (shape[-1] > 1 and st[-1] != 1):
         raise ValueError(f"out must be {shape} on {dev} with contiguous rows")
     kind = _plain_type(out, "out")
-    _L._outputs(out, "out", sa[0] if three else 1, st[0], shape[-2], st[-2], shape[-1])
+    if not out.is_contiguous():
+        _L._outputs("out", sa[0] if three else 1, st[0], shape[-2], st[-2], shape[-1])
     _L._run(_lib.avsg_fp8_matmul, "avsg_fp8_matmul", dev.index, a._c(), b._c(), sa[0] if three else 1, shape[-2], shape[-1], sa[-1],
             out.data_ptr(), kind, st[-2], st[0] if three else 0)
     return out

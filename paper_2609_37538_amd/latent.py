@@ -224,10 +224,10 @@ def _apart(n0: int, s0: int, n1: int, s1: int, run: int) -> bool:
     return True
 
 
-def _outputs(x, what: str, n0: int, s0: int, n1: int, s1: int, run: int) -> None:
-    """Refuses a tensor to write to of which several entries are one place in memory: which of their values stays is
-    left to chance."""
-    if not x.is_contiguous() and not _apart(n0, s0, n1, s1, run):
+def _outputs(what: str, n0: int, s0: int, n1: int, s1: int, run: int) -> None:
+    """Refuses a tensor to write to (not a contiguous one) of which several entries are one place in memory: which of
+    their values stays is left to chance."""
+    if not _apart(n0, s0, n1, s1, run):
         raise ValueError(f"{what}: entries must not share memory")
 
 
@@ -312,7 +312,8 @@ class LatentCache:
             shape = (t, q_rope.shape[1], AVSG_ROPE_DIM)
             qa, qs = _vectors(q_rope, shape, dev, "q_rope")
             oa, os_ = _vectors(q_out, shape, dev, "q_out")
-            _outputs(q_out, "q_out", t, os_[0], shape[1], os_[1], AVSG_ROPE_DIM)
+            if not q_out.is_contiguous():
+                _outputs("q_out", t, os_[0], shape[1], os_[1], AVSG_ROPE_DIM)
             a = AvsgAppend(t, la, ls[0], ra, rs[0], req, pos, ang, turns, style, shape[1], qa, qs[0], qs[1], oa, os_[0], os_[1])
         _run(_lib.avsg_kv_append, "avsg_kv_append", dev.index, self.c, a)
 
@@ -324,7 +325,8 @@ class LatentCache:
         if out is None:
             out = _t.empty((n, KEY_DIM), dtype=_t.bfloat16, device=dev)
         at, st = _vectors(out, (n, KEY_DIM), dev, "out")
-        _outputs(out, "out", n, st[0], 1, 0, KEY_DIM)
+        if not out.is_contiguous():
+            _outputs("out", n, st[0], 1, 0, KEY_DIM)
         _run(_lib.avsg_kv_read, "avsg_kv_read", dev.index, self.c, n, req, pos, at, st[0])
         return out
 
@@ -359,7 +361,8 @@ class LatentCache:
             oa, ot, oh = out.data_ptr(), heads * AVSG_LATENT_DIM, AVSG_LATENT_DIM
         else:
             oa, ot, oh = _tokens(out, (b, n_q, heads, AVSG_LATENT_DIM), dev, "out")
-            _outputs(out, "out", b * n_q, ot, heads, oh, AVSG_LATENT_DIM)
+            if not out.is_contiguous():
+                _outputs("out", b * n_q, ot, heads, oh, AVSG_LATENT_DIM)
         if lse is None:
             lse = _t.empty((b, n_q, heads), dtype=_t.float32, device=dev)
             lse_at = lse.data_ptr()
@@ -529,7 +532,8 @@ def mx4_matmul(a: Mx4, b: Mx4, out=None, dtype=None):
     if out.shape != shape or out.device != dev or (shape[-1] > 1 and st[-1] != 1):
         raise ValueError(f"out must be {shape} on {dev} with contiguous rows")
     kind = _plain_type(out, "out")
-    _outputs(out, "out", sa[0] if three else 1, st[0], shape[-2], st[-2], shape[-1])
+    if not out.is_contiguous():
+        _outputs("out", sa[0] if three else 1, st[0], shape[-2], st[-2], shape[-1])
     _run(_lib.avsg_mx4_matmul, "avsg_mx4_matmul", dev.index, a._c(), b._c(), sa[0] if three else 1, shape[-2], shape[-1],
          sa[-1], out.data_ptr(), kind, st[-2], st[0] if three else 0)
     return out

@@ -209,8 +209,10 @@ class KeyCache:
             wa, ws = (None, 0) if weights is None else _weights(weights, shape[:2], dev, "weights")
             oa, ot, oh = _codes(q_out, shape, dev, "q_out")
             va, vs = _weights(weights_out, shape[:2], dev, "weights_out")
-            _L._outputs(q_out, "q_out", t, ot, shape[1], oh, AVSG_KEY_DIM)
-            _L._outputs(weights_out, "weights_out", t, vs, 1, 0, shape[1])
+            if not q_out.is_contiguous():
+                _L._outputs("q_out", t, ot, shape[1], oh, AVSG_KEY_DIM)
+            if not weights_out.is_contiguous():
+                _L._outputs("weights_out", t, vs, 1, 0, shape[1])
             a = AvsgKeyAppend(t, ka, ks[0], req, pos, ang, turns, style, rope_at, shape[1], qa, qs[0], qs[1], wa, ws, oa, ot, oh,
                               va, vs)
         _L._run(_lib.avsg_key_append_rows, "avsg_key_append_rows", dev.index, self.c, a)
@@ -223,7 +225,8 @@ class KeyCache:
         if out is None:
             out = _L._t.empty((n, AVSG_KEY_DIM), dtype=_L._t.bfloat16, device=dev)
         at, st = _L._vectors(out, (n, AVSG_KEY_DIM), dev, "out")
-        _L._outputs(out, "out", n, st[0], 1, 0, AVSG_KEY_DIM)
+        if not out.is_contiguous():
+            _L._outputs("out", n, st[0], 1, 0, AVSG_KEY_DIM)
         _L._run(_lib.avsg_key_read_rows, "avsg_key_read_rows", dev.index, self.c, n, req, pos, at, st[0])
         return out
 
